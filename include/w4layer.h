@@ -13,7 +13,8 @@
  *   layer_decode      one token per sequence against a cache  (Sec. 4.4)
  *
  * plus the KV-cache calls kv_layout / kv_append (the in-place Concat of
- * Sec. 4.6.3), layer stacks (stack_*), and the model ends around the layers
+ * Sec. 4.6.3), the same cache held in 4 bits with the attention that reads it
+ * (kv4_*), layer stacks (stack_*), and the model ends around the layers
  * (lm_*: embedding, LM head and greedy sampling of the runtime loop, Sec. 2).
  *
  * Conventions shared by every call
@@ -81,6 +82,10 @@ extern "C" {
 #define W4_WEIGHTS_INT8 1   /* 8-bit codes, one fp16 scale (and, asymmetric,
                                one zero point) per output column             */
 #define W4_WEIGHTS_BF16 2   /* unquantised bf16 weights                       */
+
+/* ---- cache formats (layer_set_kv_format) ----------------------------------- */
+#define W4_KV_BF16 0   /* bf16, the kv_layout layout                           */
+#define W4_KV_INT4 1   /* 4-bit codes in groups of 32 dims, the kv4_layout one */
 
 /* ---- types ---------------------------------------------------------------- */
 
@@ -411,6 +416,106 @@ int model_decode_greedy(const layer_t* layers, int32_t n_layers, lm_t lm, const 
 int kv_append(const kv_desc* desc, void* k_cache, void* v_cache,
               const void* k_new, const void* v_new, int32_t B, int32_t T,
               const int32_t* slot_start, void* stream);
+
+/* ---- the KV cache in 4 bits ------------------------------------------------ */
+
+/* A K or V cache that holds 4-bit codes: 5 bits a value with their
+ * parameters, 80 bytes for a token's 128 values of one kv head against 256 in
+ * bf16.  The dims of a head are cut into groups of 32; of the values x of one
+ * token's group, taken as fp16 (exact for magnitudes 2^-17 .. 65280), the
+ * cache holds
+ *     lo = min x,   s = fp16((max x - lo) / 15),
+ *     c  = min(15, floor((x - lo) / s + 1/2))     (0 where s = 0),
+ * and the value that it stands for is lo + s c: within s/2 of x, plus the
+ * rounding of 15 s.  The codes are those of exact arithmetic.  A group with a
+ * value that has no fp16 value (NaN, an infinity, beyond 65504) reads back as
+ * NaN in all its places.
+ * The order of the bytes is private to the library: a cache is batch x
+ * n_kv_heads blocks (strides in bytes, multiples of 16) of ceil(max_seq / 32)
+ * tiles of 32 tokens.  Caches start at any content; what kv4_append has not
+ * written may hold anything.
+ *
+ * Every kv4_ call takes cache, key / value, query and output pointers that are
+ * 16-byte aligned, and checks its arguments on the host before anything is
+ * launched.  Calls are asynchronous on the stream, allocate nothing and may be
+ * captured into a graph (the host's slot_start is then part of the graph).  Two
+ * calls that write the same sequence's cache, or one that writes what another
+ * reads, must be ordered by the caller; different sequences of a cache may be
+ * written at once. */
+typedef struct kv4_desc {
+    int32_t batch;
+    int32_t n_kv_heads;
+    int32_t max_seq;
+    int32_t head_dim;     /* 64 or 128 */
+    int64_t stride_b;     /* bytes between sequences */
+    int64_t stride_h;     /* bytes between kv heads */
+    size_t  bytes;        /* of one cache (K or V) */
+} kv4_desc;
+
+/* The layout for a batch of sequences (pure host computation; of cfg it reads
+ * n_kv_heads, head_dim and max_seq).  Errors: W4_EINVAL, W4_EUNSUPPORTED
+ * (head_dim). */
+int kv4_layout(const layer_config* cfg, int32_t batch, kv4_desc* out);
+
+/* Quantise new keys / values k_new, v_new (bf16 [B][T][n_kv_heads][head_dim],
+ * device) into slots slot_start[b] .. slot_start[b]+T-1 of sequence b.
+ * slot_start is a host array [B].  No other slot changes.  Deterministic.
+ * Errors: W4_EINVAL, W4_ECAPACITY (slot range outside the cache or
+ * B > desc->batch), W4_EHIP. */
+int kv4_append(const kv4_desc* desc, void* k_cache, void* v_cache,
+               const void* k_new, const void* v_new, int32_t B, int32_t T,
+               const int32_t* slot_start, void* stream);
+
+/* The same for one token per sequence (k_new, v_new bf16
+ * [B][n_kv_heads][head_dim]) at the slots ctx_lens (int32 [B], device), as the
+ * decode calls take them.  A slot outside 0 .. max_seq-1 (a padded row of
+ * the batch) is not written.  Errors: W4_EINVAL, W4_ECAPACITY, W4_EHIP. */
+int kv4_append_step(const kv4_desc* desc, void* k_cache, void* v_cache,
+                    const void* k_new, const void* v_new, int32_t B,
+                    const int32_t* ctx_lens, void* stream);
+
+/* Read slots slot_start[b] .. slot_start[b]+T-1 of sequence b back into k_out,
+ * v_out (bf16 [B][T][n_kv_heads][head_dim], device): the values lo + s c,
+ * rounded once.  Errors: as kv4_append. */
+int kv4_read(const kv4_desc* desc, const void* k_cache, const void* v_cache,
+             int32_t B, int32_t T, const int32_t* slot_start,
+             void* k_out, void* v_out, void* stream);
+
+/* Attention over a 4-bit cache, n_heads query heads on the cache's kv heads
+ * (n_heads a multiple of n_kv_heads, at most 8 per kv head), scores scaled by
+ * head_dim^-1/2:
+ *   out[r][h] = sum_j softmax_j(q[r][h] . K_j / sqrt(head_dim) [+ mask_j]) V_j
+ * with K, V the values lo + s c.  q and out are bf16 [rows][n_heads][head_dim],
+ * out rounded once; softmax statistics and sums are fp32, a product's operands
+ * fp16 (codes and q exact, weights and, in the prefill, keys and values
+ * within 2^-11).  Deterministic.
+ *
+ * kv4_attn_decode: one query for each of B sequences, row b attends to slots
+ * 0 .. ctx_lens[b] (int32 [B] device, every one <= max_ctx), which are
+ * already written.  ctx_lens[b] = -1 (a padded row) gives a zero row.
+ *   attn_mask  fp32 [B][max_seq] device, added to the scores (finite or
+ *              -inf), or NULL; hidden slots (-inf) may hold anything, a row
+ *              whose slots are all hidden gives zeros;
+ *   ws         at least kv4_attn_workspace_size(desc, n_heads, 2, B, 1, max_ctx).
+ *
+ * kv4_attn_prefill: T >= 1 queries of one sequence (k_cache, v_cache: that
+ * sequence's part of the cache) after hist_len >= 0 cached tokens; query t
+ * attends to slots 0 .. hist_len+t, which are already written.
+ *   ws         at least kv4_attn_workspace_size(desc, n_heads, 1, 1, T, hist_len).
+ *
+ * The workspace may hold anything, and belongs to one call at a time.
+ * kv4_attn_workspace_size: stage 0 or 1 for the prefill, 2 for the decode, as in
+ * layer_workspace_size; 0 for invalid arguments.  It does not decrease with B, T
+ * or max_ctx.
+ * Errors: W4_EINVAL, W4_ECAPACITY (B > desc->batch, slots beyond max_seq),
+ * W4_EUNSUPPORTED (heads), W4_EWORKSPACE, W4_EHIP. */
+size_t kv4_attn_workspace_size(const kv4_desc* desc, int32_t n_heads, int32_t stage, int32_t B, int32_t T,
+                               int32_t max_ctx);
+int kv4_attn_decode(const kv4_desc* desc, const void* q, const int32_t* ctx_lens, int32_t max_ctx,
+                    const float* attn_mask, int32_t B, int32_t n_heads, const void* k_cache, const void* v_cache,
+                    void* out, void* ws, size_t ws_bytes, void* stream);
+int kv4_attn_prefill(const kv4_desc* desc, const void* q, int32_t T, int32_t hist_len, int32_t n_heads,
+                     const void* k_cache, const void* v_cache, void* out, void* ws, size_t ws_bytes, void* stream);
 
 /* ---- diagnostics ------------------------------------------------------- */
 

@@ -1,0 +1,85 @@
+"""CPU oracle for the key/value cache held in 4 bits.
+
+TEST INFRASTRUCTURE ONLY.  Only the tests may import this module; the product
+path never does, and this module imports nothing from the product path.
+
+Per token and kv head the dims are cut into groups of 32.  Of a group's values
+x, taken as fp16:  lo = min x,  s = fp16((max x - lo) / 15),
+c = min(15, floor((x - lo) / s + 1/2)) (0 where s = 0); the value held is
+lo + s c.  A group with a value that has no fp16 value is NaN throughout.
+
+Everything is fp64 and unrounded, except where the definition rounds.  fp64
+holds the differences and borders exactly: fp16 values are multiples of 2^-24
+below 2^16 (41 bits), a border (k + 1/2) s has 16 bits.
+
+Pins: tests/test_oracle_kv4.py checks each function against rational
+arithmetic and closed forms; none is "parity unpinned".
+"""
+from __future__ import annotations
+
+import numpy as np
+
+F64 = np.float64
+GROUP = 32
+
+
+def quantise(x):
+    """codes, s, lo of values [..][d]: uint8 [..][d], fp64 [..][d / 32] twice."""
+    x = np.asarray(x, dtype=F64)
+    with np.errstate(over="ignore", invalid="ignore"):
+        x = x.astype(np.float16).astype(F64)
+    g = x.reshape(x.shape[:-1] + (-1, GROUP))
+    bad = ~np.isfinite(g).all(-1)
+    g = np.where(bad[..., None], 0.0, g)
+    lo, hi = g.min(-1), g.max(-1)
+    s = ((hi - lo) / 15).astype(np.float16).astype(F64)
+    t = g - lo[..., None]
+    with np.errstate(divide="ignore", invalid="ignore"):
+        c = np.where(s[..., None] > 0, np.floor(t / s[..., None] + 0.5), 0.0)
+    c = np.minimum(c, 15).astype(np.uint8)
+    nan = np.where(bad, np.nan, 0.0)
+    return c.reshape(x.shape), s + nan, lo + nan
+
+
+def values(codes, s, lo) -> np.ndarray:
+    g = codes.astype(F64).reshape(codes.shape[:-1] + (-1, GROUP))
+    return (lo[..., None] + s[..., None] * g).reshape(codes.shape)
+
+
+def held(x) -> np.ndarray:
+    """The values a cache holds of x."""
+    return values(*quantise(x))
+
+
+def attend(q, k, v, seen, add=None, key_eps: float = 0.0):
+    """Attention of q [nq][d] over keys / values k, v [nkv][n][d] (fp64),
+    seen [n] bool, add [n] (the mask's values) or None; the scores are scaled by
+    d^-1/2.  Returns out [nq][d] and a bound on the error of a computation in
+    which the scores' sums are fp32, every key is off by at most key_eps
+    relative to its group's largest magnitude, and weights and values are each
+    rounded to fp16; without the rounding of the result:
+
+      a score is off by at most e = (key_eps + (d + 16) 2^-24) 3 sum|q| max|k| / sqrt(d)
+      (3: s, lo and code are multiplied apart, each part at most 2 max|k|, in
+      sum) plus 2^-21 max|score| (its scaling, the exponential's argument);
+      weights are then off by a factor within exp(2 e), and
+      |out error| <= sum_j w_j |v_j| (exp(2 e) - 1 + 2^-11 + 2^-11 + 2^-14) + 2^-24 (1 + max|v|)
+      (2^-14: the exponential and the fp32 sums of the weights)."""
+    nq, d = q.shape
+    nkv, n, _ = k.shape
+    r = nq // nkv
+    out, tol = np.zeros((nq, d)), np.zeros((nq, d))
+    if not np.any(seen):
+        return out, tol
+    for h in range(nq):
+        kk, vv = k[h // r][seen], v[h // r][seen]
+        z = kk @ q[h] / np.sqrt(d)
+        e = (key_eps + (d + 16) * 2.0 ** -24) * 3 * np.abs(q[h]).sum() * np.abs(kk).max() / np.sqrt(d)
+        e += 2.0 ** -21 * np.abs(z).max()
+        if add is not None:
+            z = z + add[seen]
+        p = np.exp(z - z.max())
+        w = p / p.sum()
+        out[h] = w @ vv
+        tol[h] = (w @ np.abs(vv)) * (np.expm1(2 * e) + 2.0 ** -10 + 2.0 ** -14) + 2.0 ** -24 * (1 + np.abs(vv).max())
+    return out, tol

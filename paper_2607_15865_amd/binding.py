@@ -80,6 +80,12 @@ class kv_desc(ctypes.Structure):
                 ("stride_s", ctypes.c_int64), ("bytes", ctypes.c_size_t)]
 
 
+class kv4_desc(ctypes.Structure):
+    _fields_ = [("batch", ctypes.c_int32), ("n_kv_heads", ctypes.c_int32), ("max_seq", ctypes.c_int32),
+                ("head_dim", ctypes.c_int32), ("stride_b", ctypes.c_int64), ("stride_h", ctypes.c_int64),
+                ("bytes", ctypes.c_size_t)]
+
+
 _P = ctypes.c_void_p
 _I = ctypes.c_int32
 _SIG = {
@@ -95,6 +101,14 @@ _SIG = {
     "layer_decode_noalloc": (ctypes.c_int, [_P, _P, _P, _P, _I, _P, _I, _P, _P, _P, _P]),
     "layer_decode_noalloc_max_bytes": (ctypes.c_size_t, []),
     "kv_append": (ctypes.c_int, [ctypes.POINTER(kv_desc), _P, _P, _P, _P, _I, _I, _P, _P]),
+    "kv4_layout": (ctypes.c_int, [ctypes.POINTER(layer_config), _I, ctypes.POINTER(kv4_desc)]),
+    "kv4_append": (ctypes.c_int, [ctypes.POINTER(kv4_desc), _P, _P, _P, _P, _I, _I, _P, _P]),
+    "kv4_append_step": (ctypes.c_int, [ctypes.POINTER(kv4_desc), _P, _P, _P, _P, _I, _P, _P]),
+    "kv4_read": (ctypes.c_int, [ctypes.POINTER(kv4_desc), _P, _P, _I, _I, _P, _P, _P, _P]),
+    "kv4_attn_workspace_size": (ctypes.c_size_t, [ctypes.POINTER(kv4_desc), _I, _I, _I, _I, _I]),
+    "kv4_attn_decode": (ctypes.c_int, [ctypes.POINTER(kv4_desc), _P, _P, _I, _P, _I, _I, _P, _P, _P, _P,
+                                       ctypes.c_size_t, _P]),
+    "kv4_attn_prefill": (ctypes.c_int, [ctypes.POINTER(kv4_desc), _P, _I, _I, _I, _P, _P, _P, _P, ctypes.c_size_t, _P]),
     "layer_debug_dequant": (ctypes.c_int, [_P, _I, _P, _P]),
     "layer_set_decode_path": (ctypes.c_int, [_P, _I]),
     "layer_set_gemm_plan": (ctypes.c_int, [_P, _I, _I, _I, _I, _I]),
@@ -293,6 +307,44 @@ def kv_append(desc: kv_desc, k_cache, v_cache, k_new, v_new, B, T, slot_start, s
     ss = np.ascontiguousarray(np.asarray(slot_start, dtype=np.int32))
     return _lib.kv_append(ctypes.byref(desc), _ptr(k_cache), _ptr(v_cache), _ptr(k_new), _ptr(v_new), B, T,
                           ss.ctypes.data, _stream(stream))
+
+
+def kv4_layout(cfg, batch: int):
+    d = kv4_desc()
+    rc = _lib.kv4_layout(ctypes.byref(make_config(cfg)), batch, ctypes.byref(d))
+    return rc, d
+
+
+def kv4_append(desc: kv4_desc, k_cache, v_cache, k_new, v_new, B, T, slot_start, stream=None) -> int:
+    ss = np.ascontiguousarray(np.asarray(slot_start, dtype=np.int32))
+    return _lib.kv4_append(ctypes.byref(desc), _ptr(k_cache), _ptr(v_cache), _ptr(k_new), _ptr(v_new), B, T,
+                           ss.ctypes.data, _stream(stream))
+
+
+def kv4_append_step(desc: kv4_desc, k_cache, v_cache, k_new, v_new, B, ctx_lens, stream=None) -> int:
+    return _lib.kv4_append_step(ctypes.byref(desc), _ptr(k_cache), _ptr(v_cache), _ptr(k_new), _ptr(v_new), B,
+                                _ptr(ctx_lens), _stream(stream))
+
+
+def kv4_read(desc: kv4_desc, k_cache, v_cache, B, T, slot_start, k_out, v_out, stream=None) -> int:
+    ss = np.ascontiguousarray(np.asarray(slot_start, dtype=np.int32))
+    return _lib.kv4_read(ctypes.byref(desc), _ptr(k_cache), _ptr(v_cache), B, T, ss.ctypes.data, _ptr(k_out),
+                         _ptr(v_out), _stream(stream))
+
+
+def kv4_attn_workspace_size(desc: kv4_desc, n_heads, stage, B, T, max_ctx) -> int:
+    return _lib.kv4_attn_workspace_size(ctypes.byref(desc), n_heads, stage, B, T, max_ctx)
+
+
+def kv4_attn_decode(desc: kv4_desc, q, ctx_lens, max_ctx, attn_mask, B, n_heads, k_cache, v_cache, out, ws, ws_bytes,
+                    stream=None) -> int:
+    return _lib.kv4_attn_decode(ctypes.byref(desc), _ptr(q), _ptr(ctx_lens), max_ctx, _ptr(attn_mask), B, n_heads,
+                                _ptr(k_cache), _ptr(v_cache), _ptr(out), _ptr(ws), ws_bytes, _stream(stream))
+
+
+def kv4_attn_prefill(desc: kv4_desc, q, T, hist_len, n_heads, k_cache, v_cache, out, ws, ws_bytes, stream=None) -> int:
+    return _lib.kv4_attn_prefill(ctypes.byref(desc), _ptr(q), T, hist_len, n_heads, _ptr(k_cache), _ptr(v_cache),
+                                 _ptr(out), _ptr(ws), ws_bytes, _stream(stream))
 
 
 def layer_debug_dequant(handle, which, out, stream=None) -> int:
@@ -596,3 +648,123 @@ class Stack:
         ws, n = self.workspace(STAGE_DECODE, B, 1, max_ctx)
         check(stack_decode(self.handles, x, pos, ctx_lens, max_ctx, attn_mask, B, k_caches, v_caches, y, ws, n,
                            stream))
+
+
+class KV4Cache:
+    """A K and a V cache in 4 bits (kv4_layout(cfg, batch)) with the operators
+    over them; methods raise W4Error for what the library refuses and
+    ValueError for tensors that do not fit.
+
+    Keys, values, queries and outputs are contiguous bf16 tensors (or 16-bit
+    integers holding the bits) on the cache's device, which must be the current
+    one.  Calls run on ``stream`` (default: torch's current stream).  A call's
+    workspace is kept per stream; under graph capture it is allocated in the
+    capture, so that every graph has its own."""
+
+    def __init__(self, cfg, batch: int):
+        import torch
+        rc, self.desc = kv4_layout(cfg, batch)
+        check(rc)
+        self.n_heads = cfg.n_heads
+        self.k = torch.empty(self.desc.bytes, dtype=torch.uint8, device="cuda")
+        self.v = torch.empty(self.desc.bytes, dtype=torch.uint8, device="cuda")
+        self._ws = {}
+        self._grown = []                 # outgrown workspaces: graphs and other streams may still use them
+
+    def _tensor(self, t, shape, what, dtypes=None):
+        import torch
+        if tuple(t.shape) != tuple(shape):
+            raise ValueError(f"{what}: shape {tuple(t.shape)}, expected {tuple(shape)}")
+        if t.dtype not in (dtypes or (torch.bfloat16, torch.int16, torch.uint16)):
+            raise ValueError(f"{what}: dtype {t.dtype}")
+        if t.device != self.k.device:
+            raise ValueError(f"{what} is on {t.device}, the cache on {self.k.device}")
+        if not t.is_contiguous():
+            raise ValueError(f"{what} must be contiguous")
+
+    def _here(self):
+        import torch
+        if torch.cuda.current_device() != self.k.device.index:
+            raise ValueError(f"the cache is on {self.k.device}, the current device is {torch.cuda.current_device()}")
+
+    def _workspace(self, stage, B, T, max_ctx, stream):
+        import torch
+        n = kv4_attn_workspace_size(self.desc, self.n_heads, stage, B, T, max_ctx)
+        if n == 0:
+            raise W4Error(W4_EINVAL, layer_last_error())
+        if torch.cuda.is_current_stream_capturing():
+            return torch.empty(n, dtype=torch.uint8, device=self.k.device), n
+        key = _stream(stream)
+        ws = self._ws.get(key)
+        if ws is None or ws.numel() < n:
+            if ws is not None:
+                self._grown.append(ws)
+                n = max(n, 2 * ws.numel())
+            ws = self._ws[key] = torch.empty(n, dtype=torch.uint8, device=self.k.device)
+        return ws, ws.numel()
+
+    def _slots(self, slot_start, B):
+        if len(slot_start) != B:
+            raise ValueError(f"{len(slot_start)} slots for {B} sequences")
+
+    def append(self, k_new, v_new, slot_start, stream=None):
+        """k_new, v_new [B][T][n_kv_heads][head_dim] into slots slot_start[b] .. + T - 1 (host integers)."""
+        B, T = k_new.shape[:2]
+        shape = (B, T, self.desc.n_kv_heads, self.desc.head_dim)
+        self._tensor(k_new, shape, "k_new")
+        self._tensor(v_new, shape, "v_new")
+        self._slots(slot_start, B)
+        self._here()
+        check(kv4_append(self.desc, self.k, self.v, k_new, v_new, B, T, slot_start, stream))
+
+    def append_step(self, k_new, v_new, ctx_lens, stream=None):
+        """One token per sequence, k_new, v_new [B][1][n_kv_heads][head_dim] (or without the 1), into slots ctx_lens
+        (int32 [B] on the device)."""
+        import torch
+        B = k_new.shape[0]
+        shape = (B, 1, self.desc.n_kv_heads, self.desc.head_dim) if k_new.dim() == 4 else \
+            (B, self.desc.n_kv_heads, self.desc.head_dim)
+        self._tensor(k_new, shape, "k_new")
+        self._tensor(v_new, shape, "v_new")
+        self._tensor(ctx_lens, (B,), "ctx_lens", (torch.int32,))
+        self._here()
+        check(kv4_append_step(self.desc, self.k, self.v, k_new, v_new, B, ctx_lens, stream))
+
+    def read(self, slot_start, T, k_out, v_out, stream=None):
+        """Slots slot_start[b] .. + T - 1 as bf16 values into k_out, v_out [B][T][n_kv_heads][head_dim]."""
+        B = k_out.shape[0]
+        shape = (B, T, self.desc.n_kv_heads, self.desc.head_dim)
+        self._tensor(k_out, shape, "k_out")
+        self._tensor(v_out, shape, "v_out")
+        self._slots(slot_start, B)
+        self._here()
+        check(kv4_read(self.desc, self.k, self.v, B, T, slot_start, k_out, v_out, stream))
+
+    def attn_decode(self, q, ctx_lens, max_ctx, out, attn_mask=None, stream=None):
+        """One query per sequence: q, out [B][n_heads][head_dim], slots 0 .. ctx_lens[b] (int32 [B] on the device)."""
+        import torch
+        B = q.shape[0]
+        shape = (B, self.n_heads, self.desc.head_dim)
+        self._tensor(q, shape, "q")
+        self._tensor(out, shape, "out")
+        self._tensor(ctx_lens, (B,), "ctx_lens", (torch.int32,))
+        if attn_mask is not None:
+            self._tensor(attn_mask, (B, self.desc.max_seq), "attn_mask", (torch.float32,))
+        self._here()
+        ws, n = self._workspace(STAGE_DECODE, B, 1, max_ctx, stream)
+        check(kv4_attn_decode(self.desc, q, ctx_lens, max_ctx, attn_mask, B, self.n_heads, self.k, self.v, out, ws, n,
+                              stream))
+
+    def attn_prefill(self, q, hist_len, out, row: int = 0, stream=None):
+        """T queries of sequence `row` after hist_len tokens: q, out [T][n_heads][head_dim]."""
+        T = q.shape[0]
+        shape = (T, self.n_heads, self.desc.head_dim)
+        self._tensor(q, shape, "q")
+        self._tensor(out, shape, "out")
+        if not 0 <= row < self.desc.batch:
+            raise ValueError(f"row {row} of a cache of {self.desc.batch} sequences")
+        self._here()
+        ws, n = self._workspace(STAGE_PREFILL_KV, 1, T, hist_len, stream)
+        off = row * self.desc.stride_b
+        check(kv4_attn_prefill(self.desc, q, T, hist_len, self.n_heads, self.k.data_ptr() + off,
+                               self.v.data_ptr() + off, out, ws, n, stream))

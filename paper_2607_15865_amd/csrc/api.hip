@@ -10,6 +10,7 @@
 #include <cstdio>
 #include <cstdarg>
 #include <cstring>
+#include <initializer_list>
 #include <mutex>
 #include <string>
 #include <thread>
@@ -19,6 +20,7 @@
 #include "../../include/w4layer.h"
 #include "common.h"
 #include "decode_fused.h"
+#include "kv4.h"
 #include "launch.h"
 #include "lm.h"
 
@@ -382,7 +384,7 @@ int check_device() {
 
 int load_kernels() {
     if (load_gemm_w4_qkv() || load_gemm_w4_resid() || load_gemm_w4_swiglu() || load_gemv_w4() || load_attention() ||
-        load_misc() || load_decode_fused() || load_lm())
+        load_misc() || load_decode_fused() || load_lm() || load_kv4() || load_kv4_attn())
         return fail(W4_EHIP, "kernels not loaded: %s", hipGetErrorString(hipGetLastError()));
     return W4_OK;
 }
@@ -1265,6 +1267,189 @@ int kv_append(const kv_desc* desc, void* kc, void* vc, const void* k_new, const 
                          desc->n_kv_heads, desc->head_dim, desc->stride_b, desc->stride_h, slot_start,
                          (hipStream_t)stream))
         return fail(W4_EHIP, "kv_append launch failed: %s", hipGetErrorString(hipGetLastError()));
+    return W4_OK;
+}
+
+// ---------------------------------------------------------------- 4-bit cache
+
+static bool aligned16(std::initializer_list<const void*> ps) {
+    for (const void* p : ps)
+        if ((uintptr_t)p % 16) return false;
+    return true;
+}
+
+static int check_kv4(const kv4_desc* d, int32_t B) {
+    if (d->batch < 1 || d->n_kv_heads < 1 || d->max_seq < 1) return fail(W4_EINVAL, "bad kv4_desc");
+    if (d->head_dim != 64 && d->head_dim != 128) return fail(W4_EUNSUPPORTED, "head_dim must be 64 or 128");
+    const int64_t tiles = ((int64_t)d->max_seq + KV4_TILE - 1) / KV4_TILE;
+    if (d->stride_h % 16 || d->stride_b % 16 || d->stride_h < tiles * kv4_tile_bytes(d->head_dim) ||
+        d->stride_b < d->stride_h * d->n_kv_heads)
+        return fail(W4_EINVAL, "bad kv4_desc strides");
+    if (B < 1) return fail(W4_EINVAL, "B must be >= 1");
+    if (B > d->batch || B > 65535 || d->n_kv_heads > 65535) return fail(W4_ECAPACITY, "B = %d exceeds the cache batch", B);
+    return W4_OK;
+}
+
+// Checks and launches of kv4_append (slot_start) and kv4_read; rows in lots of KV4_ROWS.
+static int kv4_store(const kv4_desc* d, const void* kc, const void* vc, const void* kx, const void* vx, int32_t B,
+                     int32_t T, const int32_t* slot_start, bool read, void* stream) {
+    if (!d || !kc || !vc || !kx || !vx || !slot_start) return fail(W4_EINVAL, "null argument");
+    int rc;
+    if ((rc = check_kv4(d, B))) return rc;
+    if (T < 1) return fail(W4_EINVAL, "T must be >= 1");
+    if (!aligned16({kc, vc, kx, vx})) return fail(W4_EINVAL, "pointers must be 16-byte aligned");
+    for (int b = 0; b < B; b++)
+        if (slot_start[b] < 0 || (long long)slot_start[b] + T > d->max_seq)
+            return fail(W4_ECAPACITY, "slots %d..%lld of sequence %d outside max_seq %d", slot_start[b],
+                        (long long)slot_start[b] + T - 1, b, d->max_seq);
+    Kv4StoreArgs a{};
+    a.stride_b = d->stride_b;
+    a.stride_h = d->stride_h;
+    a.x_h = d->head_dim;
+    a.x_t = (long long)d->n_kv_heads * d->head_dim;
+    a.x_b = a.x_t * T;
+    a.max_seq = d->max_seq;
+    a.T = T;
+    a.nkv = d->n_kv_heads;
+    a.d = d->head_dim;
+    for (int b0 = 0; b0 < B; b0 += KV4_ROWS) {
+        a.B = std::min(KV4_ROWS, B - b0);
+        a.k = (uint8_t*)kc + b0 * d->stride_b;
+        a.v = (uint8_t*)vc + b0 * d->stride_b;
+        a.k_x = (uint16_t*)kx + b0 * a.x_b;
+        a.v_x = (uint16_t*)vx + b0 * a.x_b;
+        std::copy(slot_start + b0, slot_start + b0 + a.B, a.slots.v);
+        if (read ? launch_kv4_read(a, (hipStream_t)stream) : launch_kv4_append(a, (hipStream_t)stream))
+            return fail(W4_EHIP, "kernel launch failed: %s", hipGetErrorString(hipGetLastError()));
+    }
+    return W4_OK;
+}
+
+int kv4_layout(const layer_config* cfg, int32_t batch, kv4_desc* out) {
+    if (!cfg || !out) return fail(W4_EINVAL, "null argument");
+    if (batch < 1) return fail(W4_EINVAL, "batch must be >= 1");
+    if (cfg->n_kv_heads <= 0 || cfg->max_seq <= 0) return fail(W4_EINVAL, "bad config");
+    if (cfg->head_dim != 64 && cfg->head_dim != 128) return fail(W4_EUNSUPPORTED, "head_dim must be 64 or 128");
+    out->batch = batch;
+    out->n_kv_heads = cfg->n_kv_heads;
+    out->max_seq = cfg->max_seq;
+    out->head_dim = cfg->head_dim;
+    out->stride_h = ((int64_t)cfg->max_seq + KV4_TILE - 1) / KV4_TILE * kv4_tile_bytes(cfg->head_dim);
+    out->stride_b = out->stride_h * cfg->n_kv_heads;
+    out->bytes = (size_t)out->stride_b * batch;
+    return W4_OK;
+}
+
+int kv4_append(const kv4_desc* desc, void* kc, void* vc, const void* k_new, const void* v_new, int32_t B, int32_t T,
+               const int32_t* slot_start, void* stream) {
+    return kv4_store(desc, kc, vc, k_new, v_new, B, T, slot_start, false, stream);
+}
+
+int kv4_read(const kv4_desc* desc, const void* kc, const void* vc, int32_t B, int32_t T, const int32_t* slot_start,
+             void* k_out, void* v_out, void* stream) {
+    return kv4_store(desc, kc, vc, k_out, v_out, B, T, slot_start, true, stream);
+}
+
+int kv4_append_step(const kv4_desc* d, void* kc, void* vc, const void* k_new, const void* v_new, int32_t B,
+                    const int32_t* ctx_lens, void* stream) {
+    if (!d || !kc || !vc || !k_new || !v_new || !ctx_lens) return fail(W4_EINVAL, "null argument");
+    int rc;
+    if ((rc = check_kv4(d, B))) return rc;
+    if (!aligned16({kc, vc, k_new, v_new})) return fail(W4_EINVAL, "pointers must be 16-byte aligned");
+    Kv4StoreArgs a{};
+    a.k = (uint8_t*)kc;
+    a.v = (uint8_t*)vc;
+    a.stride_b = d->stride_b;
+    a.stride_h = d->stride_h;
+    a.k_x = (uint16_t*)k_new;
+    a.v_x = (uint16_t*)v_new;
+    a.x_h = d->head_dim;
+    a.x_t = a.x_b = (long long)d->n_kv_heads * d->head_dim;
+    a.slots_dev = ctx_lens;
+    a.max_seq = d->max_seq;
+    a.B = B;
+    a.T = 1;
+    a.nkv = d->n_kv_heads;
+    a.d = d->head_dim;
+    if (launch_kv4_append(a, (hipStream_t)stream))
+        return fail(W4_EHIP, "kernel launch failed: %s", hipGetErrorString(hipGetLastError()));
+    return W4_OK;
+}
+
+static int check_kv4_heads(const kv4_desc* d, int32_t n_heads) {
+    if (n_heads < 1) return fail(W4_EINVAL, "n_heads must be >= 1");
+    if (n_heads % d->n_kv_heads) return fail(W4_EUNSUPPORTED, "n_heads must be a multiple of n_kv_heads");
+    if (n_heads / d->n_kv_heads > 8) return fail(W4_EUNSUPPORTED, "at most 8 query heads per kv head");
+    return W4_OK;
+}
+
+size_t kv4_attn_workspace_size(const kv4_desc* d, int32_t n_heads, int32_t stage, int32_t B, int32_t T,
+                               int32_t max_ctx) {
+    if (!d || stage < 0 || stage > 2 || max_ctx < 0 || check_kv4(d, stage == 2 ? B : 1) || check_kv4_heads(d, n_heads))
+        return 0;
+    if (stage != 2 && T < 1) return 0;
+    return 256;
+}
+
+// The parts of an attention call that both forms share.
+static Kv4AttnArgs kv4_attn_args(const kv4_desc* d, const void* q, int32_t n_heads, const void* kc, const void* vc,
+                                 void* out) {
+    Kv4AttnArgs a{};
+    a.q = (const uint16_t*)q;
+    a.k = (const uint8_t*)kc;
+    a.v = (const uint8_t*)vc;
+    a.stride_h = d->stride_h;
+    a.out = out;
+    a.nq = n_heads;
+    a.nkv = d->n_kv_heads;
+    a.d = d->head_dim;
+    a.max_seq = d->max_seq;
+    a.scale = (float)(1.0 / std::sqrt((double)d->head_dim));
+    return a;
+}
+
+int kv4_attn_decode(const kv4_desc* d, const void* q, const int32_t* ctx_lens, int32_t max_ctx, const float* attn_mask,
+                    int32_t B, int32_t n_heads, const void* kc, const void* vc, void* out, void* ws, size_t ws_bytes,
+                    void* stream) {
+    if (!d || !q || !ctx_lens || !kc || !vc || !out || !ws) return fail(W4_EINVAL, "null pointer argument");
+    int rc;
+    if ((rc = check_kv4(d, B)) || (rc = check_kv4_heads(d, n_heads))) return rc;
+    if (max_ctx < 0) return fail(W4_EINVAL, "max_ctx must be >= 0");
+    if ((long long)max_ctx + 1 > d->max_seq)
+        return fail(W4_ECAPACITY, "max_ctx + 1 = %lld exceeds max_seq %d", (long long)max_ctx + 1, d->max_seq);
+    if (!aligned16({q, kc, vc, out, ws})) return fail(W4_EINVAL, "pointers must be 16-byte aligned");
+    if (q == out) return fail(W4_EINVAL, "q and out must not alias");
+    const size_t need = kv4_attn_workspace_size(d, n_heads, 2, B, 1, max_ctx);
+    if (ws_bytes < need) return fail(W4_EWORKSPACE, "workspace %zu bytes, need %zu", ws_bytes, need);
+    Kv4AttnArgs a = kv4_attn_args(d, q, n_heads, kc, vc, out);
+    a.stride_b = d->stride_b;
+    a.ctx_lens = ctx_lens;
+    a.max_ctx = max_ctx;
+    a.mask = attn_mask;
+    a.rows = B;
+    if (launch_kv4_attn(a, (hipStream_t)stream))
+        return fail(W4_EHIP, "kernel launch failed: %s", hipGetErrorString(hipGetLastError()));
+    return W4_OK;
+}
+
+int kv4_attn_prefill(const kv4_desc* d, const void* q, int32_t T, int32_t hist_len, int32_t n_heads, const void* kc,
+                     const void* vc, void* out, void* ws, size_t ws_bytes, void* stream) {
+    if (!d || !q || !kc || !vc || !out || !ws) return fail(W4_EINVAL, "null pointer argument");
+    int rc;
+    if ((rc = check_kv4(d, 1)) || (rc = check_kv4_heads(d, n_heads))) return rc;
+    if (T < 1 || hist_len < 0) return fail(W4_EINVAL, "T must be >= 1 and hist_len >= 0");
+    if ((long long)hist_len + T > d->max_seq)
+        return fail(W4_ECAPACITY, "hist_len + T = %lld exceeds max_seq %d", (long long)hist_len + T, d->max_seq);
+    if (!aligned16({q, kc, vc, out, ws})) return fail(W4_EINVAL, "pointers must be 16-byte aligned");
+    if (q == out) return fail(W4_EINVAL, "q and out must not alias");
+    const size_t need = kv4_attn_workspace_size(d, n_heads, 1, 1, T, hist_len);
+    if (ws_bytes < need) return fail(W4_EWORKSPACE, "workspace %zu bytes, need %zu", ws_bytes, need);
+    Kv4AttnArgs a = kv4_attn_args(d, q, n_heads, kc, vc, out);
+    a.ctx_base = hist_len;
+    a.max_ctx = hist_len + T - 1;
+    a.rows = T;
+    if (launch_kv4_attn(a, (hipStream_t)stream))
+        return fail(W4_EHIP, "kernel launch failed: %s", hipGetErrorString(hipGetLastError()));
     return W4_OK;
 }
 
