@@ -1383,11 +1383,26 @@ static int check_kv4_heads(const kv4_desc* d, int32_t n_heads) {
     return W4_OK;
 }
 
+// Workspace of a decode: for the plan of any batch up to B and context up to max_ctx.
+struct Kv4DecodeWs {
+    size_t cnt, part, total;
+};
+static Kv4DecodeWs kv4_decode_ws(const kv4_desc* d, int32_t n_heads, int32_t B, int32_t max_ctx) {
+    const int r = n_heads / d->n_kv_heads;
+    Carve cv;
+    Kv4DecodeWs w;
+    w.cnt = cv.take(std::max((size_t)256, (size_t)B * d->n_kv_heads * 4));
+    w.part = cv.take(kv4_decode_part_bound(B, d->n_kv_heads, r, d->head_dim, max_ctx));
+    w.total = cv.off;
+    return w;
+}
+
 size_t kv4_attn_workspace_size(const kv4_desc* d, int32_t n_heads, int32_t stage, int32_t B, int32_t T,
                                int32_t max_ctx) {
     if (!d || stage < 0 || stage > 2 || max_ctx < 0 || check_kv4(d, stage == 2 ? B : 1) || check_kv4_heads(d, n_heads))
         return 0;
-    if (stage != 2 && T < 1) return 0;
+    if (stage == 2) return kv4_decode_ws(d, n_heads, B, max_ctx).total;
+    if (T < 1) return 0;
     return 256;
 }
 
@@ -1427,7 +1442,11 @@ int kv4_attn_decode(const kv4_desc* d, const void* q, const int32_t* ctx_lens, i
     a.max_ctx = max_ctx;
     a.mask = attn_mask;
     a.rows = B;
-    if (launch_kv4_attn(a, (hipStream_t)stream))
+    const Kv4DecodeWs w = kv4_decode_ws(d, n_heads, B, max_ctx);
+    a.nsplit = kv4_decode_plan(B, d->n_kv_heads, n_heads / d->n_kv_heads, d->head_dim, max_ctx).nsplit;
+    a.cnt = (unsigned*)((char*)ws + w.cnt);
+    a.part = (float*)((char*)ws + w.part);
+    if (launch_kv4_decode(a, false, (hipStream_t)stream))
         return fail(W4_EHIP, "kernel launch failed: %s", hipGetErrorString(hipGetLastError()));
     return W4_OK;
 }

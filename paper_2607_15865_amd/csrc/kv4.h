@@ -64,8 +64,19 @@ struct Kv4AttnArgs {
     int out_f16;
     int rows, nq, nkv, d;
     float scale;             // of the scores
+    int nsplit;              // decode: shares of a (row, kv head)'s tiles
+    float* part;             // share states, plan.part_bytes (nsplit > 1)
+    unsigned* cnt;           // arrival counters, plan.cnt_bytes (nsplit > 1)
     int* err;                // raised with W4_FLAG_F16_RANGE (out_f16), or null
 };
+struct Kv4DecodePlan {
+    int nsplit = 1;
+    size_t part_bytes = 0, cnt_bytes = 0;
+};
+Kv4DecodePlan kv4_decode_plan(int rows, int nkv, int r, int d, int max_ctx);
+size_t kv4_decode_part_bound(int rows, int nkv, int r, int d, int max_ctx);
+// zeroed: an earlier launch on the stream has cleared the counters
+int launch_kv4_decode(const Kv4AttnArgs& a, bool zeroed, hipStream_t stream);
 int launch_kv4_attn(const Kv4AttnArgs& a, hipStream_t stream);
 
 int load_kv4();
