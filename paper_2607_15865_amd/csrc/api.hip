@@ -1403,7 +1403,7 @@ size_t kv4_attn_workspace_size(const kv4_desc* d, int32_t n_heads, int32_t stage
         return 0;
     if (stage == 2) return kv4_decode_ws(d, n_heads, B, max_ctx).total;
     if (T < 1) return 0;
-    return 256;
+    return kv4_prefill_plan(T, max_ctx, d->n_kv_heads, n_heads / d->n_kv_heads, d->head_dim).part_bytes;
 }
 
 // The parts of an attention call that both forms share.
@@ -1467,7 +1467,8 @@ int kv4_attn_prefill(const kv4_desc* d, const void* q, int32_t T, int32_t hist_l
     a.ctx_base = hist_len;
     a.max_ctx = hist_len + T - 1;
     a.rows = T;
-    if (launch_kv4_attn(a, (hipStream_t)stream))
+    a.part = (float*)ws;
+    if (launch_kv4_prefill(a, (hipStream_t)stream))
         return fail(W4_EHIP, "kernel launch failed: %s", hipGetErrorString(hipGetLastError()));
     return W4_OK;
 }

@@ -66,6 +66,7 @@ struct Kv4AttnArgs {
     float scale;             // of the scores
     int nsplit;              // decode: shares of a (row, kv head)'s tiles
     float* part;             // share states, plan.part_bytes (nsplit > 1)
+    long long pf_units;      // prefill: set by the launcher
     unsigned* cnt;           // arrival counters, plan.cnt_bytes (nsplit > 1)
     int* err;                // raised with W4_FLAG_F16_RANGE (out_f16), or null
 };
@@ -77,7 +78,14 @@ Kv4DecodePlan kv4_decode_plan(int rows, int nkv, int r, int d, int max_ctx);
 size_t kv4_decode_part_bound(int rows, int nkv, int r, int d, int max_ctx);
 // zeroed: an earlier launch on the stream has cleared the counters
 int launch_kv4_decode(const Kv4AttnArgs& a, bool zeroed, hipStream_t stream);
-int launch_kv4_attn(const Kv4AttnArgs& a, hipStream_t stream);
+// Prefill: rows queries of one sequence after ctx_base tokens (part: part_bytes).
+struct Kv4PrefillPlan {
+    long long units = 0;     // stages of one kv head's row tiles
+    int blocks = 0;
+    size_t part_bytes = 0;   // grows with T and hist
+};
+Kv4PrefillPlan kv4_prefill_plan(int T, int hist, int nkv, int r, int d);
+int launch_kv4_prefill(const Kv4AttnArgs& a, hipStream_t stream);
 
 int load_kv4();
 int load_kv4_attn();

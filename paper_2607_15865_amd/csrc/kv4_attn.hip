@@ -21,6 +21,7 @@
 
 namespace {
 
+typedef float f32x2 __attribute__((ext_vector_type(2)));
 typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 
 constexpr float LOG2E = 1.4426950408889634f;
@@ -436,96 +437,414 @@ __global__ void __launch_bounds__(256) kv4_zero_kernel(unsigned* cnt, int n) {
     if (i < n) cnt[i] = 0u;
 }
 
-__device__ __forceinline__ float kv4_half(const uint8_t* p) {
-    return (float)__builtin_bit_cast(f16, *reinterpret_cast<const uint16_t*>(p));
+// ---------------------------------------------------------------- prefill
+
+// Rows are the (query, head) pairs of one kv head's group, r per query in
+// order, so a block's 256 rows are full whatever r is; wave w has rows 32 w ..
+// + 31.  Keys come in stages of 64: every thread unpacks two words of K and two
+// of V (d = 64: one) to fp16, s c + lo rounded once, and writes them to LDS in the
+// order of the 32x32x16 MFMAs' operand registers, 16 bytes a lane, where all
+// eight waves read them.  Scores are formed transposed, S^T = K Q^T, with the
+// keys of a tile in an order (bits 2 and 3 of the row index swapped) that leaves the weights
+// in the operand layout of P^T; a V word holds 8 tokens of one dim and is, once
+// unpacked, an operand of O^T = V^T P^T as it stands.  A lane owns one row: the
+// online softmax needs a lane exchange only when a maximum moves, which it does when a
+// score passes it by more than 8 (log2 units; weights stay below 2^8, in fp16).
+//
+// The stages of all row tiles of all kv heads form one line of work that the
+// blocks cut into equal runs, so that the blocks end together whatever the
+// causal lengths; a row tile that a cut parts leaves its pieces' states in the
+// workspace, and a second launch merges them in order.
+constexpr int PF_W = 8;                      // waves per block
+constexpr int PF_ROWS = 32 * PF_W;
+constexpr int PF_KST = 64;                   // keys per stage
+
+__host__ __device__ inline int pf_stages(int q, int R, int r, int hist) {     // of row tile q
+    const int last = (q + 1) * PF_ROWS < R ? (q + 1) * PF_ROWS - 1 : R - 1;
+    return (hist + last / r) / PF_KST + 1;
 }
 
-// One block per (row, query head); its four waves take the tiles in turn.
+// Row tile and first unit of the tile that holds unit u of a kv head (u below the
+// head's sum); whole waves call it.
+__device__ __forceinline__ void pf_find(const Kv4AttnArgs& a, int R, int r, long long u, int& q, long long& first) {
+    const int lane = threadIdx.x & 63, nqt = (R + PF_ROWS - 1) / PF_ROWS;
+    first = 0;
+    for (int q0 = 0;; q0 += 64) {
+        int x = q0 + lane < nqt ? pf_stages(q0 + lane, R, r, a.ctx_base) : 0;
+        const int own = x;
+#pragma unroll
+        for (int off = 1; off < 64; off *= 2) {              // inclusive sums over the lanes
+            const int y = __shfl_up(x, off, 64);
+            x += lane >= off ? y : 0;
+        }
+        const unsigned long long past = __builtin_amdgcn_ballot_w64(first + x > u);
+        if (past != 0 || q0 + 64 >= nqt) {
+            const int l = past != 0 ? __builtin_ctzll(past) : 0;
+            q = q0 + l;
+            first += __shfl(x - own, l, 64);
+            return;
+        }
+        first += __shfl(x, 63, 64);
+    }
+}
+
 template <int D>
-__global__ void __launch_bounds__(256) kv4_attn_kernel(Kv4AttnArgs a) {
-    constexpr int NS = D / 32, NV = D / 64;
-    __shared__ float qs[D], om[4][D], ml[4][2];
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-    const int b = blockIdx.x, head = blockIdx.y, g = head / (a.nq / a.nkv);
-    const int ctx = min(a.ctx_lens ? a.ctx_lens[b] : a.ctx_base + b, a.max_ctx);
-    const long long base = (long long)b * a.stride_b + (long long)g * a.stride_h;
-    if (tid < D) qs[tid] = bf16_bits_to_f32(a.q[((size_t)b * a.nq + head) * D + tid]);
-    __syncthreads();
-    const int j = lane & 31, hs = lane >> 5;                 // key of the tile, half of the dims
-    const int t = j >> 2 & 1, n16 = (j >> 3) << 2 | (j & 3);
-    float m = -INFINITY, l = 0.f, o[NV] = {};
-    for (int tile = wave; tile * KV4_TILE <= ctx; tile += 4) {
-        const uint8_t* kt = a.k + base + (long long)tile * kv4_tile_bytes(D);
-        const uint8_t* vt = a.v + base + (long long)tile * kv4_tile_bytes(D);
-        const int key = tile * KV4_TILE + j;
-        float sc = 0.f;
-#pragma unroll
-        for (int s = 0; s < NS; s++) {
-            const float ks = kv4_half(kt + kv4_code_bytes(D) + s * 128 + 2 * j);
-            const float lo = kv4_half(kt + kv4_code_bytes(D) + s * 128 + 64 + 2 * j);
-#pragma unroll
-            for (int qq = 0; qq < 2; qq++) {
-                const int q4 = 2 * hs + qq;
-                const uint32_t w = reinterpret_cast<const uint32_t*>(kt)[(t * 64 + q4 * 16 + n16) * NS + s];
-#pragma unroll
-                for (int e = 0; e < 8; e++)
-                    sc += qs[32 * s + 8 * q4 + e] * __builtin_fmaf((float)(w >> (4 * (e / 2) + 16 * (e % 2)) & 15u), ks, lo);
-            }
-        }
-        sc += __shfl_xor(sc, 32, 64);
-        sc *= a.scale;
-        bool seen = key <= ctx;
-        if (a.mask && seen) {
-            const float mk = a.mask[(size_t)b * a.max_seq + key];
-            seen = mk != -INFINITY;
-            sc += mk;
-        }
-        sc = seen ? sc : -INFINITY;
-        const float mn = fmaxf(m, wave_max(sc));
-        const float mb = mn == -INFINITY ? 0.f : mn;
-        const float alpha = m == -INFINITY ? 0.f : __expf(m - mb);
-        const float p = seen ? __expf(sc - mb) : 0.f;
-        l = l * alpha + 0.5f * wave_sum(p);
-        m = mn;
-#pragma unroll
-        for (int i = 0; i < NV; i++) o[i] *= alpha;
-        for (int k = 0; k < KV4_TILE; k++) {
-            const float pk = __shfl(p, k, 64);
-            if (pk == 0.f) continue;
-#pragma unroll
-            for (int i = 0; i < NV; i++) {
-                const int dim = lane + 64 * i, db = dim >> 4;
-                const uint32_t w = reinterpret_cast<const uint32_t*>(vt)[((db >> 2) * 64 + (k >> 3) * 16 + (dim & 15)) * 4 + (db & 3)];
-                const uint8_t* par = vt + kv4_code_bytes(D) + (dim >> 5) * 128 + 2 * k;
-                const int e = k & 7;
-                o[i] += pk * __builtin_fmaf((float)(w >> (4 * (e / 2) + 16 * (e % 2)) & 15u), kv4_half(par), kv4_half(par + 64));
-            }
-        }
-    }
-#pragma unroll
-    for (int i = 0; i < NV; i++) om[wave][lane + 64 * i] = o[i];
-    if (lane == 0) {
-        ml[wave][0] = m;
-        ml[wave][1] = l;
-    }
-    __syncthreads();
-    if (tid >= D) return;
-    float M = -INFINITY, L = 0.f, x = 0.f;
-    for (int w = 0; w < 4; w++) M = fmaxf(M, ml[w][0]);
-    for (int w = 0; w < 4; w++) {
-        const float f = ml[w][0] == -INFINITY ? 0.f : __expf(ml[w][0] - M);
-        L += f * ml[w][1];
-        x += f * om[w][tid];
-    }
-    x = L == 0.f ? 0.f : x / L;
-    const size_t oi = ((size_t)b * a.nq + head) * D + tid;
+constexpr int PF_NREG = 2 + 16 * (D / 32);   // floats of a lane's state: maximum, sum, output
+
+__device__ __forceinline__ float max_xor32(float v) {
+    const auto x = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    return fmaxf(__uint_as_float(x[0]), __uint_as_float(x[1]));
+}
+
+__device__ __forceinline__ int key_perm(int x) { return (x & ~12) | (x & 4) << 1 | (x & 8) >> 1; }   // swap bits 2 and 3
+
+template <int D, int N>
+__device__ __forceinline__ void pf_put(const Kv4AttnArgs& a, size_t off, const float (&x)[N], bool& bad) {   // 4 dims
+    uint2 w;
     if (a.out_f16) {
-        bool bad = false;
-        static_cast<f16*>(a.out)[oi] = act_f16(x, bad);
-        flag_range(a.err, bad);
+        f16 v[4];
+#pragma unroll
+        for (int j = 0; j < 4; j++) v[j] = act_f16(x[j], bad);
+        __builtin_memcpy(&w, v, 8);
     } else {
-        static_cast<uint16_t*>(a.out)[oi] = bf16_bits_rne(x);
+        w = uint2{(uint32_t)bf16_bits_rne(x[0]) | (uint32_t)bf16_bits_rne(x[1]) << 16,
+                  (uint32_t)bf16_bits_rne(x[2]) | (uint32_t)bf16_bits_rne(x[3]) << 16};
     }
+    *reinterpret_cast<uint2*>(static_cast<uint16_t*>(a.out) + off) = w;
+}
+
+template <int D>
+__global__ void __launch_bounds__(64 * PF_W) kv4_prefill_kernel(Kv4AttnArgs a) {
+    constexpr int NS = D / 32, NF = D / 16, NW = D / 64;     // groups, K fragments, words per thread
+    constexpr int TB = kv4_tile_bytes(D), CB = kv4_code_bytes(D);
+    constexpr int FB = 32 * D * 2;                           // bytes of a 32-key tile's fragments
+    extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
+    unsigned char* const Ks = smem;                          // [2 buffers][2 tiles][NF][64 lanes][16]
+    unsigned char* const Vs = smem + 4 * FB;                 // [2][2][NS][2][64][16]
+    unsigned long long* const vbad = reinterpret_cast<unsigned long long*>(smem + 8 * FB);   // [3][NS + 1] NaN keys of V, by stage % 3
+    const int tid = threadIdx.x, lane = tid & 63;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int h = lane >> 5, c = lane & 31;
+    const int r = a.nq / a.nkv, R = a.rows * r, nkeys = a.ctx_base + a.rows;
+    const int nqt = (R + PF_ROWS - 1) / PF_ROWS;
+    // this block's run of units
+    const long long total = a.pf_units * a.nkv;
+    long long u = total * blockIdx.x / gridDim.x;
+    const long long u1 = total * (blockIdx.x + 1) / gridDim.x;
+
+    // words of this thread: tile tt of the stage
+    const int tt = tid >> 8, w = tid & 255;
+    const int kL = w & 127, ksub = w >> 7;                   // K: lane slot t 64 + q4 16 + n16, words NW ksub ..
+    const int kkey = 8 * ((kL & 15) >> 2) + 4 * (kL >> 6) + (kL & 3), kq4 = kL >> 4 & 3;
+    const int vL = D == 128 ? w & 127 : w & 63, vsub = D == 128 ? w >> 7 : w >> 6;   // V: lane slot, words NW vsub ..
+    const int vn = vL & 15, vq4 = vL >> 4 & 3, vdb = D == 128 ? 4 * (vL >> 6) + 2 * vsub : vsub, vg = vdb >> 1;
+    uint32_t kw[NW], vw[NW];
+    uint16_t ksc[NW], klo[NW];
+    u32x4 vsc, vlo;
+    const uint8_t *kb = nullptr, *vb = nullptr;
+    auto load_raw = [&](int st) __attribute__((always_inline)) {
+        // (a tile past the last key's repeats that one: its keys are never seen)
+        const int tile = min(2 * st + tt, (nkeys - 1) / KV4_TILE);
+        const uint8_t* kt = kb + (long long)tile * TB;
+        const uint8_t* vt = vb + (long long)tile * TB;
+        if constexpr (NW == 2) {
+            const u32x2 x = *reinterpret_cast<const u32x2*>(kt + kL * 16 + ksub * 8);
+            const u32x2 y = *reinterpret_cast<const u32x2*>(vt + vL * 16 + vsub * 8);
+            kw[0] = x[0]; kw[1] = x[1];
+            vw[0] = y[0]; vw[1] = y[1];
+        } else {
+            kw[0] = *reinterpret_cast<const uint32_t*>(kt + kL * 8 + ksub * 4);
+            vw[0] = *reinterpret_cast<const uint32_t*>(vt + vL * 16 + vsub * 4);
+        }
+#pragma unroll
+        for (int i = 0; i < NW; i++) {
+            const uint8_t* pp = kt + CB + (NW * ksub + i) * 128 + 2 * kkey;
+            ksc[i] = *reinterpret_cast<const uint16_t*>(pp);
+            klo[i] = *reinterpret_cast<const uint16_t*>(pp + 64);
+        }
+        vsc = *reinterpret_cast<const u32x4*>(vt + CB + vg * 128 + vq4 * 16);
+        vlo = *reinterpret_cast<const u32x4*>(vt + CB + vg * 128 + 64 + vq4 * 16);
+    };
+    const DqConst dq = dq_const();
+    const ZeroOff zo = zero_off(0.f);
+    auto unpack = [&](int st, int buf, int nb) __attribute__((always_inline)) {
+        unsigned char* const kd = Ks + (buf * 2 + tt) * FB;
+        unsigned char* const vd = Vs + (buf * 2 + tt) * FB;
+        const int row = key_perm(kkey);                      // of the score tile (its chunks rotated: fewer bank conflicts)
+        const int kch = (row & 16) | ((row ^ (row >> 1 & 8)) & 15);
+#pragma unroll
+        for (int i = 0; i < NW; i++) {
+            const f16x8 x = dequant8(kw[i], zo, dq);
+            const f16 s = __builtin_bit_cast(f16, ksc[i]), lo = __builtin_bit_cast(f16, klo[i]);
+            const f16x8 y = __builtin_elementwise_fma(x, f16x8{s, s, s, s, s, s, s, s}, f16x8{lo, lo, lo, lo, lo, lo, lo, lo});
+            const int f = 2 * (NW * ksub + i) + (kq4 >> 1);
+            *reinterpret_cast<f16x8*>(kd + (f * 64 + (kq4 & 1) * 32 + kch) * 16) = y;
+        }
+        f16x8 s = __builtin_bit_cast(f16x8, vsc), lo = __builtin_bit_cast(f16x8, vlo);
+        const int key0 = st * PF_KST + tt * 32 + 8 * vq4;    // of the words' eight
+        if (key0 + 8 > nkeys) {                              // what lies behind the last key may be anything
+#pragma unroll
+            for (int e = 0; e < 8; e++) {
+                s[e] = key0 + e < nkeys ? s[e] : (f16)0.f;
+                lo[e] = key0 + e < nkeys ? lo[e] : (f16)0.f;
+            }
+        }
+        // A NaN value would reach the rows that do not see its key as 0 * NaN: it is 0 here, and the rows that do see it
+        // get their NaN from the list.
+        const f16x2 l0{lo[0], lo[1]}, l1{lo[2], lo[3]}, l2{lo[4], lo[5]}, l3{lo[6], lo[7]};
+        const f16x2 any = (l0 * (f16)0.f + l1 * (f16)0.f) + (l2 * (f16)0.f + l3 * (f16)0.f);
+        if (!(any[0] + any[1] == (f16)0.f)) {
+            unsigned long long m = 0;
+#pragma unroll
+            for (int e = 0; e < 8; e++)
+                if (lo[e] != lo[e]) {
+                    m |= 1ull << (tt * 32 + 8 * vq4 + e);
+                    s[e] = lo[e] = (f16)0.f;
+                }
+            if (vn == 0) {
+                atomicOr(vbad + nb * (NS + 1) + vg, m);
+                atomicOr(vbad + nb * (NS + 1) + NS, m);
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < NW; i++) {
+            const f16x8 y = __builtin_elementwise_fma(dequant8(vw[i], zo, dq), s, lo);
+            const int db = vdb + i;
+            *reinterpret_cast<f16x8*>(vd + (((db >> 1) * 2 + (vq4 >> 1)) * 64 + (vq4 & 1) * 32 + (db & 1) * 16 + vn) * 16) = y;
+        }
+    };
+    const int kch = (c & 16) | ((c ^ (c >> 1 & 8)) & 15);    // chunk of score row c
+    bool bad = false;
+
+    while (u < u1) {
+        const int hk = (int)(u / a.pf_units);
+        int q;
+        long long first;
+        pf_find(a, R, r, u - (long long)hk * a.pf_units, q, first);
+        first += (long long)hk * a.pf_units;
+        const int nst = pf_stages(q, R, r, a.ctx_base);      // stages of the tile
+        const int st0 = (int)(u - first), st1 = (int)min((long long)nst, u1 - first);
+        u = first + st1;
+        kb = a.k + (long long)hk * a.stride_h;
+        vb = a.v + (long long)hk * a.stride_h;
+        load_raw(st0);
+
+        // ---- queries: this lane's row, dims 16 f + 8 h .. + 7 of every fragment f, times 2^qe
+        const int row = q * PF_ROWS + wave * 32 + c;
+        const int rowc = min(row, R - 1), tok = rowc / r, hd = hk * r + rowc % r;
+        const uint16_t* qp = a.q + ((size_t)tok * a.nq + hd) * D + 8 * h;
+        u32x4 qw[NF];
+        float mx = 0.f;
+#pragma unroll
+        for (int f = 0; f < NF; f++) {
+            qw[f] = *reinterpret_cast<const u32x4*>(qp + 16 * f);
+#pragma unroll
+            for (int i = 0; i < 4; i++)
+                mx = fmaxf(mx, fmaxf(__builtin_fabsf(__uint_as_float(qw[f][i] << 16)),
+                                     __builtin_fabsf(__uint_as_float(qw[f][i] & 0xFFFF0000u))));
+        }
+        mx = max_xor32(mx);
+        const int qe = max(-113, min(120, 137 - (int)(__float_as_uint(mx) >> 23)));       // (to 2^10 ..: products stay small)
+        const float up = __uint_as_float((uint32_t)(127 + qe) << 23);
+        const float sl = a.scale * LOG2E * __uint_as_float((uint32_t)(127 - qe) << 23);
+        f16x8 qf[NF];
+#pragma unroll
+        for (int f = 0; f < NF; f++)
+#pragma unroll
+            for (int i = 0; i < 4; i++) {
+                qf[f][2 * i] = (f16)(__uint_as_float(qw[f][i] << 16) * up);
+                qf[f][2 * i + 1] = (f16)(__uint_as_float(qw[f][i] & 0xFFFF0000u) * up);
+            }
+        const int lim = a.ctx_base + tok;                    // this row's last key
+        const int row_lo = min(q * PF_ROWS + wave * 32, R - 1), row_hi = min(q * PF_ROWS + wave * 32 + 31, R - 1);
+        const int lim_lo = a.ctx_base + row_lo / r, lim_hi = a.ctx_base + row_hi / r;     // of the wave's rows
+        const bool active = q * PF_ROWS + wave * 32 < R;
+
+        f32x16 o[NS];
+#pragma unroll
+        for (int i = 0; i < NS; i++) o[i] = f32x16{};
+        float m = -INFINITY, l = 0.f;
+
+        __syncthreads();                                     // (the last tile's readers are done)
+        if (tid < 3 * (NS + 1)) vbad[tid] = 0;
+        __syncthreads();
+        unpack(st0, 0, 0);
+        if (st0 + 1 < st1) load_raw(st0 + 1);
+        __syncthreads();
+        int nb = 0;
+        for (int st = st0; st < st1; st++) {
+            const int buf = (st - st0) & 1;
+            const int nb1 = nb == 2 ? 0 : nb + 1, nb2 = nb1 == 2 ? 0 : nb1 + 1;
+            // (the list of stage st + 2 was last read in stage st - 1)
+            if (tid <= NS) vbad[nb2 * (NS + 1) + tid] = 0;
+            if (st + 1 < st1) {
+                unpack(st + 1, buf ^ 1, nb1);
+                if (st + 2 < st1) load_raw(st + 2);
+            }
+            const int kbase = st * PF_KST;
+            if (active && kbase <= lim_hi) {
+                const unsigned char* K = Ks + buf * 2 * FB;
+                const unsigned char* V = Vs + buf * 2 * FB;
+                f32x16 sc[2];
+                sc[0] = f32x16{};
+                sc[1] = f32x16{};
+#pragma unroll
+                for (int f = 0; f < NF; f++)
+#pragma unroll
+                    for (int t = 0; t < 2; t++) {
+                        const f16x8 kf = *reinterpret_cast<const f16x8*>(K + t * FB + (f * 64 + h * 32 + kch) * 16);
+                        sc[t] = __builtin_amdgcn_mfma_f32_32x32x16_f16(kf, qf[f], sc[t], 0, 0, 0);
+                    }
+                float p[32];
+#pragma unroll
+                for (int e = 0; e < 32; e++) p[e] = sc[e / 16][e % 16];
+                if (kbase + PF_KST - 1 > lim_lo) {
+#pragma unroll
+                    for (int e = 0; e < 32; e++) {
+                        const int key = kbase + 32 * (e / 16) + 16 * ((e % 16) / 8) + 8 * h + e % 8;
+                        p[e] = key <= lim ? p[e] : -INFINITY;
+                    }
+                }
+                float mt = fmaxf(p[0], p[1]);
+#pragma unroll
+                for (int e = 2; e < 32; e++) mt = fmaxf(mt, p[e]);
+                if (__builtin_amdgcn_ballot_w64(mt * sl > m + 8.f) != 0) {
+                    const float mn = fmaxf(m, max_xor32(mt) * sl);
+                    const float alpha = exp2_hw(m - (mn == -INFINITY ? 0.f : mn));
+                    l *= alpha;
+#pragma unroll
+                    for (int i = 0; i < NS; i++)
+#pragma unroll
+                        for (int e = 0; e < 16; e++) o[i][e] *= alpha;
+                    m = mn;
+                }
+                const float mb = m == -INFINITY ? 0.f : m;
+                float ls[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                for (int e = 0; e < 32; e++) {
+                    p[e] = exp2_hw(__builtin_fmaf(p[e], sl, -mb));
+                    ls[e % 4] += p[e];
+                }
+                l += (ls[0] + ls[1]) + (ls[2] + ls[3]);
+#pragma unroll
+                for (int ks = 0; ks < 4; ks++) {
+                    f16x8 pf;
+#pragma unroll
+                    for (int e = 0; e < 8; e += 2) {
+                        const f16x2 x = __builtin_convertvector(f32x2{p[8 * ks + e], p[8 * ks + e + 1]}, f16x2);
+                        pf[e] = x[0];
+                        pf[e + 1] = x[1];
+                    }
+#pragma unroll
+                    for (int i = 0; i < NS; i++) {
+                        const f16x8 vf = *reinterpret_cast<const f16x8*>(V + (ks >> 1) * FB + ((i * 2 + (ks & 1)) * 64 + lane) * 16);
+                        o[i] = __builtin_amdgcn_mfma_f32_32x32x16_f16(vf, pf, o[i], 0, 0, 0);
+                    }
+                }
+                if (vbad[nb * (NS + 1) + NS] != 0) {         // NaN for the rows that see one of the keys, in its group
+                    const long long left = lim - kbase;
+                    const unsigned long long see = left >= 63 ? ~0ull : left < 0 ? 0ull : (2ull << left) - 1;
+#pragma unroll
+                    for (int i = 0; i < NS; i++)
+                        if (vbad[nb * (NS + 1) + i] & see)
+#pragma unroll
+                            for (int e = 0; e < 16; e++) o[i][e] = __builtin_nanf("");
+                }
+            }
+            __syncthreads();
+            nb = nb1;
+        }
+        const bool whole = st0 == 0 && st1 == nst;
+        const float lt = l + __shfl_xor(l, 32, 64);
+        if (whole && row < R) {
+            const float inv = lt == 0.f ? 0.f : 1.f / lt;
+            const size_t orow = ((size_t)tok * a.nq + hd) * D;
+#pragma unroll
+            for (int i = 0; i < NS; i++)
+#pragma unroll
+                for (int e = 0; e < 16; e += 4) {
+                    const float x[4] = {o[i][e] * inv, o[i][e + 1] * inv, o[i][e + 2] * inv, o[i][e + 3] * inv};
+                    pf_put<D>(a, orow + i * 32 + 2 * e + 4 * h, x, bad);
+                }
+        }
+        if (!whole && active) {
+            // state of this piece: slot 0 of the block if it does not begin the tile, else 1
+            float* pp = a.part + (((size_t)blockIdx.x * 2 + (st0 == 0)) * PF_W + wave) * PF_NREG<D> * 64 + lane;
+            pp[0] = m;
+            pp[64] = l;
+#pragma unroll
+            for (int i = 0; i < NS; i++)
+#pragma unroll
+                for (int e = 0; e < 16; e++) pp[(2 + i * 16 + e) * 64] = o[i][e];
+        }
+    }
+    flag_range(a.err, bad);
+}
+
+// Merges the pieces of the row tiles that a cut parts: block (row tile, kv head,
+// 32-dim slice), thread (wave, lane) the lane's registers of the slice, piece
+// after piece in key order.
+template <int D>
+__global__ void __launch_bounds__(64 * PF_W) kv4_prefill_merge_kernel(Kv4AttnArgs a, int nblocks) {
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, h = lane >> 5, c = lane & 31;
+    const int q = blockIdx.x, hk = blockIdx.y, i = blockIdx.z;
+    const int r = a.nq / a.nkv, R = a.rows * r;
+    const long long total = a.pf_units * a.nkv;
+    long long before = 0;                                    // units of the head's tiles before q
+    for (int q0 = 0; q0 < q; q0 += 64) {
+        int x = q0 + lane < q ? pf_stages(q0 + lane, R, r, a.ctx_base) : 0;
+#pragma unroll
+        for (int off = 32; off > 0; off >>= 1) x += __shfl_xor(x, off, 64);
+        before += x;
+    }
+    const long long first = hk * a.pf_units + before, last = first + pf_stages(q, R, r, a.ctx_base) - 1;
+    // block that has unit u: the largest b with total * b / nblocks <= u
+    auto block_of = [&](long long x) { return (int)(((x + 1) * nblocks - 1) / total); };
+    const int b0 = block_of(first), b1 = block_of(last);
+    if (b0 == b1 || q * PF_ROWS + wave * 32 >= R) return;
+    constexpr int CB = 4;                                    // pieces requested together
+    float M = -INFINITY, L = 0.f, acc[16] = {};
+    for (int p0 = b0; p0 <= b1; p0 += CB) {
+        float mc[CB], lc[CB], v[CB][16];
+#pragma unroll
+        for (int j = 0; j < CB; j++) {
+            const int b = min(p0 + j, b1);
+            const float* pp = a.part + (((size_t)b * 2 + (b == b0)) * PF_W + wave) * PF_NREG<D> * 64 + lane;
+            mc[j] = pp[0];
+            lc[j] = pp[64];
+#pragma unroll
+            for (int e = 0; e < 16; e++) v[j][e] = pp[(2 + i * 16 + e) * 64];
+        }
+        float Mn = M;
+#pragma unroll
+        for (int j = 0; j < CB; j++)
+            if (p0 + j <= b1) Mn = fmaxf(Mn, mc[j]);
+        const float Mb = Mn == -INFINITY ? 0.f : Mn, s0 = exp2_hw(M - Mb);
+        L *= s0;
+#pragma unroll
+        for (int e = 0; e < 16; e++) acc[e] *= s0;
+#pragma unroll
+        for (int j = 0; j < CB; j++) {
+            if (p0 + j > b1) break;
+            const float s = exp2_hw(mc[j] - Mb);
+            L += s * lc[j];
+#pragma unroll
+            for (int e = 0; e < 16; e++) acc[e] += s * v[j][e];
+        }
+        M = Mn;
+    }
+    const int row = q * PF_ROWS + wave * 32 + c;
+    const float lt = L + __shfl_xor(L, 32, 64);
+    if (row >= R) return;
+    const float inv = lt == 0.f ? 0.f : 1.f / lt;
+    const size_t orow = ((size_t)(row / r) * a.nq + hk * r + row % r) * D;
+    bool bad = false;
+#pragma unroll
+    for (int e = 0; e < 16; e += 4) {
+        const float x[4] = {acc[e] * inv, acc[e + 1] * inv, acc[e + 2] * inv, acc[e + 3] * inv};
+        pf_put<D>(a, orow + i * 32 + 2 * e + 4 * h, x, bad);
+    }
+    flag_range(a.err, bad);
 }
 
 }  // namespace
@@ -561,12 +880,38 @@ int launch_kv4_decode(const Kv4AttnArgs& a, bool zeroed, hipStream_t stream) {
     return hipGetLastError() == hipSuccess ? 0 : -1;
 }
 
-int launch_kv4_attn(const Kv4AttnArgs& a, hipStream_t stream) {
-    const dim3 grid(a.rows, a.nq);
-    if (a.d == 128) hipLaunchKernelGGL(kv4_attn_kernel<128>, grid, dim3(256), 0, stream, a);
-    else if (a.d == 64) hipLaunchKernelGGL(kv4_attn_kernel<64>, grid, dim3(256), 0, stream, a);
-    else return -1;
+constexpr int kCus = 256;
+
+Kv4PrefillPlan kv4_prefill_plan(int T, int hist, int nkv, int r, int d) {
+    const int R = T * r, nqt = (R + PF_ROWS - 1) / PF_ROWS;
+    Kv4PrefillPlan p;
+    for (int q = 0; q < nqt; q++) p.units += pf_stages(q, R, r, hist);
+    const long long total = p.units * nkv;
+    p.blocks = (int)std::min<long long>(kCus, total);
+    // (of as many blocks as there may be: grows with T and hist)
+    p.part_bytes = (size_t)std::min<long long>(kCus, total) * 2 * PF_W * (2 + 16 * (d / 32)) * 64 * 4;
+    return p;
+}
+
+template <int D>
+static int launch_prefill(const Kv4AttnArgs& a, int blocks, hipStream_t stream) {
+    const size_t lds = (size_t)8 * 32 * D * 2 + 3 * (D / 32 + 1) * 8;
+    static LdsLimit lim;
+    if (ensure_lds_limit(lim, (const void*)kv4_prefill_kernel<D>, lds)) return -1;
+    hipLaunchKernelGGL(kv4_prefill_kernel<D>, dim3(blocks), dim3(64 * PF_W), lds, stream, a);
+    const int R = a.rows * (a.nq / a.nkv);
+    if (blocks > 1)
+        hipLaunchKernelGGL(kv4_prefill_merge_kernel<D>, dim3((R + PF_ROWS - 1) / PF_ROWS, a.nkv, D / 32), dim3(64 * PF_W), 0,
+                           stream, a, blocks);
     return hipGetLastError() == hipSuccess ? 0 : -1;
 }
 
-int load_kv4_attn() { return load_code((const void*)kv4_attn_kernel<128>); }
+int launch_kv4_prefill(const Kv4AttnArgs& a, hipStream_t stream) {
+    if (a.rows < 1 || !a.part) return -1;
+    const Kv4PrefillPlan p = kv4_prefill_plan(a.rows, a.ctx_base, a.nkv, a.nq / a.nkv, a.d);
+    Kv4AttnArgs b = a;
+    b.pf_units = p.units;
+    return a.d == 128 ? launch_prefill<128>(b, p.blocks, stream) : a.d == 64 ? launch_prefill<64>(b, p.blocks, stream) : -1;
+}
+
+int load_kv4_attn() { return load_code((const void*)kv4_decode_kernel<128, 1>); }
