@@ -37,7 +37,8 @@
  *   - The block's intermediate activations -- the normalised matmul inputs,
  *     q/k after RoPE, v, the attention output and the MLP hidden
  *     activation -- are rounded once to bf16 (round to nearest even), which
- *     is the W4BF16 precision; the K/V cache holds bf16.
+ *     is the W4BF16 precision; the K/V cache holds bf16, or, of a layer set to
+ *     W4_KV_INT4, the 4-bit codes of those bf16 values.
  *   - Weights are used exactly: W[k][n] = s[k/G][n] * (q[k][n] - z), sums in
  *     fp32.
  *   - The matrix units take the bf16-rounded activations as fp16 operands.
@@ -516,6 +517,18 @@ int kv4_attn_decode(const kv4_desc* desc, const void* q, const int32_t* ctx_lens
                     void* out, void* ws, size_t ws_bytes, void* stream);
 int kv4_attn_prefill(const kv4_desc* desc, const void* q, int32_t T, int32_t hist_len, int32_t n_heads,
                      const void* k_cache, const void* v_cache, void* out, void* ws, size_t ws_bytes, void* stream);
+
+/* Cache format of a layer's calls from now on: W4_KV_BF16 (the default) or
+ * W4_KV_INT4.  With the latter every stage, chunk, stack and model call takes
+ * k_cache and v_cache in the kv4_layout(cfg, B) layout (16-byte aligned;
+ * prefill calls: one sequence's part), quantises its new keys and
+ * values (bf16 after RoPE) into it as kv4_append does and attends through the
+ * cache alone, to the call's own tokens too, so chunked prefills, single steps
+ * and a whole prefill see the same keys.  A key or value without fp16 value
+ * raises W4_FLAG_F16_RANGE.  Workspace sizes depend on the format: set it
+ * first.  Such a layer decodes as the kernel sequence; with decode path 2 its
+ * decode calls are refused (W4_EUNSUPPORTED).  Errors: W4_EINVAL. */
+int layer_set_kv_format(layer_t layer, int32_t format);
 
 /* ---- diagnostics ------------------------------------------------------- */
 

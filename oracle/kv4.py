@@ -19,6 +19,8 @@ from __future__ import annotations
 
 import numpy as np
 
+from oracle import layer as _layer
+
 F64 = np.float64
 GROUP = 32
 
@@ -83,3 +85,30 @@ def attend(q, k, v, seen, add=None, key_eps: float = 0.0):
         out[h] = w @ vv
         tol[h] = (w @ np.abs(vv)) * (np.expm1(2 * e) + 2.0 ** -10 + 2.0 ** -14) + 2.0 ** -24 * (1 + np.abs(vv).max())
     return out, tol
+
+
+def block(w: dict, cfg, x, pos, k_hist=None, v_hist=None, bias=None, rows=None, W=None):
+    """oracle.layer.block for a layer whose cache is held in 4 bits: the new
+    keys and values (bf16 after RoPE, as they are formed there) enter the cache,
+    and every key and value that the attention sees, the call's own among them,
+    is what the cache holds.  k_hist, v_hist: the values held, [nkv][L][d].
+    Returns y and the values held of the new k, v [T][nkv][d]."""
+    nq, d = cfg.n_heads, cfg.head_dim
+    W = _layer.dequant_layer(w, cfg) if W is None else W
+    x = np.asarray(x, dtype=F64)
+    T = x.shape[0]
+    sel = np.arange(T) if rows is None else np.asarray(rows)
+    xn = _layer.round_bf16(_layer.rmsnorm(x, _layer.bf16_to_f64(w["attn_norm"]), cfg.rms_eps))
+    cos, sin = _layer.rope_cos_sin(pos, d, cfg.rope_base)
+    q = _layer.round_bf16(_layer.rope((xn[sel] @ W["q"]).reshape(len(sel), nq, d), cos[sel], sin[sel]))
+    k = held(_layer.round_bf16(_layer.rope((xn @ W["k"]).reshape(T, -1, d), cos, sin)))
+    v = held(_layer.round_bf16((xn @ W["v"]).reshape(T, -1, d)))
+    L = 0 if k_hist is None else k_hist.shape[1]
+    k_all = k if not L else np.concatenate([k_hist.transpose(1, 0, 2), k])
+    v_all = v if not L else np.concatenate([v_hist.transpose(1, 0, 2), v])
+    b = None if bias is None else np.asarray(bias, dtype=F64)[sel]
+    a = _layer.round_bf16(_layer.attention(q, k_all, v_all, L + sel, b).reshape(len(sel), nq * d))
+    h = x[sel] + a @ W["o"]
+    hn = _layer.round_bf16(_layer.rmsnorm(h, _layer.bf16_to_f64(w["mlp_norm"]), cfg.rms_eps))
+    g = _layer.round_bf16(_layer.silu(hn @ W["gate"]) * (hn @ W["up"]))
+    return h + g @ W["down"], k, v

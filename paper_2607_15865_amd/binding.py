@@ -29,6 +29,8 @@ W4_FLAG_WAIT_TIMEOUT, W4_FLAG_F16_RANGE, W4_FLAG_TOKEN_ID = 1, 2, 4
 W4_WEIGHTS_INT4, W4_WEIGHTS_INT8, W4_WEIGHTS_BF16 = 0, 1, 2
 WEIGHT_FORMAT_CODE = {"int4": W4_WEIGHTS_INT4, "int8": W4_WEIGHTS_INT8, "bf16": W4_WEIGHTS_BF16}
 STAGE_PREFILL, STAGE_PREFILL_KV, STAGE_DECODE = 0, 1, 2
+W4_KV_BF16, W4_KV_INT4 = 0, 1
+KV_FORMAT_CODE = {"bf16": W4_KV_BF16, "int4": W4_KV_INT4}
 LINEAR_INDEX = {"q": 0, "k": 1, "v": 2, "o": 3, "gate": 4, "up": 5, "down": 6}
 
 if not os.path.exists(LIB_PATH):
@@ -111,6 +113,7 @@ _SIG = {
     "kv4_attn_prefill": (ctypes.c_int, [ctypes.POINTER(kv4_desc), _P, _I, _I, _I, _P, _P, _P, _P, ctypes.c_size_t, _P]),
     "layer_debug_dequant": (ctypes.c_int, [_P, _I, _P, _P]),
     "layer_set_decode_path": (ctypes.c_int, [_P, _I]),
+    "layer_set_kv_format": (ctypes.c_int, [_P, _I]),
     "layer_set_gemm_plan": (ctypes.c_int, [_P, _I, _I, _I, _I, _I]),
     "layer_decode_phase_times": (ctypes.c_int, [_P, _P, _P]),
     "layer_debug_decode_stamps": (ctypes.c_int, [_P, _P, _I]),
@@ -392,6 +395,10 @@ def layer_set_decode_spin_limit(handle, polls: int) -> int:
     return _lib.layer_set_decode_spin_limit(handle, polls)
 
 
+def layer_set_kv_format(handle, fmt: int) -> int:
+    return _lib.layer_set_kv_format(handle, fmt)
+
+
 def layer_set_gemm_plan(handle, gemm: int, row_tile: int, waves: int, k_groups: int, k_splits: int) -> int:
     return _lib.layer_set_gemm_plan(handle, gemm, row_tile, waves, k_groups, k_splits)
 
@@ -537,6 +544,7 @@ class Layer:
         self.cfg = cfg
         rc, self.handle = layer_create(cfg, weights)
         check(rc)
+        self.kv_format = "bf16"
         _live.add(self)
         self._ws = torch.empty(0, dtype=torch.uint8, device="cuda")
 
@@ -568,10 +576,22 @@ class Layer:
             self._ws = torch.empty(n, dtype=torch.uint8, device="cuda")
         return self._ws, self._ws.numel()
 
+    def set_kv_format(self, fmt: str):
+        """"bf16" (the default) or "int4": the format of the caches that the layer's calls take from now on."""
+        check(layer_set_kv_format(self.handle, KV_FORMAT_CODE[fmt]))
+        self.kv_format = fmt
+
     def new_cache(self, batch: int, fill_bits: Optional[int] = None):
-        """A K and a V cache in the kv_layout(cfg, batch) layout (uint16 bf16
-        bit patterns), optionally filled with one bit pattern."""
+        """A K and a V cache in the layout of the layer's cache format:
+        kv_layout(cfg, batch) (uint16 bf16 bit patterns), optionally filled with
+        one bit pattern, or kv4_layout(cfg, batch) (bytes, [batch][stride_b])."""
         import torch
+        if self.kv_format == "int4":
+            if fill_bits is not None:
+                raise ValueError("fill_bits is for bf16 caches")
+            rc, d4 = kv4_layout(self.cfg, batch)
+            check(rc)
+            return tuple(torch.empty((batch, d4.stride_b), dtype=torch.uint8, device="cuda") for _ in range(2))
         rc, d = kv_layout(self.cfg, batch)
         check(rc)
         shape = (batch, d.n_kv_heads, d.max_seq, d.head_dim)

@@ -285,6 +285,7 @@ struct layer_s {
     int* err = nullptr;
     unsigned long long* stamps = nullptr;
     int decode_path = 0;   // 0 auto, 1 separate kernels, 2 persistent
+    int kv_format = W4_KV_BF16;
     bool decode_trace = false;   // persistent decode records its time stamps
     int spin_max = kSpinDefault; // polls per thread per persistent launch before a wait gives up
 };
@@ -437,8 +438,12 @@ GemmPlan prefill_gemm_plan(const layer_s* L, int T, int gemm, const DevLinear& W
     return p.TM ? gemm_w4_plan_of(T, W, p.TM, p.WN, p.KG, p.S) : gemm_w4_plan(T, W, L->num_cus);
 }
 
+// A call's new keys, then its values: bf16 [n_kv_heads][rows][head_dim] each.
+size_t kv_stage_half(const layer_s* L, int rows) { return (size_t)rows * L->cfg.n_kv_heads * L->cfg.head_dim * 2; }
+size_t kv_stage_bytes(const layer_s* L, int rows) { return 2 * kv_stage_half(L, rows); }
+
 struct PrefillWs {
-    size_t xn1, q, attn, h, xn2, g, part, cnt, total;
+    size_t xn1, q, attn, h, xn2, g, part, cnt, kv, total;   // kv: bf16 keys and values on their way into a 4-bit cache
     GemmPlan qkv, o, gu, down;
     AttnPrefillPlan at;
 };
@@ -451,7 +456,10 @@ PrefillWs plan_prefill(const layer_s* L, int T, int hist) {
     w.o = prefill_gemm_plan(L, T, 1, L->o.d);
     w.gu = prefill_gemm_plan(L, T, 2, L->gu.d);
     w.down = prefill_gemm_plan(L, T, 3, L->down.d);
-    w.at = attn_prefill_plan(T, hist, c.n_heads, c.n_kv_heads, c.head_dim, L->num_cus);
+    const bool kv4 = L->kv_format == W4_KV_INT4;
+    if (!kv4) w.at = attn_prefill_plan(T, hist, c.n_heads, c.n_kv_heads, c.head_dim, L->num_cus);
+    const size_t at_part = kv4 ? kv4_prefill_plan(T, hist, c.n_kv_heads, c.n_heads / c.n_kv_heads, c.head_dim).part_bytes
+                               : w.at.part_bound;
     w.xn1 = cv.take((size_t)T * c.hidden * 2);
     w.q = cv.take((size_t)T * qd * 2);
     w.attn = cv.take((size_t)T * qd * 2);
@@ -460,29 +468,36 @@ PrefillWs plan_prefill(const layer_s* L, int T, int hist) {
     w.g = cv.take((size_t)T * L->F_pad * 2);
     // split-K partials of each GEMM and the attention chunk states, used one kernel at a time
     const size_t split = L->split_bytes[std::min((T - 1) / 32, (int)L->split_bytes.size() - 1)];
-    w.part = cv.take(std::max({split, w.at.part_bound, w.qkv.part_bytes, w.o.part_bytes, w.gu.part_bytes, w.down.part_bytes}));
+    w.part = cv.take(std::max({split, at_part, w.qkv.part_bytes, w.o.part_bytes, w.gu.part_bytes, w.down.part_bytes}));
     w.cnt = cv.take((size_t)4 * kGemmCounters * 4);   // split-K arrival counters, one set per GEMM
+    w.kv = cv.take(kv4 ? kv_stage_bytes(L, T) : 0);
     w.total = cv.off;
     return w;
 }
 
-struct DecodeWs { size_t q, part, attn, h, g, xn, total; int nsplit; };
+struct DecodeWs { size_t q, part, attn, h, g, xn, kv, cnt, total; int nsplit; };
 DecodeWs plan_decode(const layer_s* L, int B, int max_ctx) {
     const layer_config& c = L->cfg;
     const size_t qd = (size_t)c.n_heads * c.head_dim;
     DecodeWs w;
+    const bool kv4 = L->kv_format == W4_KV_INT4;
+    const int r = c.n_heads / c.n_kv_heads;
     // attention shares; their arrival counters live in g, which is written
     // only after the attention (a layer whose g is too small takes one share)
     w.nsplit = c.n_kv_heads * 4 <= L->F_pad * 2 ? attn_decode_splits(B, c.n_kv_heads, max_ctx, L->num_cus) : 1;
+    if (kv4) w.nsplit = kv4_decode_plan(B, c.n_kv_heads, r, c.head_dim, max_ctx).nsplit;
     // (sized for a share per 64 keys, at least as many as there are)
     const int nchunks = (max_ctx + 64) / 64;
     Carve cv;
     w.q = cv.take((size_t)B * qd * 2);
-    w.part = cv.take((size_t)B * c.n_heads * nchunks * (c.head_dim + 2) * 4);
+    w.part = cv.take(kv4 ? kv4_decode_part_bound(B, c.n_kv_heads, r, c.head_dim, max_ctx)
+                         : (size_t)B * c.n_heads * nchunks * (c.head_dim + 2) * 4);
     w.attn = cv.take((size_t)B * qd * 2);
     w.h = cv.take((size_t)B * c.hidden * 4);
     w.g = cv.take((size_t)B * L->F_pad * 2);
     w.xn = cv.take((size_t)B * c.hidden * 2);
+    w.kv = cv.take(kv4 ? kv_stage_bytes(L, B) : 0);
+    w.cnt = cv.take(kv4 ? (size_t)B * c.n_kv_heads * 4 : 0);
     w.total = cv.off;
     return w;
 }
@@ -505,6 +520,7 @@ FusedPlan plan_fused(const layer_s* L, int B, int max_ctx, bool query_device) {
     FusedPlan p;
     const layer_config& c = L->cfg;
     if (B > 4 || L->decode_path == 1) return p;
+    if (L->kv_format != W4_KV_BF16) return p;                                // 4-bit cache: separate kernels
     if (L->qkv.d.wf != WF_INT4) return p;                                    // 8- and 16-bit weights: separate kernels
     if (L->qkv.d.sz || L->o.d.sz || L->gu.d.sz || L->down.d.sz) return p;   // zero points: separate kernels
     if (c.group_size < 64) return p;                                         // groups of 32: separate kernels
@@ -691,6 +707,77 @@ int launch_fused(layer_s* L, const FusedPlan& fp, const float* x, const int32_t*
     return launch_decode_fused(a, st);
 }
 
+// With a 4-bit cache the q/k/v product leaves its keys and values (after RoPE, rounded to
+// bf16 as for a bf16 cache) in the workspace, in place of a cache ...
+void kv_stage_epi(const layer_s* L, EpiArgs& e, char* stage, int rows) {
+    e.k_cache = (uint16_t*)stage;
+    e.v_cache = (uint16_t*)(stage + kv_stage_half(L, rows));
+    e.cache_stride_b = 0;
+    e.cache_stride_h = (long long)rows * L->cfg.head_dim;
+    e.slot_dev = nullptr;
+    e.slot_base = 0;
+}
+
+long long kv4_stride_h(const layer_config& c) {
+    return ((long long)c.max_seq + KV4_TILE - 1) / KV4_TILE * kv4_tile_bytes(c.head_dim);
+}
+
+// ... from where they are quantised into it.  shared: the rows are consecutive tokens
+// of one sequence from slot ctx_base on; else row b goes to slot ctx_lens[b] of sequence b.
+Kv4StoreArgs kv_stage_store(const layer_s* L, char* stage, int rows, bool shared, const int32_t* ctx_lens, int ctx_base,
+                            void* kc, void* vc) {
+    const layer_config& c = L->cfg;
+    Kv4StoreArgs s{};
+    s.k = (uint8_t*)kc;
+    s.v = (uint8_t*)vc;
+    s.stride_h = kv4_stride_h(c);
+    s.stride_b = s.stride_h * c.n_kv_heads;
+    s.k_x = (uint16_t*)stage;
+    s.v_x = (uint16_t*)(stage + kv_stage_half(L, rows));
+    s.x_h = (long long)rows * c.head_dim;
+    s.x_b = s.x_t = c.head_dim;
+    s.slots_dev = shared ? nullptr : ctx_lens;
+    s.slots.v[0] = ctx_base;
+    s.max_seq = c.max_seq;
+    s.B = shared ? 1 : rows;
+    s.T = shared ? rows : 1;
+    s.nkv = c.n_kv_heads;
+    s.d = c.head_dim;
+    s.err = L->err;
+    return s;
+}
+
+Kv4AttnArgs kv4_layer_attn(const layer_s* L, const uint16_t* q, const void* kc, const void* vc, f16* out, int rows,
+                           bool shared, const int32_t* ctx_lens, int ctx_base, int max_ctx) {
+    const layer_config& c = L->cfg;
+    Kv4AttnArgs a{};
+    a.q = q;
+    a.k = (const uint8_t*)kc;
+    a.v = (const uint8_t*)vc;
+    a.stride_h = kv4_stride_h(c);
+    a.stride_b = shared ? 0 : a.stride_h * c.n_kv_heads;
+    a.ctx_lens = shared ? nullptr : ctx_lens;
+    a.ctx_base = ctx_base;
+    a.max_ctx = max_ctx;
+    a.max_seq = c.max_seq;
+    a.out = out;
+    a.out_f16 = 1;
+    a.rows = rows;
+    a.nq = c.n_heads;
+    a.nkv = c.n_kv_heads;
+    a.d = c.head_dim;
+    a.scale = (float)(1.0 / std::sqrt((double)c.head_dim));
+    a.err = L->err;
+    return a;
+}
+
+// A 4-bit cache's kernels take its tiles in 16-byte words.
+int check_cache(const layer_s* L, const void* kc, const void* vc) {
+    if (L->kv_format == W4_KV_INT4 && ((uintptr_t)kc % 16 || (uintptr_t)vc % 16))
+        return fail(W4_EINVAL, "a 4-bit cache must be 16-byte aligned");
+    return W4_OK;
+}
+
 // The decode as a sequence of kernels (GEMVs on up to 8 rows, split-KV
 // attention that merges its shares itself).  shared: the B rows are consecutive tokens of one
 // sequence with one cache (prefill / prefill_kv of at most 8 tokens), row b
@@ -731,6 +818,8 @@ int run_decode_seq(layer_s* L, const float* x, const int32_t* pos, const int32_t
     a1.ep.pos = pos;
     a1.ep.slot_dev = shared ? nullptr : ctx_lens;
     a1.ep.slot_base = ctx_base;
+    const bool kv4 = L->kv_format == W4_KV_INT4;
+    if (kv4) kv_stage_epi(L, a1.ep, base + w.kv, B);
     GemvArgs a2{}, a4{};                    // o_proj and down: h = x + A Wo, y = h + g Wd
     a2.W = L->o.d;
     a4.W = L->down.d;
@@ -740,7 +829,7 @@ int run_decode_seq(layer_s* L, const float* x, const int32_t* pos, const int32_t
     gemv_resid_plan(a4, ordered);
     a1.clear = h;
     a1.nclear = a2.ksplit > 1 ? B * H : 0;
-    a1.zero = (unsigned*)g;                 // the attention's arrival counters
+    a1.zero = kv4 ? (unsigned*)(base + w.cnt) : (unsigned*)g;     // the attention's arrival counters
     a1.nzero = w.nsplit > 1 ? B * c.n_kv_heads : 0;
     // the rows are normalised in every block, or, many of them, once beforehand
     const bool prenorm = !gemv_norm_fits(B, H);
@@ -752,6 +841,16 @@ int run_decode_seq(layer_s* L, const float* x, const int32_t* pos, const int32_t
     }
     { ProfScope ps(L, ps_stage, ps_stage == 2 ? 0 : 1, st); rc |= launch_gemv_w4(EPI_QKV, !prenorm, a1, st); }
 
+    if (kv4) {
+        rc |= launch_kv4_append(kv_stage_store(L, base + w.kv, B, shared, ctx_lens, ctx_base, kc, vc), st);
+        Kv4AttnArgs ka = kv4_layer_attn(L, q, kc, vc, attn, B, shared, ctx_lens, ctx_base, max_ctx);
+        ka.mask = attn_mask;
+        ka.nsplit = w.nsplit;
+        ka.part = part;
+        ka.cnt = (unsigned*)(base + w.cnt);
+        ProfScope ps(L, ps_stage, ps_stage == 2 ? 1 : 2, st);
+        rc |= launch_kv4_decode(ka, true, st);
+    }
     AttnDecodeArgs ad{};
     ad.q = q;
     ad.k_cache = (const uint16_t*)kc;
@@ -772,7 +871,10 @@ int run_decode_seq(layer_s* L, const float* x, const int32_t* pos, const int32_t
     ad.cnt = (unsigned*)g;
     ad.scale_log2 = (float)(1.4426950408889634 / std::sqrt((double)d));
     ad.err = L->err;
-    { ProfScope ps(L, ps_stage, ps_stage == 2 ? 1 : 2, st); rc |= launch_attn_decode(ad, st); }
+    if (!kv4) {
+        ProfScope ps(L, ps_stage, ps_stage == 2 ? 1 : 2, st);
+        rc |= launch_attn_decode(ad, st);
+    }
 
     a2.x_f16 = attn;
     a2.ldx = qd;
@@ -867,6 +969,8 @@ int run_prefill(layer_s* L, const float* x, const int32_t* pos, int T, int hist,
     if (T < 1 || hist < 0) return fail(W4_EINVAL, "T must be >= 1 and hist_len >= 0");
     if ((long long)hist + T > c.max_seq) return fail(W4_ECAPACITY, "hist_len + T = %lld exceeds max_seq %d", (long long)hist + T, c.max_seq);
     hipStream_t st = (hipStream_t)stream_;
+    int rc0;
+    if ((rc0 = check_cache(L, kc, vc))) return rc0;
     const int stage = hist > 0 ? 1 : 0;
     FusedPlan fp = small_prefill_plan(L, T, hist);
     const bool cap = fp.ok && capturing(st);
@@ -906,7 +1010,16 @@ int run_prefill(layer_s* L, const float* x, const int32_t* pos, int T, int hist,
     e.cache_stride_h = (long long)c.max_seq * d;
     e.pos = pos;
     e.slot_base = hist;
+    const bool kv4 = L->kv_format == W4_KV_INT4;
+    if (kv4) kv_stage_epi(L, e, base + w.kv, T);
     { ProfScope ps(L, stage, 1, st); rc |= launch_gemm_w4(EPI_QKV, xn1, H, L->qkv.d, e, w.qkv, T, part, cnt, st); }
+    if (kv4) {
+        rc |= launch_kv4_append(kv_stage_store(L, base + w.kv, T, true, nullptr, hist, kc, vc), st);
+        Kv4AttnArgs ka = kv4_layer_attn(L, q, kc, vc, attn, T, true, nullptr, hist, hist + T - 1);
+        ka.part = part;
+        ProfScope ps(L, stage, 2, st);
+        rc |= launch_kv4_prefill(ka, st);
+    }
     AttnPrefillArgs aa{};
     aa.q = q;
     aa.k_cache = (const uint16_t*)kc;
@@ -921,7 +1034,10 @@ int run_prefill(layer_s* L, const float* x, const int32_t* pos, int T, int hist,
     aa.scale_log2 = (float)(1.4426950408889634 / std::sqrt((double)d));
     aa.part = part;
     aa.err = L->err;
-    { ProfScope ps(L, stage, 2, st); rc |= launch_attn_prefill(aa, w.at, st); }
+    if (!kv4) {
+        ProfScope ps(L, stage, 2, st);
+        rc |= launch_attn_prefill(aa, w.at, st);
+    }
     EpiArgs eo = base_epi(L);
     eo.resid = x;
     eo.out_f32 = h;
@@ -1229,7 +1345,7 @@ int layer_decode(layer_t L, const float* x, const int32_t* pos, const int32_t* c
     if ((const void*)x == (const void*)y) return fail(W4_EINVAL, "x and y must not alias");
     int rc;
     const hipStream_t st = (hipStream_t)stream;
-    if ((rc = decode_check(L, B, max_ctx, &st))) return rc;
+    if ((rc = decode_check(L, B, max_ctx, &st)) || (rc = check_cache(L, kc, vc))) return rc;
     return decode_run(L, x, pos, ctx_lens, max_ctx, attn_mask, B, kc, vc, y, ws, ws_bytes, (hipStream_t)stream, 2);
 }
 
@@ -1240,7 +1356,7 @@ int layer_decode_noalloc(layer_t L, const float* x, const int32_t* pos, const in
     if ((const void*)x == (const void*)y) return fail(W4_EINVAL, "x and y must not alias");
     int rc;
     const hipStream_t st = (hipStream_t)stream;
-    if ((rc = decode_check(L, B, max_ctx, &st))) return rc;
+    if ((rc = decode_check(L, B, max_ctx, &st)) || (rc = check_cache(L, kc, vc))) return rc;
     if (L->device < 0 || L->device >= kMaxDevices || !g_scratch[L->device])
         return fail(W4_EHIP, "scratch array not set up on device %d", L->device);
     const size_t need = layer_workspace_size(L, 2, B, 1, max_ctx);
@@ -1530,7 +1646,7 @@ int stack_prefill(const layer_t* layers, int32_t n, const float* x, const int32_
     if (!x || !y || !ws || !k_caches || !v_caches) return fail(W4_EINVAL, "null pointer argument");
     if ((const void*)x == (const void*)y) return fail(W4_EINVAL, "x and y must not alias");
     for (int i = 0; i < n; i++)
-        if ((rc = prefill_check(layers[i], T, hist_len))) return rc;
+        if ((rc = prefill_check(layers[i], T, hist_len)) || (rc = check_cache(layers[i], k_caches[i], v_caches[i]))) return rc;
     const size_t need = stack_workspace_size(layers, n, hist_len > 0 ? 1 : 0, 1, T, hist_len);
     if (need == 0 || ws_bytes < need) return fail(W4_EWORKSPACE, "workspace %zu bytes, need %zu", ws_bytes, need);
     const size_t act = stack_act_offset(need - 2 * (size_t)T * layers[0]->cfg.hidden * sizeof(float));
@@ -1553,7 +1669,8 @@ int stack_decode(const layer_t* layers, int32_t n, const float* x, const int32_t
     if ((const void*)x == (const void*)y) return fail(W4_EINVAL, "x and y must not alias");
     const hipStream_t st = (hipStream_t)stream;
     for (int i = 0; i < n; i++)
-        if ((rc = decode_check(layers[i], B, max_ctx, &st))) return rc;
+        if ((rc = decode_check(layers[i], B, max_ctx, &st)) || (rc = check_cache(layers[i], k_caches[i], v_caches[i])))
+            return rc;
     const size_t need = stack_workspace_size(layers, n, 2, B, 1, max_ctx);
     if (need == 0 || ws_bytes < need) return fail(W4_EWORKSPACE, "workspace %zu bytes, need %zu", ws_bytes, need);
     const size_t act = stack_act_offset(need - 2 * (size_t)B * layers[0]->cfg.hidden * sizeof(float));
@@ -1613,6 +1730,13 @@ int layer_set_decode_path(layer_t L, int32_t path) {
     if (!L) return fail(W4_EINVAL, "null layer");
     if (path < 0 || path > 2) return fail(W4_EINVAL, "path must be 0, 1 or 2");
     L->decode_path = path;
+    return W4_OK;
+}
+
+int layer_set_kv_format(layer_t L, int32_t format) {
+    if (!L) return fail(W4_EINVAL, "null layer");
+    if (format != W4_KV_BF16 && format != W4_KV_INT4) return fail(W4_EINVAL, "unknown cache format %d", format);
+    L->kv_format = format;
     return W4_OK;
 }
 
@@ -1847,8 +1971,10 @@ int model_decode_greedy(const layer_t* layers, int32_t n_layers, lm_t lm, const 
     if (!layers || n_layers < 1 || !lm || !tokens || !pos || !ctx_lens || !k_caches || !v_caches || !logits ||
         !next_tokens)
         return fail(W4_EINVAL, "null pointer argument");
-    for (int i = 0; i < n_layers; i++)
+    for (int i = 0; i < n_layers; i++) {
         if (!layers[i] || !k_caches[i] || !v_caches[i]) return fail(W4_EINVAL, "null layer or cache %d", i);
+        if (int rc = check_cache(layers[i], k_caches[i], v_caches[i])) return rc;
+    }
     if (layers[0]->cfg.hidden != lm->cfg.hidden) return fail(W4_EINVAL, "layers and LM ends differ in hidden size");
     if (B < 1 || max_ctx < 0) return fail(W4_EINVAL, "B must be >= 1 and max_ctx >= 0");
     if (B > lm->cfg.max_batch) return fail(W4_ECAPACITY, "B %d > the LM ends' max_batch %d", B, lm->cfg.max_batch);

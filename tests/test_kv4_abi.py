@@ -122,3 +122,7 @@ def test_workspace_size():
 
 def test_struct_matches_the_header():
     assert ctypes.sizeof(B.kv4_desc) == 4 * 4 + 2 * 8 + 8
+
+
+def test_set_kv_format_refusals():
+    assert B.layer_set_kv_format(None, B.W4_KV_INT4) == B.W4_EINVAL
