@@ -689,102 +689,121 @@ class KV4Cache:
         self.k = torch.empty(self.desc.bytes, dtype=torch.uint8, device="cuda")
         self.v = torch.empty(self.desc.bytes, dtype=torch.uint8, device="cuda")
         self._ws = {}
-        self._grown = []                 # outgrown workspaces: graphs and other streams may still use them
+        self._grown = []                 # outgrown workspaces: work in flight may still use them
+        # what every call needs, in the form that costs a call least
+        self._desc_ref = ctypes.byref(self.desc)
+        self._dev = self.k.device.index
+        self._kp, self._vp = self.k.data_ptr(), self.v.data_ptr()
+        self._head = (self.desc.n_kv_heads, self.desc.head_dim)
+        self._q_head = (cfg.n_heads, self.desc.head_dim)
+        self._torch = torch
+        self._bits16 = (torch.bfloat16, torch.int16, torch.uint16)
+        # (torch.cuda.current_stream() builds a Stream object, 2.7 us; its handle alone takes 0.1)
+        self._raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream",
+                                   lambda dev: torch.cuda.current_stream(dev).cuda_stream)
 
-    def _tensor(self, t, shape, what, dtypes=None):
-        import torch
-        if tuple(t.shape) != tuple(shape):
-            raise ValueError(f"{what}: shape {tuple(t.shape)}, expected {tuple(shape)}")
-        if t.dtype not in (dtypes or (torch.bfloat16, torch.int16, torch.uint16)):
+    def _refuse(self, t, shape, what, dtypes):
+        """The reason why a tensor does not fit."""
+        if tuple(t.shape) != shape:
+            raise ValueError(f"{what}: shape {tuple(t.shape)}, expected {shape}")
+        if t.dtype not in dtypes:
             raise ValueError(f"{what}: dtype {t.dtype}")
-        if t.device != self.k.device:
+        if t.get_device() != self._dev:
             raise ValueError(f"{what} is on {t.device}, the cache on {self.k.device}")
-        if not t.is_contiguous():
-            raise ValueError(f"{what} must be contiguous")
+        raise ValueError(f"{what} must be contiguous")
 
-    def _here(self):
-        import torch
-        if torch.cuda.current_device() != self.k.device.index:
-            raise ValueError(f"the cache is on {self.k.device}, the current device is {torch.cuda.current_device()}")
+    def _tensor(self, t, shape, what):
+        """Address of a bf16 tensor of the shape."""
+        if t.shape != shape or t.dtype not in self._bits16 or t.get_device() != self._dev or not t.is_contiguous():
+            self._refuse(t, shape, what, self._bits16)
+        return t.data_ptr()
 
-    def _workspace(self, stage, B, T, max_ctx, stream):
-        import torch
-        n = kv4_attn_workspace_size(self.desc, self.n_heads, stage, B, T, max_ctx)
-        if n == 0:
-            raise W4Error(W4_EINVAL, layer_last_error())
-        if torch.cuda.is_current_stream_capturing():
-            return torch.empty(n, dtype=torch.uint8, device=self.k.device), n
-        key = _stream(stream)
-        ws = self._ws.get(key)
-        if ws is None or ws.numel() < n:
-            if ws is not None:
-                self._grown.append(ws)
-                n = max(n, 2 * ws.numel())
-            ws = self._ws[key] = torch.empty(n, dtype=torch.uint8, device=self.k.device)
-        return ws, ws.numel()
+    def _ints(self, t, B, what):
+        if t.dtype != self._torch.int32 or t.shape != (B,) or t.get_device() != self._dev or not t.is_contiguous():
+            self._refuse(t, (B,), what, (self._torch.int32,))
+        return t.data_ptr()
+
+    def _on(self, stream):
+        """The stream's handle; the cache's device has to be the current one."""
+        if self._torch.cuda.current_device() != self._dev:
+            raise ValueError(f"the cache is on {self.k.device}, the current device is {self._torch.cuda.current_device()}")
+        if stream is None:
+            return self._raw_stream(self._dev)
+        return stream if isinstance(stream, int) else stream.cuda_stream
 
     def _slots(self, slot_start, B):
         if len(slot_start) != B:
             raise ValueError(f"{len(slot_start)} slots for {B} sequences")
+        return (ctypes.c_int32 * B)(*[int(s) for s in slot_start])
+
+    def _attend(self, call, size, stream):
+        """Runs call(workspace address, bytes) on the stream's workspace; one that is too small is replaced."""
+        if self._torch.cuda.is_current_stream_capturing():
+            n = size()
+            ws = self._torch.empty(n, dtype=self._torch.uint8, device=self.k.device)
+            check(call(ws.data_ptr(), n))
+            return
+        ws = self._ws.get(stream)
+        rc = W4_EWORKSPACE if ws is None else call(ws.data_ptr(), ws.numel())
+        if rc == W4_EWORKSPACE:
+            n = size()
+            if n == 0:
+                raise W4Error(W4_EINVAL, layer_last_error())
+            if ws is not None:
+                self._grown.append(ws)
+                n = max(n, 2 * ws.numel())
+            ws = self._ws[stream] = self._torch.empty(n, dtype=self._torch.uint8, device=self.k.device)
+            rc = call(ws.data_ptr(), n)
+        check(rc)
 
     def append(self, k_new, v_new, slot_start, stream=None):
         """k_new, v_new [B][T][n_kv_heads][head_dim] into slots slot_start[b] .. + T - 1 (host integers)."""
         B, T = k_new.shape[:2]
-        shape = (B, T, self.desc.n_kv_heads, self.desc.head_dim)
-        self._tensor(k_new, shape, "k_new")
-        self._tensor(v_new, shape, "v_new")
-        self._slots(slot_start, B)
-        self._here()
-        check(kv4_append(self.desc, self.k, self.v, k_new, v_new, B, T, slot_start, stream))
+        shape = (B, T) + self._head
+        kp, vp = self._tensor(k_new, shape, "k_new"), self._tensor(v_new, shape, "v_new")
+        check(_lib.kv4_append(self._desc_ref, self._kp, self._vp, kp, vp, B, T, self._slots(slot_start, B),
+                              self._on(stream)))
 
     def append_step(self, k_new, v_new, ctx_lens, stream=None):
         """One token per sequence, k_new, v_new [B][1][n_kv_heads][head_dim] (or without the 1), into slots ctx_lens
         (int32 [B] on the device)."""
-        import torch
         B = k_new.shape[0]
-        shape = (B, 1, self.desc.n_kv_heads, self.desc.head_dim) if k_new.dim() == 4 else \
-            (B, self.desc.n_kv_heads, self.desc.head_dim)
-        self._tensor(k_new, shape, "k_new")
-        self._tensor(v_new, shape, "v_new")
-        self._tensor(ctx_lens, (B,), "ctx_lens", (torch.int32,))
-        self._here()
-        check(kv4_append_step(self.desc, self.k, self.v, k_new, v_new, B, ctx_lens, stream))
+        shape = (B, 1) + self._head if k_new.dim() == 4 else (B,) + self._head
+        kp, vp = self._tensor(k_new, shape, "k_new"), self._tensor(v_new, shape, "v_new")
+        check(_lib.kv4_append_step(self._desc_ref, self._kp, self._vp, kp, vp, B, self._ints(ctx_lens, B, "ctx_lens"),
+                                   self._on(stream)))
 
     def read(self, slot_start, T, k_out, v_out, stream=None):
         """Slots slot_start[b] .. + T - 1 as bf16 values into k_out, v_out [B][T][n_kv_heads][head_dim]."""
         B = k_out.shape[0]
-        shape = (B, T, self.desc.n_kv_heads, self.desc.head_dim)
-        self._tensor(k_out, shape, "k_out")
-        self._tensor(v_out, shape, "v_out")
-        self._slots(slot_start, B)
-        self._here()
-        check(kv4_read(self.desc, self.k, self.v, B, T, slot_start, k_out, v_out, stream))
+        shape = (B, T) + self._head
+        kp, vp = self._tensor(k_out, shape, "k_out"), self._tensor(v_out, shape, "v_out")
+        check(_lib.kv4_read(self._desc_ref, self._kp, self._vp, B, T, self._slots(slot_start, B), kp, vp, self._on(stream)))
 
     def attn_decode(self, q, ctx_lens, max_ctx, out, attn_mask=None, stream=None):
         """One query per sequence: q, out [B][n_heads][head_dim], slots 0 .. ctx_lens[b] (int32 [B] on the device)."""
-        import torch
         B = q.shape[0]
-        shape = (B, self.n_heads, self.desc.head_dim)
-        self._tensor(q, shape, "q")
-        self._tensor(out, shape, "out")
-        self._tensor(ctx_lens, (B,), "ctx_lens", (torch.int32,))
+        shape = (B,) + self._q_head
+        qp, op, cp, mp = self._tensor(q, shape, "q"), self._tensor(out, shape, "out"), self._ints(ctx_lens, B, "ctx_lens"), None
         if attn_mask is not None:
-            self._tensor(attn_mask, (B, self.desc.max_seq), "attn_mask", (torch.float32,))
-        self._here()
-        ws, n = self._workspace(STAGE_DECODE, B, 1, max_ctx, stream)
-        check(kv4_attn_decode(self.desc, q, ctx_lens, max_ctx, attn_mask, B, self.n_heads, self.k, self.v, out, ws, n,
-                              stream))
+            mshape, f32 = (B, self.desc.max_seq), self._torch.float32
+            if attn_mask.shape != mshape or attn_mask.dtype != f32 or attn_mask.get_device() != self._dev or \
+                    not attn_mask.is_contiguous():
+                self._refuse(attn_mask, mshape, "attn_mask", (f32,))
+            mp = attn_mask.data_ptr()
+        st = self._on(stream)
+        self._attend(lambda ws, n: _lib.kv4_attn_decode(self._desc_ref, qp, cp, max_ctx, mp, B, self.n_heads, self._kp,
+                                                        self._vp, op, ws, n, st),
+                     lambda: kv4_attn_workspace_size(self.desc, self.n_heads, STAGE_DECODE, B, 1, max_ctx), st)
 
     def attn_prefill(self, q, hist_len, out, row: int = 0, stream=None):
         """T queries of sequence `row` after hist_len tokens: q, out [T][n_heads][head_dim]."""
         T = q.shape[0]
-        shape = (T, self.n_heads, self.desc.head_dim)
-        self._tensor(q, shape, "q")
-        self._tensor(out, shape, "out")
+        shape = (T,) + self._q_head
+        qp, op = self._tensor(q, shape, "q"), self._tensor(out, shape, "out")
         if not 0 <= row < self.desc.batch:
             raise ValueError(f"row {row} of a cache of {self.desc.batch} sequences")
-        self._here()
-        ws, n = self._workspace(STAGE_PREFILL_KV, 1, T, hist_len, stream)
-        off = row * self.desc.stride_b
-        check(kv4_attn_prefill(self.desc, q, T, hist_len, self.n_heads, self.k.data_ptr() + off,
-                               self.v.data_ptr() + off, out, ws, n, stream))
+        off, st = row * self.desc.stride_b, self._on(stream)
+        self._attend(lambda ws, n: _lib.kv4_attn_prefill(self._desc_ref, qp, T, hist_len, self.n_heads, self._kp + off,
+                                                         self._vp + off, op, ws, n, st),
+                     lambda: kv4_attn_workspace_size(self.desc, self.n_heads, STAGE_PREFILL_KV, 1, T, hist_len), st)

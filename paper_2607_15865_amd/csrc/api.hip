@@ -475,7 +475,7 @@ PrefillWs plan_prefill(const layer_s* L, int T, int hist) {
     return w;
 }
 
-struct DecodeWs { size_t q, part, attn, h, g, xn, kv, cnt, total; int nsplit; };
+struct DecodeWs { size_t q, part, attn, h, g, xn, kv, cnt, total; int nsplit, waves; };
 DecodeWs plan_decode(const layer_s* L, int B, int max_ctx) {
     const layer_config& c = L->cfg;
     const size_t qd = (size_t)c.n_heads * c.head_dim;
@@ -485,7 +485,11 @@ DecodeWs plan_decode(const layer_s* L, int B, int max_ctx) {
     // attention shares; their arrival counters live in g, which is written
     // only after the attention (a layer whose g is too small takes one share)
     w.nsplit = c.n_kv_heads * 4 <= L->F_pad * 2 ? attn_decode_splits(B, c.n_kv_heads, max_ctx, L->num_cus) : 1;
-    if (kv4) w.nsplit = kv4_decode_plan(B, c.n_kv_heads, r, c.head_dim, max_ctx).nsplit;
+    if (kv4) {
+        const Kv4DecodePlan p = kv4_decode_plan(B, c.n_kv_heads, r, c.head_dim, max_ctx);
+        w.nsplit = p.nsplit;
+        w.waves = p.waves;
+    }
     // (sized for a share per 64 keys, at least as many as there are)
     const int nchunks = (max_ctx + 64) / 64;
     Carve cv;
@@ -849,7 +853,7 @@ int run_decode_seq(layer_s* L, const float* x, const int32_t* pos, const int32_t
         ka.part = part;
         ka.cnt = (unsigned*)(base + w.cnt);
         ProfScope ps(L, ps_stage, ps_stage == 2 ? 1 : 2, st);
-        rc |= launch_kv4_decode(ka, true, st);
+        rc |= launch_kv4_decode(ka, w.waves, true, st);
     }
     AttnDecodeArgs ad{};
     ad.q = q;
@@ -1559,10 +1563,11 @@ int kv4_attn_decode(const kv4_desc* d, const void* q, const int32_t* ctx_lens, i
     a.mask = attn_mask;
     a.rows = B;
     const Kv4DecodeWs w = kv4_decode_ws(d, n_heads, B, max_ctx);
-    a.nsplit = kv4_decode_plan(B, d->n_kv_heads, n_heads / d->n_kv_heads, d->head_dim, max_ctx).nsplit;
+    const Kv4DecodePlan plan = kv4_decode_plan(B, d->n_kv_heads, n_heads / d->n_kv_heads, d->head_dim, max_ctx);
+    a.nsplit = plan.nsplit;
     a.cnt = (unsigned*)((char*)ws + w.cnt);
     a.part = (float*)((char*)ws + w.part);
-    if (launch_kv4_decode(a, false, (hipStream_t)stream))
+    if (launch_kv4_decode(a, plan.waves, false, (hipStream_t)stream))
         return fail(W4_EHIP, "kernel launch failed: %s", hipGetErrorString(hipGetLastError()));
     return W4_OK;
 }

@@ -28,7 +28,9 @@ constexpr float LOG2E = 1.4426950408889634f;
 
 // ---------------------------------------------------------------- decode
 
-constexpr int DEC_W = 8;         // waves per block
+constexpr int MAXW = 8;          // waves per block
+constexpr long long kMaxShares = 1024;   // beyond one per (row, kv head), of a launch
+constexpr int kCus = 256;
 constexpr int MAXR = 8;          // query heads per kv head
 
 // Eight codes of a word as fp16 multiples of 2^-24: elements 0, 1, 4, 5 are
@@ -38,6 +40,23 @@ __device__ __forceinline__ f16x8 code_frag(uint32_t w) {
     const u32x4 r{w & 0x000F000Fu, w & 0x00F000F0u, w8 & 0x000F000Fu, w8 & 0x00F000F0u};
     return __builtin_bit_cast(f16x8, r);
 }
+
+// Over lanes l, l ^ 16, l ^ 32, l ^ 48.
+__device__ __forceinline__ float max_quarters(float v) {
+    auto x = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    v = fmaxf(__uint_as_float(x[0]), __uint_as_float(x[1]));
+    x = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    return fmaxf(__uint_as_float(x[0]), __uint_as_float(x[1]));
+}
+__device__ __forceinline__ float sum_quarters(float v) {
+    auto x = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    v = __uint_as_float(x[0]) + __uint_as_float(x[1]);
+    x = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    return __uint_as_float(x[0]) + __uint_as_float(x[1]);
+}
+
+// h x + y, h widened in the operation.
+__device__ __forceinline__ float mix_fma(f16 h, float x, float y) { return __builtin_fmaf((float)h, x, y); }
 
 template <int N>                 // lanes xor 1 .. N / 2, N = 2 or 4
 __device__ __forceinline__ float group_max(float v) {
@@ -52,19 +71,12 @@ __device__ __forceinline__ float group_sum(float v) {
     return v;
 }
 
-// A tile's registers of one lane.
-template <int D>
-struct KvTile {
-    static constexpr int NS = D / 32;
-    uint32_t kc[2][NS];          // words of score tiles 0 and 1
-    u32x4 vc[NS / 2];            // words of dim blocks 0 .. 3 (4 .. 7)
-    f16x8 ks, kl, vs, vl;        // scale and offset of group g, tokens 8 q4 .. + 7
-    float mk[8 / NS];            // mask of this lane's scores
-};
-
-// One block: a share of the tiles of one (row, kv head), all r query heads of
-// the group.  Wave w takes tiles w, w + 8, .. of the share on its own; the next
-// tile's loads are in flight while one is computed.  CT column tiles of 16 /
+// One block: a share (a.per tiles) of one (row, kv head), all r query heads of the
+// group.  Wave w of W takes tiles w, w + W, .. of the share on its own; the next
+// tile's K is requested when this one's scores are formed and its V when its
+// output is, into the same registers, so that two blocks fit a CU (CT 1).  The first
+// tile's requests do not wait for the context length: a share's place is fixed by
+// the longest context, and blocks past a row's own end leave.  CT column tiles of 16 /
 // NS heads.  Softmax: the maximum of a head moves only when a score passes it by
 // more than 2 (all lanes of the wave then agree on the new one), so weights stay
 // below e^2.  Weights times scales are a pair of fp16 numbers, hi + lo: s c and lo of a
@@ -73,21 +85,15 @@ struct KvTile {
 // passes the fp16 range after all (a scale above 8), ef drops to 1 for the rest of
 // the share: e^2 times the largest scale (8734) is 64536.
 template <int D, int CT>
-__global__ void __launch_bounds__(64 * DEC_W) kv4_decode_kernel(Kv4AttnArgs a) {
+__global__ void __launch_bounds__(64 * MAXW, CT == 1 ? 4 : 2) kv4_decode_kernel(Kv4AttnArgs a) {
     constexpr int NS = D / 32, NDB = D / 16, HC = 16 / NS, PS = 8 / NS;
     constexpr int TB = kv4_tile_bytes(D), CB = kv4_code_bytes(D);
-    __shared__ __attribute__((aligned(16))) float ored[DEC_W][MAXR][D];
-    __shared__ float gst[DEC_W][MAXR][2], glo[DEC_W][MAXR][NS];
+    extern __shared__ __attribute__((aligned(16))) float ored[];          // [W][r][D]
+    __shared__ float gst[MAXW][MAXR][2], glo[MAXW][MAXR][NS];
     __shared__ unsigned last_flag;
-    const int tid = threadIdx.x, lane = tid & 63;
+    const int tid = threadIdx.x, lane = tid & 63, NT = blockDim.x, W = NT >> 6;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    const int b = blockIdx.x / a.nkv, hk = blockIdx.x % a.nkv;
-    const int ctx = min(a.ctx_lens ? a.ctx_lens[b] : a.ctx_base + b, a.max_ctx);
-    const int ntiles = (ctx + KV4_TILE) / KV4_TILE;             // of ctx + 1 keys
-    const int n = max(1, min(a.nsplit, ntiles)), part = blockIdx.y;
-    if (part >= n) return;
-    const int tile0 = (int)((long long)part * ntiles / n), tile1 = (int)((long long)(part + 1) * ntiles / n);
-    const int r = a.nq / a.nkv;
+    const int hk = blockIdx.x, part = blockIdx.y, b = blockIdx.z, r = a.r;
     const int n16 = lane & 15, q4 = lane >> 4, g = n16 % NS;
     const long long base = (long long)b * a.stride_b + (long long)hk * a.stride_h;
     const uint8_t* const kb = a.k + base;
@@ -96,36 +102,46 @@ __global__ void __launch_bounds__(64 * DEC_W) kv4_decode_kernel(Kv4AttnArgs a) {
     // key of score i (NS 4: tile i; NS 2: tile i / 2) of this lane, of 32
     auto score_key = [&](int i) { return NS == 4 ? 8 * q4 + 4 * i + g : 8 * q4 + 4 * (i >> 1) + 2 * (i & 1) + g; };
 
-    KvTile<D> nx;
-    auto load_tile = [&](int tile) __attribute__((always_inline)) {
+    uint32_t kc[2][NS];              // words of score tiles 0 and 1
+    u32x4 vc[NS / 2];                // words of dim blocks 0 .. 3 (4 .. 7)
+    f16x8 ks, kl, vs, vl;            // scale and offset of group g, tokens 8 q4 .. + 7
+    float mk[PS];                    // mask of this lane's scores
+    const int paro = CB + g * 128 + q4 * 16;
+    auto load_k = [&](int tile) __attribute__((always_inline)) {
         const uint8_t* kt = kb + (long long)tile * TB;
-        const uint8_t* vt = vb + (long long)tile * TB;
 #pragma unroll
         for (int t = 0; t < 2; t++) {
             if constexpr (NS == 4) {
                 const u32x4 w = *reinterpret_cast<const u32x4*>(kt + (t * 64 + lane) * 16);
 #pragma unroll
-                for (int s = 0; s < NS; s++) nx.kc[t][s] = w[s];
+                for (int s = 0; s < NS; s++) kc[t][s] = w[s];
             } else {
                 const u32x2 w = *reinterpret_cast<const u32x2*>(kt + (t * 64 + lane) * 8);
-                nx.kc[t][0] = w[0];
-                nx.kc[t][1] = w[1];
+                kc[t][0] = w[0];
+                kc[t][1] = w[1];
             }
         }
-        const int po = CB + g * 128 + q4 * 16;
-        nx.ks = *reinterpret_cast<const f16x8*>(kt + po);
-        nx.kl = *reinterpret_cast<const f16x8*>(kt + po + 64);
-#pragma unroll
-        for (int i = 0; i < NS / 2; i++) nx.vc[i] = *reinterpret_cast<const u32x4*>(vt + (i * 64 + lane) * 16);
-        nx.vs = *reinterpret_cast<const f16x8*>(vt + po);
-        nx.vl = *reinterpret_cast<const f16x8*>(vt + po + 64);
+        ks = *reinterpret_cast<const f16x8*>(kt + paro);
+        kl = *reinterpret_cast<const f16x8*>(kt + paro + 64);
         if (mrow) {
 #pragma unroll
-            for (int i = 0; i < PS; i++) nx.mk[i] = mrow[min(tile * KV4_TILE + score_key(i), ctx)];
+            for (int i = 0; i < PS; i++) mk[i] = mrow[min(tile * KV4_TILE + score_key(i), a.max_ctx)];
         }
     };
+    auto load_v = [&](int tile) __attribute__((always_inline)) {
+        const uint8_t* vt = vb + (long long)tile * TB;
+#pragma unroll
+        for (int i = 0; i < NS / 2; i++) vc[i] = *reinterpret_cast<const u32x4*>(vt + (i * 64 + lane) * 16);
+        vs = *reinterpret_cast<const f16x8*>(vt + paro);
+        vl = *reinterpret_cast<const f16x8*>(vt + paro + 64);
+    };
+    const int tile0 = part * a.per;
     int tile = tile0 + wave;
-    if (tile < tile1) load_tile(tile);
+    int ctx = a.ctx_lens ? a.ctx_lens[b] : a.ctx_base + b;
+    if (tile * KV4_TILE <= a.max_ctx) {
+        load_k(tile);
+        load_v(tile);
+    }
 
     // ---- queries: head ct HC + n16 / NS, dims 32 g + 8 q4 .. + 7, times 2^qe (the head's largest becomes 2^14 ..)
     f16x8 qf[CT][NS];
@@ -142,9 +158,7 @@ __global__ void __launch_bounds__(64 * DEC_W) kv4_decode_kernel(Kv4AttnArgs a) {
             x[2 * i + 1] = __uint_as_float(w[i] & 0xFFFF0000u);
             mx = fmaxf(mx, fmaxf(__builtin_fabsf(x[2 * i]), __builtin_fabsf(x[2 * i + 1])));
         }
-        mx = group_max<NS>(mx);
-        mx = fmaxf(mx, __shfl_xor(mx, 16, 64));
-        mx = fmaxf(mx, __shfl_xor(mx, 32, 64));
+        mx = max_quarters(group_max<NS>(mx));
         // exponent field of the largest; 2^qe and 2^-qe are both normal numbers
         const int qe = max(-113, min(126, 141 - (int)(__float_as_uint(mx) >> 23)));
         const float up = __uint_as_float((uint32_t)(127 + qe) << 23);
@@ -157,28 +171,30 @@ __global__ void __launch_bounds__(64 * DEC_W) kv4_decode_kernel(Kv4AttnArgs a) {
             sum += v;
             fr[e] = (f16)(e & 2 ? v * 0.0625f : v);
         }
-        sum += __shfl_xor(sum, 16, 64);
-        sum += __shfl_xor(sum, 32, 64);
-        qs[ct] = sum * 0x1p-24f;
+        qs[ct] = sum_quarters(sum) * 0x1p-24f;
 #pragma unroll
         for (int s = 0; s < NS; s++) qf[ct][s] = g == s ? fr : f16x8{};
     }
     const float f1 = a.scale * 0x1p24f;
 
+    ctx = min(ctx, a.max_ctx);
+    const int ntiles = (ctx + KV4_TILE) / KV4_TILE;             // of ctx + 1 keys
+    const int n = max(1, (ntiles + a.per - 1) / a.per);         // shares of this row
+    if (part >= n) return;
+    const int tile1 = min(tile0 + a.per, ntiles);
+
     f32x4 o[CT][NDB];
-    float m[CT], l[CT], olo[CT];
+    float m[CT], l[CT], olo[CT][2];  // olo: sums of the offsets, of keys whose weights are held as they are, and / 16
 #pragma unroll
     for (int ct = 0; ct < CT; ct++) {
 #pragma unroll
         for (int i = 0; i < NDB; i++) o[ct][i] = f32x4{0.f, 0.f, 0.f, 0.f};
         m[ct] = -INFINITY;
-        l[ct] = olo[ct] = 0.f;
+        l[ct] = olo[ct][0] = olo[ct][1] = 0.f;
     }
     float ef = 1024.f;
 
-    for (; tile < tile1; tile += DEC_W) {
-        const KvTile<D> c = nx;
-        if (tile + DEC_W < tile1) load_tile(tile + DEC_W);
+    for (; tile < tile1; tile += W) {
         f32x4 acc[CT][2];
 #pragma unroll
         for (int ct = 0; ct < CT; ct++) acc[ct][0] = acc[ct][1] = f32x4{0.f, 0.f, 0.f, 0.f};
@@ -186,55 +202,59 @@ __global__ void __launch_bounds__(64 * DEC_W) kv4_decode_kernel(Kv4AttnArgs a) {
         for (int s = 0; s < NS; s++)
 #pragma unroll
             for (int t = 0; t < 2; t++) {
-                const f16x8 kf = code_frag(c.kc[t][s]);
+                const f16x8 kf = code_frag(kc[t][s]);
 #pragma unroll
                 for (int ct = 0; ct < CT; ct++) acc[ct][t] = __builtin_amdgcn_mfma_f32_16x16x32_f16(kf, qf[ct][s], acc[ct][t], 0, 0, 0);
             }
-        const bool special = mrow || (tile + 1) * KV4_TILE > ctx + 1;
+        const bool special = mrow || (tile + 1) * KV4_TILE > ctx + 1;       // some key may be hidden
         float p[CT][PS];
 #pragma unroll
         for (int ct = 0; ct < CT; ct++) {
-            float sc[PS];
 #pragma unroll
             for (int t = 0; t < 2; t++) {
                 float v[4];
 #pragma unroll
                 for (int j = 0; j < 4; j++)
-                    v[j] = __builtin_fmaf((float)c.ks[4 * t + j], acc[ct][t][j], (float)c.kl[4 * t + j] * qs[ct]);
+                    v[j] = mix_fma(ks[4 * t + j], acc[ct][t][j], mix_fma(kl[4 * t + j], qs[ct], 0.f));
                 // sums over the groups (lanes g): lane g keeps the key 4 t + g (NS 2: keys 4 t + g, 4 t + 2 + g)
                 const bool b0 = lane & 1;
                 const float r0 = (b0 ? v[1] : v[0]) + dpp_mov<0xB1>(b0 ? v[0] : v[1]);
                 const float r1 = (b0 ? v[3] : v[2]) + dpp_mov<0xB1>(b0 ? v[2] : v[3]);
                 if constexpr (NS == 4) {
                     const bool b1 = lane & 2;
-                    sc[t] = (b1 ? r1 : r0) + dpp_mov<0x4E>(b1 ? r0 : r1);
+                    p[ct][t] = ((b1 ? r1 : r0) + dpp_mov<0x4E>(b1 ? r0 : r1)) * f1 * f2[ct];
                 } else {
-                    sc[2 * t] = r0;
-                    sc[2 * t + 1] = r1;
+                    p[ct][2 * t] = r0 * f1 * f2[ct];
+                    p[ct][2 * t + 1] = r1 * f1 * f2[ct];
                 }
             }
-            float mx = -INFINITY;
+            if (special) {
+                int lim = ctx;
+                asm volatile("" : "+s"(lim));                   // (a branch, not selects on every tile)
 #pragma unroll
-            for (int i = 0; i < PS; i++) {
-                sc[i] = sc[i] * f1 * f2[ct];
-                if (special) {
-                    bool seen = tile * KV4_TILE + score_key(i) <= ctx;
+                for (int i = 0; i < PS; i++) {
+                    bool seen = tile * KV4_TILE + score_key(i) <= lim;
                     if (mrow) {
-                        seen = seen && c.mk[i] != -INFINITY;
-                        sc[i] += c.mk[i];
+                        seen = seen && mk[i] != -INFINITY;
+                        p[ct][i] += mk[i];
                     }
-                    sc[i] = seen ? sc[i] : -INFINITY;
+                    p[ct][i] = seen ? p[ct][i] : -INFINITY;
                 }
-                mx = fmaxf(mx, sc[i]);
             }
+        }
+        if (tile + W < tile1) load_k(tile + W);
+        f16x8 pf[CT], pl[CT];
+#pragma unroll
+        for (int ct = 0; ct < CT; ct++) {
+            float mx = p[ct][0];
+#pragma unroll
+            for (int i = 1; i < PS; i++) mx = fmaxf(mx, p[ct][i]);
             if (__builtin_amdgcn_ballot_w64(mx > m[ct] + 2.f) != 0) {
-                mx = group_max<NS>(mx);
-                mx = fmaxf(mx, __shfl_xor(mx, 16, 64));
-                mx = fmaxf(mx, __shfl_xor(mx, 32, 64));
-                const float mn = fmaxf(m[ct], mx);
+                const float mn = fmaxf(m[ct], max_quarters(group_max<NS>(mx)));
                 const float alpha = exp2_hw((m[ct] - (mn == -INFINITY ? 0.f : mn)) * LOG2E);
                 l[ct] *= alpha;
-                olo[ct] *= alpha;
+                olo[ct][0] *= alpha;
+                olo[ct][1] *= alpha;
                 m[ct] = mn;
                 // register j of lane (., q4) is row 4 q4 + j, of head (4 q4 + j) / NS
                 const float a0 = __shfl(alpha, 4 * q4, 64), a1 = NS == 4 ? a0 : __shfl(alpha, 4 * q4 + 2, 64);
@@ -247,55 +267,62 @@ __global__ void __launch_bounds__(64 * DEC_W) kv4_decode_kernel(Kv4AttnArgs a) {
                 }
             }
             const float mb = m[ct] == -INFINITY ? 0.f : m[ct];
+            // weights, times ef and, of keys whose codes come times 16 (element & 2), / 16
+            float u[PS];
 #pragma unroll
             for (int i = 0; i < PS; i++) {
-                p[ct][i] = exp2_hw((sc[i] - mb) * LOG2E);
-                l[ct] += p[ct][i];
+                const float w = exp2_hw((p[ct][i] - mb) * LOG2E);
+                l[ct] += w;
+                u[i] = w * ((NS == 4 ? g & 2 : i & 1) ? ef * 0.0625f : ef);
             }
-        }
-        // P'_(h,g) of keys 8 q4 + e: weights from the lanes that hold them; offsets summed on the way
-        f16x8 pf[CT], pl[CT];
-#pragma unroll
-        for (int ct = 0; ct < CT; ct++) {
+            // P'_(h,g) of keys 8 q4 + e: weights from the lanes that hold them
             float w[8];
 #pragma unroll
             for (int t = 0; t < 2; t++) {
                 if constexpr (NS == 4) {
-                    w[4 * t + 0] = dpp_mov<0x00>(p[ct][t]);
-                    w[4 * t + 1] = dpp_mov<0x55>(p[ct][t]);
-                    w[4 * t + 2] = dpp_mov<0xAA>(p[ct][t]);
-                    w[4 * t + 3] = dpp_mov<0xFF>(p[ct][t]);
+                    w[4 * t + 0] = dpp_mov<0x00>(u[t]);
+                    w[4 * t + 1] = dpp_mov<0x55>(u[t]);
+                    w[4 * t + 2] = dpp_mov<0xAA>(u[t]);
+                    w[4 * t + 3] = dpp_mov<0xFF>(u[t]);
                 } else {
-                    w[4 * t + 0] = dpp_mov<0xA0>(p[ct][2 * t]);
-                    w[4 * t + 1] = dpp_mov<0xF5>(p[ct][2 * t]);
-                    w[4 * t + 2] = dpp_mov<0xA0>(p[ct][2 * t + 1]);
-                    w[4 * t + 3] = dpp_mov<0xF5>(p[ct][2 * t + 1]);
+                    w[4 * t + 0] = dpp_mov<0xA0>(u[2 * t]);
+                    w[4 * t + 1] = dpp_mov<0xF5>(u[2 * t]);
+                    w[4 * t + 2] = dpp_mov<0xA0>(u[2 * t + 1]);
+                    w[4 * t + 3] = dpp_mov<0xF5>(u[2 * t + 1]);
                 }
             }
-            float ps[8], pmax = 0.f;
+            f16x8 cs = vs, cl = vl;
+            if (special) {                                      // (hidden keys may hold NaN)
 #pragma unroll
-            for (int e = 0; e < 8; e++) {
-                float s = (float)c.vs[e], lo = (float)c.vl[e];
-                if (special) {                       // (hidden keys may hold NaN)
-                    s = w[e] == 0.f ? 0.f : s;
-                    lo = w[e] == 0.f ? 0.f : lo;
+                for (int e = 0; e < 8; e++) {
+                    float z = w[e];
+                    asm volatile("" : "+v"(z));
+                    cs[e] = z == 0.f ? (f16)0.f : cs[e];
+                    cl[e] = z == 0.f ? (f16)0.f : cl[e];
                 }
-                ps[e] = w[e] * s;
-                olo[ct] = __builtin_fmaf(w[e], lo, olo[ct]);
-                pmax = fmaxf(pmax, ps[e]);
             }
-            if (__builtin_amdgcn_ballot_w64(pmax * ef > 65504.f) != 0) {
-                const float down = 1.f / ef;
+            float ps[8];
+#pragma unroll
+            for (int e = 0; e < 8; e++) ps[e] = mix_fma(cs[e], w[e], 0.f);
+            const float pmax = fmaxf(fmaxf(fmaxf(ps[0], ps[1]), fmaxf(ps[2], ps[3])), fmaxf(fmaxf(ps[4], ps[5]), fmaxf(ps[6], ps[7])));
+            if (__builtin_amdgcn_ballot_w64(pmax > 65504.f) != 0) {
+                float down = 0x1p-10f;
+                asm volatile("" : "+v"(down));
                 ef = 1.f;
 #pragma unroll
-                for (int c2 = 0; c2 < CT; c2++)
+                for (int c2 = 0; c2 < CT; c2++) {
+                    olo[c2][0] *= down;
+                    olo[c2][1] *= down;
 #pragma unroll
                     for (int i = 0; i < NDB; i++)
 #pragma unroll
                         for (int e = 0; e < 4; e++) o[c2][i][e] *= down;
-                if (ct == 1) {
+                }
 #pragma unroll
-                    for (int e = 0; e < 8; e++) {
+                for (int e = 0; e < 8; e++) {
+                    ps[e] *= down;
+                    w[e] *= down;
+                    if (ct == 1) {
                         pf[0][e] = (f16)((float)pf[0][e] * down);
                         pl[0][e] = (f16)((float)pl[0][e] * down);
                     }
@@ -303,36 +330,35 @@ __global__ void __launch_bounds__(64 * DEC_W) kv4_decode_kernel(Kv4AttnArgs a) {
             }
 #pragma unroll
             for (int e = 0; e < 8; e += 2) {
-                const float es = e & 2 ? ef * 0.0625f : ef, x = ps[e] * es, y = ps[e + 1] * es;
-                const f16x2 hi = __builtin_bit_cast(f16x2, __builtin_amdgcn_cvt_pkrtz(x, y));
-                const f16x2 lo = __builtin_bit_cast(f16x2, __builtin_amdgcn_cvt_pkrtz(x - (float)hi[0], y - (float)hi[1]));
+                olo[ct][e >> 1 & 1] = mix_fma(cl[e], w[e], olo[ct][e >> 1 & 1]);
+                olo[ct][e >> 1 & 1] = mix_fma(cl[e + 1], w[e + 1], olo[ct][e >> 1 & 1]);
+                const f16x2 hi = __builtin_bit_cast(f16x2, __builtin_amdgcn_cvt_pkrtz(ps[e], ps[e + 1]));
+                const f16x2 lo = __builtin_bit_cast(f16x2, __builtin_amdgcn_cvt_pkrtz(ps[e] - (float)hi[0], ps[e + 1] - (float)hi[1]));
                 pf[ct][e] = hi[0]; pf[ct][e + 1] = hi[1];
                 pl[ct][e] = lo[0]; pl[ct][e + 1] = lo[1];
             }
         }
 #pragma unroll
         for (int i = 0; i < NDB; i++) {
-            const f16x8 vf = code_frag(c.vc[i / 4][i % 4]);
+            const f16x8 vf = code_frag(vc[i / 4][i % 4]);
 #pragma unroll
             for (int ct = 0; ct < CT; ct++) {
                 o[ct][i] = __builtin_amdgcn_mfma_f32_16x16x32_f16(pf[ct], vf, o[ct][i], 0, 0, 0);
                 o[ct][i] = __builtin_amdgcn_mfma_f32_16x16x32_f16(pl[ct], vf, o[ct][i], 0, 0, 0);
             }
         }
+        if (tile + W < tile1) load_v(tile + W);
     }
 
     // ---- the waves' states meet in LDS
-    const float of = 0x1p24f / ef;
+    const float eo = ef == 1.f ? 1.f : 0x1p-10f;                // 1 / ef
 #pragma unroll
     for (int ct = 0; ct < CT; ct++) {
-        l[ct] = group_sum<NS>(l[ct]);
-        l[ct] += __shfl_xor(l[ct], 16, 64);
-        l[ct] += __shfl_xor(l[ct], 32, 64);
-        olo[ct] += __shfl_xor(olo[ct], 16, 64);
-        olo[ct] += __shfl_xor(olo[ct], 32, 64);
+        l[ct] = sum_quarters(group_sum<NS>(l[ct]));
+        const float lo = sum_quarters(olo[ct][0] + 16.f * olo[ct][1]) * eo;
         const int h = ct * HC + n16 / NS;
         if (q4 == 0 && h < r) {
-            glo[wave][h][g] = olo[ct];
+            glo[wave][h][g] = lo;
             if (g == 0) {
                 gst[wave][h][0] = m[ct];
                 gst[wave][h][1] = l[ct];
@@ -343,15 +369,14 @@ __global__ void __launch_bounds__(64 * DEC_W) kv4_decode_kernel(Kv4AttnArgs a) {
 #pragma unroll
             for (int j = i / 2; j < 4; j += NS) {               // the rows of dim block i's group
                 const int ho = ct * HC + (4 * q4 + j) / NS;
-                if (ho < r) ored[wave][ho][16 * i + n16] = o[ct][i][j] * of;
+                if (ho < r) ored[(wave * r + ho) * D + 16 * i + n16] = o[ct][i][j] * (0x1p24f * eo);
             }
     }
     __syncthreads();
-    // share state: [row, kv head][share][r heads][D] outputs, then [..][r][2] (max, sum)
-    const size_t slot = (size_t)blockIdx.x * a.nsplit;
-    unsigned long long* const po = reinterpret_cast<unsigned long long*>(a.part) + slot * r * (D / 2);
-    unsigned long long* const pst = reinterpret_cast<unsigned long long*>(a.part) +
-                                    (size_t)gridDim.x * a.nsplit * r * (D / 2) + slot * r;
+    // share state: [row, kv head][share][r heads][D] outputs, then [..][r] (max, sum)
+    const size_t pair = (size_t)b * a.nkv + hk, pairs = (size_t)a.rows * a.nkv;
+    unsigned long long* const po = reinterpret_cast<unsigned long long*>(a.part) + pair * a.nsplit * r * (D / 2);
+    unsigned long long* const pst = reinterpret_cast<unsigned long long*>(a.part) + pairs * a.nsplit * r * (D / 2) + pair * a.nsplit * r;
     auto pack = [](float x, float y) { return (unsigned long long)__float_as_uint(y) << 32 | __float_as_uint(x); };
     const size_t orow = ((size_t)b * a.nq + hk * r) * D;
     bool bad = false;
@@ -366,25 +391,23 @@ __global__ void __launch_bounds__(64 * DEC_W) kv4_decode_kernel(Kv4AttnArgs a) {
         }
         reinterpret_cast<uint32_t*>(static_cast<uint16_t*>(a.out) + orow)[idx] = w;
     };
-    for (int idx = tid; idx < r * (D / 2); idx += 64 * DEC_W) {
+    for (int idx = tid; idx < r * (D / 2); idx += NT) {
         const int i = idx / (D / 2), d = 2 * (idx % (D / 2));
         float M = -INFINITY;
-#pragma unroll
-        for (int w = 0; w < DEC_W; w++) M = fmaxf(M, gst[w][i][0]);
+        for (int w = 0; w < W; w++) M = fmaxf(M, gst[w][i][0]);
         float x = 0.f, y = 0.f, lt = 0.f;
-#pragma unroll
-        for (int w = 0; w < DEC_W; w++) {
-            const float sc = gst[w][i][0] == -INFINITY ? 0.f : exp2f((gst[w][i][0] - M) * LOG2E);
-            x += sc * (ored[w][i][d] + glo[w][i][d / 32]);
-            y += sc * (ored[w][i][d + 1] + glo[w][i][d / 32]);
+        for (int w = 0; w < W; w++) {
+            const float sc = gst[w][i][0] == -INFINITY ? 0.f : exp2_hw((gst[w][i][0] - M) * LOG2E);
+            const float2 v = *reinterpret_cast<const float2*>(ored + (w * r + i) * D + d);
+            x += sc * (v.x + glo[w][i][d / 32]);
+            y += sc * (v.y + glo[w][i][d / 32]);
             lt += sc * gst[w][i][1];
         }
         if (n == 1) {
             put(idx, x, y, lt);
         } else {
             __hip_atomic_store(po + (size_t)part * r * (D / 2) + idx, pack(x, y), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-            if (d == 0)
-                __hip_atomic_store(pst + part * r + i, pack(M, lt), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+            if (d == 0) __hip_atomic_store(pst + part * r + i, pack(M, lt), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
         }
     }
     if (n > 1) {
@@ -392,18 +415,18 @@ __global__ void __launch_bounds__(64 * DEC_W) kv4_decode_kernel(Kv4AttnArgs a) {
         asm volatile("s_waitcnt vmcnt(0)" ::: "memory");   // this thread's stores are complete
         __syncthreads();
         if (tid == 0)
-            last_flag = __hip_atomic_fetch_add(a.cnt + blockIdx.x, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) + 1 ==
+            last_flag = __hip_atomic_fetch_add(a.cnt + pair, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) + 1 ==
                         (unsigned)n;
         __syncthreads();
         if (!last_flag) return;
-        float2* const st = reinterpret_cast<float2*>(&ored[0][0][0]);     // [share][r] (max, sum)
-        for (int i = tid; i < n * r; i += 64 * DEC_W) {
+        float2* const st = reinterpret_cast<float2*>(ored);     // [share][r] (max, sum)
+        for (int i = tid; i < n * r; i += NT) {
             const unsigned long long u = __hip_atomic_load(pst + i, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
             st[i] = float2{__uint_as_float((unsigned)u), __uint_as_float((unsigned)(u >> 32))};
         }
         __syncthreads();
         constexpr int CBK = 16;              // shares requested together
-        for (int idx = tid; idx < r * (D / 2); idx += 64 * DEC_W) {
+        for (int idx = tid; idx < r * (D / 2); idx += NT) {
             const int i = idx / (D / 2);
             float M = -INFINITY;
             for (int c = 0; c < n; c++) M = fmaxf(M, st[c * r + i].x);
@@ -412,14 +435,14 @@ __global__ void __launch_bounds__(64 * DEC_W) kv4_decode_kernel(Kv4AttnArgs a) {
                 unsigned long long v[CBK];
 #pragma unroll
                 for (int c = 0; c < CBK; c++)
-                    v[c] = __hip_atomic_load(po + (size_t)(c0 + c < n ? c0 + c : n - 1) * r * (D / 2) + idx,
+                    v[c] = __hip_atomic_load(po + (size_t)min(c0 + c, n - 1) * r * (D / 2) + idx,
                                              __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
 #pragma unroll
                 for (int c = 0; c < CBK; c++) {
                     if (c0 + c >= n) break;
                     const float2 s = st[(c0 + c) * r + i];
                     if (s.x == -INFINITY && s.y == 0.f) continue;
-                    const float w = exp2f((s.x - M) * LOG2E);
+                    const float w = exp2_hw((s.x - M) * LOG2E);
                     lt += w * s.y;
                     x += w * __uint_as_float((unsigned)v[c]);
                     y += w * __uint_as_float((unsigned)(v[c] >> 32));
@@ -849,38 +872,53 @@ __global__ void __launch_bounds__(64 * PF_W) kv4_prefill_merge_kernel(Kv4AttnArg
 
 }  // namespace
 
+// Waves per block and shares per (row, kv head).  A block costs about 5 us to begin
+// and end and 0.12 us a tile (eight waves to a CU; d = 128), a second share the clearing launch and the
+// hand-off, about 3.5 us: below 32 tiles one block is the faster.  Else a tile per
+// wave, as long as the blocks fit the CUs at once (two to a CU; one of more than 4 heads
+// of d = 128).  Llama-8B shape, 1 row of 2048 keys: 1 share 13.3 us, 2 12.4, 4
+// 10.4, 8 9.7, 16 10.5; 16 rows of up to 32768: 1 192, 2 114, 4 105, 8 109; Qwen-0.5B,
+// 512 keys: 1 5.7, 2 8.2; Qwen-7B, 8 rows of up to 8192: 4 26.5, 8 20.1, 16 29.3.
 Kv4DecodePlan kv4_decode_plan(int rows, int nkv, int r, int d, int max_ctx) {
-    const long long tiles = ((long long)max_ctx + KV4_TILE) / KV4_TILE, groups = (long long)rows * nkv;
+    const long long tiles = ((long long)max_ctx + KV4_TILE) / KV4_TILE, pairs = (long long)rows * nkv;
+    const bool wide = d == 128 && r > 4;
     Kv4DecodePlan p;
-    const long long want = (512 + groups - 1) / groups;
-    p.nsplit = (int)std::max(1ll, std::min({want, (tiles + 2 * DEC_W - 1) / (2 * DEC_W), 256ll}));
-    p.part_bytes = p.nsplit > 1 ? (size_t)groups * p.nsplit * r * (d + 2) * 4 : 0;
-    p.cnt_bytes = p.nsplit > 1 ? (size_t)groups * 4 : 0;
+    p.waves = 8;
+    const long long n = tiles < 32 ? 1 : std::min((wide ? 1 : 2) * kCus / pairs, (tiles + p.waves - 1) / p.waves);
+    p.nsplit = (int)std::max(1ll, std::min({n, tiles, kMaxShares / pairs + 1}));
     return p;
 }
 
 // Share states of any plan up to `rows` and max_ctx (grows with both).
 size_t kv4_decode_part_bound(int rows, int nkv, int r, int d, int max_ctx) {
-    const long long tiles = ((long long)max_ctx + KV4_TILE) / KV4_TILE, groups = (long long)rows * nkv;
-    const long long shares = std::min(groups * ((tiles + 2 * DEC_W - 1) / (2 * DEC_W)), groups + 511);
-    return (size_t)shares * r * (d + 2) * 4;
+    const long long tiles = ((long long)max_ctx + KV4_TILE) / KV4_TILE, pairs = (long long)rows * nkv;
+    return (size_t)std::min(pairs * tiles, pairs + kMaxShares) * r * (d + 2) * 4;
 }
 
-int launch_kv4_decode(const Kv4AttnArgs& a, bool zeroed, hipStream_t stream) {
-    const int r = a.nq / a.nkv;
-    if (r < 1 || r > MAXR || a.nsplit < 1 || (a.nsplit > 1 && (!a.part || !a.cnt))) return -1;
-    const int groups = a.rows * a.nkv;
-    if (a.nsplit > 1 && !zeroed)
-        hipLaunchKernelGGL(kv4_zero_kernel, dim3((groups + 255) / 256), dim3(256), 0, stream, a.cnt, groups);
-    const dim3 grid(groups, a.nsplit), block(64 * DEC_W);
-    if (a.d == 128 && r <= 4) hipLaunchKernelGGL((kv4_decode_kernel<128, 1>), grid, block, 0, stream, a);
-    else if (a.d == 128) hipLaunchKernelGGL((kv4_decode_kernel<128, 2>), grid, block, 0, stream, a);
-    else if (a.d == 64) hipLaunchKernelGGL((kv4_decode_kernel<64, 1>), grid, block, 0, stream, a);
-    else return -1;
+template <int D, int CT>
+static int launch_decode(const Kv4AttnArgs& a, int waves, hipStream_t stream) {
+    // the waves' outputs; over them the shares' statistics
+    const size_t lds = std::max((size_t)waves * a.r * D * 4, (size_t)a.nsplit * a.r * 8);
+    static LdsLimit lim;
+    if (ensure_lds_limit(lim, (const void*)kv4_decode_kernel<D, CT>, lds)) return -1;
+    hipLaunchKernelGGL((kv4_decode_kernel<D, CT>), dim3(a.nkv, a.nsplit, a.rows), dim3(64 * waves), lds, stream, a);
     return hipGetLastError() == hipSuccess ? 0 : -1;
 }
 
-constexpr int kCus = 256;
+int launch_kv4_decode(const Kv4AttnArgs& args, int waves, bool zeroed, hipStream_t stream) {
+    Kv4AttnArgs a = args;
+    const int r = a.r = a.nq / a.nkv, pairs = a.rows * a.nkv;
+    const int tiles = (int)(((long long)a.max_ctx + KV4_TILE) / KV4_TILE);
+    if (r < 1 || r > MAXR || waves < 1 || waves > MAXW || a.nsplit < 1 || a.nsplit > tiles) return -1;
+    if (a.nsplit > 1 && (!a.part || !a.cnt)) return -1;
+    a.per = (tiles + a.nsplit - 1) / a.nsplit;
+    a.nsplit = (tiles + a.per - 1) / a.per;              // (no share beyond the longest context)
+    if (a.nsplit > 1 && !zeroed)
+        hipLaunchKernelGGL(kv4_zero_kernel, dim3((pairs + 255) / 256), dim3(256), 0, stream, a.cnt, pairs);
+    if (a.d == 128 && r <= 4) return launch_decode<128, 1>(a, waves, stream);
+    if (a.d == 128) return waves <= 8 ? launch_decode<128, 2>(a, waves, stream) : -1;
+    return a.d == 64 ? launch_decode<64, 1>(a, waves, stream) : -1;
+}
 
 Kv4PrefillPlan kv4_prefill_plan(int T, int hist, int nkv, int r, int d) {
     const int R = T * r, nqt = (R + PF_ROWS - 1) / PF_ROWS;
