@@ -475,7 +475,7 @@ PrefillWs plan_prefill(const layer_s* L, int T, int hist) {
     return w;
 }
 
-struct DecodeWs { size_t q, part, attn, h, g, xn, kv, cnt, total; int nsplit, waves; };
+struct DecodeWs { size_t q, part, attn, h, g, xn, kv, total; int nsplit, waves; };
 DecodeWs plan_decode(const layer_s* L, int B, int max_ctx) {
     const layer_config& c = L->cfg;
     const size_t qd = (size_t)c.n_heads * c.head_dim;
@@ -501,7 +501,6 @@ DecodeWs plan_decode(const layer_s* L, int B, int max_ctx) {
     w.g = cv.take((size_t)B * L->F_pad * 2);
     w.xn = cv.take((size_t)B * c.hidden * 2);
     w.kv = cv.take(kv4 ? kv_stage_bytes(L, B) : 0);
-    w.cnt = cv.take(kv4 ? (size_t)B * c.n_kv_heads * 4 : 0);
     w.total = cv.off;
     return w;
 }
@@ -833,8 +832,8 @@ int run_decode_seq(layer_s* L, const float* x, const int32_t* pos, const int32_t
     gemv_resid_plan(a4, ordered);
     a1.clear = h;
     a1.nclear = a2.ksplit > 1 ? B * H : 0;
-    a1.zero = kv4 ? (unsigned*)(base + w.cnt) : (unsigned*)g;     // the attention's arrival counters
-    a1.nzero = w.nsplit > 1 ? B * c.n_kv_heads : 0;
+    a1.zero = (unsigned*)g;                 // the attention's arrival counters
+    a1.nzero = !kv4 && w.nsplit > 1 ? B * c.n_kv_heads : 0;
     // the rows are normalised in every block, or, many of them, once beforehand
     const bool prenorm = !gemv_norm_fits(B, H);
     f16* xn = (f16*)(base + w.xn);
@@ -851,9 +850,8 @@ int run_decode_seq(layer_s* L, const float* x, const int32_t* pos, const int32_t
         ka.mask = attn_mask;
         ka.nsplit = w.nsplit;
         ka.part = part;
-        ka.cnt = (unsigned*)(base + w.cnt);
         ProfScope ps(L, ps_stage, ps_stage == 2 ? 1 : 2, st);
-        rc |= launch_kv4_decode(ka, w.waves, true, st);
+        rc |= launch_kv4_decode(ka, w.waves, st);
     }
     AttnDecodeArgs ad{};
     ad.q = q;
@@ -1503,25 +1501,12 @@ static int check_kv4_heads(const kv4_desc* d, int32_t n_heads) {
     return W4_OK;
 }
 
-// Workspace of a decode: for the plan of any batch up to B and context up to max_ctx.
-struct Kv4DecodeWs {
-    size_t cnt, part, total;
-};
-static Kv4DecodeWs kv4_decode_ws(const kv4_desc* d, int32_t n_heads, int32_t B, int32_t max_ctx) {
-    const int r = n_heads / d->n_kv_heads;
-    Carve cv;
-    Kv4DecodeWs w;
-    w.cnt = cv.take(std::max((size_t)256, (size_t)B * d->n_kv_heads * 4));
-    w.part = cv.take(kv4_decode_part_bound(B, d->n_kv_heads, r, d->head_dim, max_ctx));
-    w.total = cv.off;
-    return w;
-}
-
 size_t kv4_attn_workspace_size(const kv4_desc* d, int32_t n_heads, int32_t stage, int32_t B, int32_t T,
                                int32_t max_ctx) {
     if (!d || stage < 0 || stage > 2 || max_ctx < 0 || check_kv4(d, stage == 2 ? B : 1) || check_kv4_heads(d, n_heads))
         return 0;
-    if (stage == 2) return kv4_decode_ws(d, n_heads, B, max_ctx).total;
+    if (stage == 2)          // (for the plan of any batch up to B and context up to max_ctx; never 0)
+        return std::max((size_t)256, kv4_decode_part_bound(B, d->n_kv_heads, n_heads / d->n_kv_heads, d->head_dim, max_ctx));
     if (T < 1) return 0;
     return kv4_prefill_plan(T, max_ctx, d->n_kv_heads, n_heads / d->n_kv_heads, d->head_dim).part_bytes;
 }
@@ -1562,12 +1547,10 @@ int kv4_attn_decode(const kv4_desc* d, const void* q, const int32_t* ctx_lens, i
     a.max_ctx = max_ctx;
     a.mask = attn_mask;
     a.rows = B;
-    const Kv4DecodeWs w = kv4_decode_ws(d, n_heads, B, max_ctx);
     const Kv4DecodePlan plan = kv4_decode_plan(B, d->n_kv_heads, n_heads / d->n_kv_heads, d->head_dim, max_ctx);
     a.nsplit = plan.nsplit;
-    a.cnt = (unsigned*)((char*)ws + w.cnt);
-    a.part = (float*)((char*)ws + w.part);
-    if (launch_kv4_decode(a, plan.waves, false, (hipStream_t)stream))
+    a.part = (float*)ws;
+    if (launch_kv4_decode(a, plan.waves, (hipStream_t)stream))
         return fail(W4_EHIP, "kernel launch failed: %s", hipGetErrorString(hipGetLastError()));
     return W4_OK;
 }

@@ -68,7 +68,6 @@ struct Kv4AttnArgs {
     float* part;             // decode: share states (nsplit > 1), [rows nkv][nsplit] of r (d + 2) floats; prefill: plan.part_bytes
     long long pf_units;      // prefill: set by the launcher
     int r, per;              // set by the launcher: nq / nkv; decode: tiles per share
-    unsigned* cnt;           // decode: [rows nkv] arrival counters (nsplit > 1)
     int* err;                // raised with W4_FLAG_F16_RANGE (out_f16), or null
 };
 struct Kv4DecodePlan {
@@ -76,8 +75,7 @@ struct Kv4DecodePlan {
 };
 Kv4DecodePlan kv4_decode_plan(int rows, int nkv, int r, int d, int max_ctx);
 size_t kv4_decode_part_bound(int rows, int nkv, int r, int d, int max_ctx);
-// zeroed: an earlier launch on the stream has cleared the counters
-int launch_kv4_decode(const Kv4AttnArgs& a, int waves, bool zeroed, hipStream_t stream);
+int launch_kv4_decode(const Kv4AttnArgs& a, int waves, hipStream_t stream);
 // Prefill: rows queries of one sequence after ctx_base tokens (part: part_bytes).
 struct Kv4PrefillPlan {
     long long units = 0;     // stages of one kv head's row tiles

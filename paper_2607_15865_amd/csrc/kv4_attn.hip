@@ -71,6 +71,19 @@ __device__ __forceinline__ float group_sum(float v) {
     return v;
 }
 
+// Output elements off, off + 1: sums x, y over the sum of the weights.
+__device__ __forceinline__ void put_pair(const Kv4AttnArgs& a, size_t off, float x, float y, float lt, bool& bad) {
+    const float u = lt == 0.f ? 0.f : x / lt, v = lt == 0.f ? 0.f : y / lt;              // (NaN stays)
+    uint32_t w;
+    if (a.out_f16) {
+        const f16 h0 = act_f16(u, bad), h1 = act_f16(v, bad);
+        w = (uint32_t)__builtin_bit_cast(uint16_t, h0) | (uint32_t)__builtin_bit_cast(uint16_t, h1) << 16;
+    } else {
+        w = (uint32_t)bf16_bits_rne(u) | (uint32_t)bf16_bits_rne(v) << 16;
+    }
+    *reinterpret_cast<uint32_t*>(static_cast<uint16_t*>(a.out) + off) = w;
+}
+
 // One block: a share (a.per tiles) of one (row, kv head), all r query heads of the
 // group.  Wave w of W takes tiles w, w + W, .. of the share on its own; the next
 // tile's K is requested when this one's scores are formed and its V when its
@@ -90,7 +103,6 @@ __global__ void __launch_bounds__(64 * MAXW, CT == 1 ? 4 : 2) kv4_decode_kernel(
     constexpr int TB = kv4_tile_bytes(D), CB = kv4_code_bytes(D);
     extern __shared__ __attribute__((aligned(16))) float ored[];          // [W][r][D]
     __shared__ float gst[MAXW][MAXR][2], glo[MAXW][MAXR][NS];
-    __shared__ unsigned last_flag;
     const int tid = threadIdx.x, lane = tid & 63, NT = blockDim.x, W = NT >> 6;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int hk = blockIdx.x, part = blockIdx.y, b = blockIdx.z, r = a.r;
@@ -180,7 +192,12 @@ __global__ void __launch_bounds__(64 * MAXW, CT == 1 ? 4 : 2) kv4_decode_kernel(
     ctx = min(ctx, a.max_ctx);
     const int ntiles = (ctx + KV4_TILE) / KV4_TILE;             // of ctx + 1 keys
     const int n = max(1, (ntiles + a.per - 1) / a.per);         // shares of this row
-    if (part >= n) return;
+    const size_t slot = (((size_t)b * a.nkv + hk) * a.nsplit + part) * r;      // of the share's state
+    float2* const pst = reinterpret_cast<float2*>(a.part + (size_t)a.rows * a.nq * a.nsplit * D) + slot;
+    if (part >= n) {
+        if (tid < r) pst[tid] = float2{-INFINITY, 0.f};
+        return;
+    }
     const int tile1 = min(tile0 + a.per, ntiles);
 
     f32x4 o[CT][NDB];
@@ -373,24 +390,9 @@ __global__ void __launch_bounds__(64 * MAXW, CT == 1 ? 4 : 2) kv4_decode_kernel(
             }
     }
     __syncthreads();
-    // share state: [row, kv head][share][r heads][D] outputs, then [..][r] (max, sum)
-    const size_t pair = (size_t)b * a.nkv + hk, pairs = (size_t)a.rows * a.nkv;
-    unsigned long long* const po = reinterpret_cast<unsigned long long*>(a.part) + pair * a.nsplit * r * (D / 2);
-    unsigned long long* const pst = reinterpret_cast<unsigned long long*>(a.part) + pairs * a.nsplit * r * (D / 2) + pair * a.nsplit * r;
-    auto pack = [](float x, float y) { return (unsigned long long)__float_as_uint(y) << 32 | __float_as_uint(x); };
-    const size_t orow = ((size_t)b * a.nq + hk * r) * D;
+    // one share: the output; more: its state, [row, kv head][share][r heads][D] outputs, then [..][r] (max, sum)
+    float* const po = a.part + slot * D;
     bool bad = false;
-    auto put = [&](int idx, float x, float y, float lt) __attribute__((always_inline)) {     // output pair idx
-        const float u = lt == 0.f ? 0.f : x / lt, v = lt == 0.f ? 0.f : y / lt;              // (NaN stays)
-        uint32_t w;
-        if (a.out_f16) {
-            const f16 h0 = act_f16(u, bad), h1 = act_f16(v, bad);
-            w = (uint32_t)__builtin_bit_cast(uint16_t, h0) | (uint32_t)__builtin_bit_cast(uint16_t, h1) << 16;
-        } else {
-            w = (uint32_t)bf16_bits_rne(u) | (uint32_t)bf16_bits_rne(v) << 16;
-        }
-        reinterpret_cast<uint32_t*>(static_cast<uint16_t*>(a.out) + orow)[idx] = w;
-    };
     for (int idx = tid; idx < r * (D / 2); idx += NT) {
         const int i = idx / (D / 2), d = 2 * (idx % (D / 2));
         float M = -INFINITY;
@@ -403,61 +405,88 @@ __global__ void __launch_bounds__(64 * MAXW, CT == 1 ? 4 : 2) kv4_decode_kernel(
             y += sc * (v.y + glo[w][i][d / 32]);
             lt += sc * gst[w][i][1];
         }
-        if (n == 1) {
-            put(idx, x, y, lt);
+        if (a.nsplit == 1) {
+            put_pair(a, ((size_t)b * a.nq + hk * r) * D + 2 * idx, x, y, lt, bad);
         } else {
-            __hip_atomic_store(po + (size_t)part * r * (D / 2) + idx, pack(x, y), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-            if (d == 0) __hip_atomic_store(pst + part * r + i, pack(M, lt), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-        }
-    }
-    if (n > 1) {
-        // the last share to arrive merges all of them, in their order
-        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");   // this thread's stores are complete
-        __syncthreads();
-        if (tid == 0)
-            last_flag = __hip_atomic_fetch_add(a.cnt + pair, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) + 1 ==
-                        (unsigned)n;
-        __syncthreads();
-        if (!last_flag) return;
-        float2* const st = reinterpret_cast<float2*>(ored);     // [share][r] (max, sum)
-        for (int i = tid; i < n * r; i += NT) {
-            const unsigned long long u = __hip_atomic_load(pst + i, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-            st[i] = float2{__uint_as_float((unsigned)u), __uint_as_float((unsigned)(u >> 32))};
-        }
-        __syncthreads();
-        constexpr int CBK = 16;              // shares requested together
-        for (int idx = tid; idx < r * (D / 2); idx += NT) {
-            const int i = idx / (D / 2);
-            float M = -INFINITY;
-            for (int c = 0; c < n; c++) M = fmaxf(M, st[c * r + i].x);
-            float x = 0.f, y = 0.f, lt = 0.f;
-            for (int c0 = 0; c0 < n; c0 += CBK) {
-                unsigned long long v[CBK];
-#pragma unroll
-                for (int c = 0; c < CBK; c++)
-                    v[c] = __hip_atomic_load(po + (size_t)min(c0 + c, n - 1) * r * (D / 2) + idx,
-                                             __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-#pragma unroll
-                for (int c = 0; c < CBK; c++) {
-                    if (c0 + c >= n) break;
-                    const float2 s = st[(c0 + c) * r + i];
-                    if (s.x == -INFINITY && s.y == 0.f) continue;
-                    const float w = exp2_hw((s.x - M) * LOG2E);
-                    lt += w * s.y;
-                    x += w * __uint_as_float((unsigned)v[c]);
-                    y += w * __uint_as_float((unsigned)(v[c] >> 32));
-                }
-            }
-            put(idx, x, y, lt);
+            *reinterpret_cast<float2*>(po + 2 * idx) = float2{x, y};
+            if (d == 0) pst[i] = float2{M, lt};
         }
     }
     flag_range(a.err, bad);
 }
 
-// Clears the arrival counters (a kernel, so that it can be captured).
-__global__ void __launch_bounds__(256) kv4_zero_kernel(unsigned* cnt, int n) {
-    const int i = blockIdx.x * 256 + threadIdx.x;
-    if (i < n) cnt[i] = 0u;
+// Merges the shares of a row and head: one block each, wave w takes shares w, w +
+// 4, ..; their order does not depend on timing.
+template <int D>
+__global__ void __launch_bounds__(256) kv4_decode_merge_kernel(Kv4AttnArgs a) {
+    constexpr int CB = 4, E = D / 64;        // shares of a wave requested together, dims of a lane
+    __shared__ float sm[4][2 + E][64];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int hk = blockIdx.x, i = blockIdx.y, b = blockIdx.z, n = a.nsplit;
+    const size_t slot = ((size_t)b * a.nkv + hk) * n * a.r + i;
+    const float* const po = a.part + slot * D + E * lane;
+    const float2* const pst = reinterpret_cast<const float2*>(a.part + (size_t)a.rows * a.nq * n * D) + slot;
+    float M = -INFINITY, L = 0.f, acc[E] = {};
+    for (int c0 = wave; c0 < n; c0 += 4 * CB) {
+        float2 s[CB];
+        float v[CB][E];
+#pragma unroll
+        for (int c = 0; c < CB; c++) {
+            const size_t o = (size_t)min(c0 + 4 * c, n - 1) * a.r;
+            s[c] = pst[o];
+#pragma unroll
+            for (int e = 0; e < E; e++) v[c][e] = po[o * D + e];
+        }
+        float Mn = M;
+#pragma unroll
+        for (int c = 0; c < CB; c++) {
+            // a share past the row's end has (-inf, 0) and no output
+            const bool none = c0 + 4 * c >= n || (s[c].x == -INFINITY && s[c].y == 0.f);
+            if (none) s[c] = float2{-INFINITY, 0.f};
+#pragma unroll
+            for (int e = 0; e < E; e++) v[c][e] = none ? 0.f : v[c][e];
+            Mn = fmaxf(Mn, s[c].x);
+        }
+        const float Mb = Mn == -INFINITY ? 0.f : Mn, keep = exp2_hw((M - Mb) * LOG2E);
+        L *= keep;
+#pragma unroll
+        for (int e = 0; e < E; e++) acc[e] *= keep;
+#pragma unroll
+        for (int c = 0; c < CB; c++) {
+            const float w = exp2_hw((s[c].x - Mb) * LOG2E);
+            L += w * s[c].y;
+#pragma unroll
+            for (int e = 0; e < E; e++) acc[e] += w * v[c][e];
+        }
+        M = Mn;
+    }
+    sm[wave][0][lane] = M;
+    sm[wave][1][lane] = L;
+#pragma unroll
+    for (int e = 0; e < E; e++) sm[wave][2 + e][lane] = acc[e];
+    __syncthreads();
+    if (wave) return;
+    const float Mn = fmaxf(fmaxf(sm[0][0][lane], sm[1][0][lane]), fmaxf(sm[2][0][lane], sm[3][0][lane]));
+    const float Mb = Mn == -INFINITY ? 0.f : Mn;
+    L = 0.f;
+#pragma unroll
+    for (int e = 0; e < E; e++) acc[e] = 0.f;
+#pragma unroll
+    for (int w = 0; w < 4; w++) {
+        const float f = exp2_hw((sm[w][0][lane] - Mb) * LOG2E);
+        L += f * sm[w][1][lane];
+#pragma unroll
+        for (int e = 0; e < E; e++) acc[e] += f * sm[w][2 + e][lane];
+    }
+    bool bad = false;
+    const size_t off = ((size_t)b * a.nq + hk * a.r + i) * D + E * lane;
+    if constexpr (E == 2) {
+        put_pair(a, off, acc[0], acc[1], L, bad);
+    } else {
+        const float next = __shfl_down(acc[0], 1, 64);
+        if (!(lane & 1)) put_pair(a, off, acc[0], next, L, bad);
+    }
+    flag_range(a.err, bad);
 }
 
 // ---------------------------------------------------------------- prefill
@@ -897,24 +926,20 @@ size_t kv4_decode_part_bound(int rows, int nkv, int r, int d, int max_ctx) {
 
 template <int D, int CT>
 static int launch_decode(const Kv4AttnArgs& a, int waves, hipStream_t stream) {
-    // the waves' outputs; over them the shares' statistics
-    const size_t lds = std::max((size_t)waves * a.r * D * 4, (size_t)a.nsplit * a.r * 8);
-    static LdsLimit lim;
-    if (ensure_lds_limit(lim, (const void*)kv4_decode_kernel<D, CT>, lds)) return -1;
+    const size_t lds = (size_t)waves * a.r * D * 4;       // the waves' outputs (at most 32 KB)
     hipLaunchKernelGGL((kv4_decode_kernel<D, CT>), dim3(a.nkv, a.nsplit, a.rows), dim3(64 * waves), lds, stream, a);
+    if (a.nsplit > 1) hipLaunchKernelGGL(kv4_decode_merge_kernel<D>, dim3(a.nkv, a.r, a.rows), dim3(256), 0, stream, a);
     return hipGetLastError() == hipSuccess ? 0 : -1;
 }
 
-int launch_kv4_decode(const Kv4AttnArgs& args, int waves, bool zeroed, hipStream_t stream) {
+int launch_kv4_decode(const Kv4AttnArgs& args, int waves, hipStream_t stream) {
     Kv4AttnArgs a = args;
-    const int r = a.r = a.nq / a.nkv, pairs = a.rows * a.nkv;
+    const int r = a.r = a.nq / a.nkv;
     const int tiles = (int)(((long long)a.max_ctx + KV4_TILE) / KV4_TILE);
     if (r < 1 || r > MAXR || waves < 1 || waves > MAXW || a.nsplit < 1 || a.nsplit > tiles) return -1;
-    if (a.nsplit > 1 && (!a.part || !a.cnt)) return -1;
+    if (a.nsplit > 1 && !a.part) return -1;
     a.per = (tiles + a.nsplit - 1) / a.nsplit;
     a.nsplit = (tiles + a.per - 1) / a.per;              // (no share beyond the longest context)
-    if (a.nsplit > 1 && !zeroed)
-        hipLaunchKernelGGL(kv4_zero_kernel, dim3((pairs + 255) / 256), dim3(256), 0, stream, a.cnt, pairs);
     if (a.d == 128 && r <= 4) return launch_decode<128, 1>(a, waves, stream);
     if (a.d == 128) return waves <= 8 ? launch_decode<128, 2>(a, waves, stream) : -1;
     return a.d == 64 ? launch_decode<64, 1>(a, waves, stream) : -1;
