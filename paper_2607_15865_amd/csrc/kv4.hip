@@ -2,16 +2,91 @@
 // definition of the codes: kv4.h).
 //
 // Both kernels are streams: bf16 rows on one side, 5 bits a value on the other.
-// A block has one tile of 32 tokens of one (row, kv head): two waves take K (16
-// tokens each), two take V.  The lanes of a wave are laid out so that a lane
-// holds whole words and, of the parameters, whole groups with one or two lane
-// exchanges: for K a lane has the 8 dims of each group that form its words; for
-// V, whose words span 8 tokens, it has 8 dims of its token in four dim
-// blocks, and the eight lanes of a token block transpose their 8x8 nibbles by three
-// exchanges.
+// A lane has one group (32 dims of one token): the group's extremes, scale and
+// codes need no other lane.  A wave has 64 / NS tokens of K or of V.  In memory the NS
+// lanes of a token take 16 bytes of each group side by side, and a transpose among them
+// gives each its group (a lane that reads its own 64 bytes costs the largest read
+// 11 us of 47).  V, whose words span 8 tokens: the eight lanes of a token block
+// transpose their 8x8 nibbles, one word of dims each for one word of tokens, in
+// three exchanges; a run that ends inside a block replaces its nibbles alone.
+#include <type_traits>
+
 #include "kv4.h"
 
 namespace {
+
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+
+template <int CTRL>
+__device__ __forceinline__ uint32_t dpp_u32(uint32_t x) {
+    return (uint32_t)__builtin_amdgcn_mov_dpp((int)x, CTRL, 0xF, 0xF, false);
+}
+
+// The value of lane ^ M.
+template <int M>
+__device__ __forceinline__ uint32_t lane_xor(uint32_t x) {
+    static_assert(M == 1 || M == 2 || M == 4 || M == 8 || M == 16, "");
+    if constexpr (M == 1) return dpp_u32<0xB1>(x);
+    if constexpr (M == 2) return dpp_u32<0x4E>(x);
+    if constexpr (M == 4) return dpp_u32<0x1B>(dpp_u32<0x141>(x));           // mirrored in 8, then in 4
+    if constexpr (M == 8) return dpp_u32<0x128>(x);                          // rotated by 8 in 16
+    return (uint32_t)__builtin_amdgcn_ds_swizzle((int)x, 0x401F);            // (lane ^ 16)
+}
+
+// 8x8 nibble transpose over the eight lanes that differ in the bits M, 2 M, 4 M of
+// their number: nibble j of the lane with bits i becomes nibble i of the lane with bits j.
+template <int M>
+__device__ __forceinline__ uint32_t nibble_transpose(uint32_t w, int lane) {
+    uint32_t p = lane_xor<4 * M>(w);
+    w = lane & 4 * M ? (w & 0xFFFF0000u) | p >> 16 : (w & 0x0000FFFFu) | p << 16;
+    p = lane_xor<2 * M>(w);
+    w = lane & 2 * M ? (w & 0xFF00FF00u) | (p >> 8 & 0x00FF00FFu) : (w & 0x00FF00FFu) | (p & 0x00FF00FFu) << 8;
+    p = lane_xor<M>(w);
+    return lane & M ? (w & 0xF0F0F0F0u) | (p >> 4 & 0x0F0F0F0Fu) : (w & 0x0F0F0F0Fu) | (p & 0x0F0F0F0Fu) << 4;
+}
+
+// Transpose of x[i] among the NS lanes of a token: afterwards (NS 4) x[i] of lane s is
+// what x[s] of lane i was; (NS 2) what x[2 s + i / 2] of lane i % 2 was.  For NS 4 it is its own
+// inverse; for NS 2 `back` undoes it.
+template <int NS, typename T>
+__device__ __forceinline__ void group_transpose(T (&x)[4], int lane, bool back = false) {
+    auto swap2 = [&](T& p, T& q, auto m) __attribute__((always_inline)) {     // 2x2: off-diagonal elements change lanes
+        constexpr int M = decltype(m)::value;
+        const bool odd = lane & M;
+        constexpr int W = sizeof(T) / 4;
+        uint32_t pw[W], qw[W];
+        __builtin_memcpy(pw, &p, sizeof(T));
+        __builtin_memcpy(qw, &q, sizeof(T));
+#pragma unroll
+        for (int k = 0; k < W; k++) {
+            const uint32_t a = lane_xor<M>(qw[k]), b = lane_xor<M>(pw[k]);
+            pw[k] = odd ? a : pw[k];
+            qw[k] = odd ? qw[k] : b;
+        }
+        __builtin_memcpy(&p, pw, sizeof(T));
+        __builtin_memcpy(&q, qw, sizeof(T));
+    };
+    if constexpr (NS == 4) {
+        swap2(x[0], x[1], std::integral_constant<int, 1>{});
+        swap2(x[2], x[3], std::integral_constant<int, 1>{});
+        swap2(x[0], x[2], std::integral_constant<int, 2>{});
+        swap2(x[1], x[3], std::integral_constant<int, 2>{});
+    } else {
+        T t;
+        if (back) { t = x[1]; x[1] = x[2]; x[2] = t; }
+        swap2(x[0], x[2], std::integral_constant<int, 1>{});
+        swap2(x[1], x[3], std::integral_constant<int, 1>{});
+        if (!back) { t = x[1]; x[1] = x[2]; x[2] = t; }
+    }
+}
+
+// Dims of the 16 bytes that a token's lane s takes as its i-th: (NS 4) chunk s of group i; (NS 2) chunk 2 (i % 2) + s of
+// group i / 2.
+template <int NS>
+__device__ __forceinline__ int chunk_dim(int s, int i) { return NS == 4 ? 32 * i + 8 * s : 32 * (i >> 1) + 16 * (i & 1) + 8 * s; }
+
+// Token (of eight) whose code is nibble n of a V word.
+__device__ __forceinline__ int nibble_elem(int n) { return 2 * (n & 3) + (n >> 2); }
 
 // The code of x in a group (lo, s), r = 1 / s roughly: exact.  floor((x - lo) / s)
 // by the reciprocal may be one off next to a whole number, where the border
@@ -33,181 +108,175 @@ __device__ __forceinline__ uint32_t kv4_code(float x, float lo, float s, float r
     return (uint32_t)(c < 15 ? c : 15);
 }
 
+// A group: its values as fp16 pairs, parameters, and the line z = x r + b whose
+// whole part is the code, but for values within eps of a border.
 struct Kv4Group {
-    float lo, s, r;
-    uint16_t lo_bits, s_bits;
-    bool bad;
+    f16x2 x[16];
+    float lo, s, r, b, eps;
+    uint32_t params;             // scale bits | offset bits << 16
+    bool bad, clamp;
 };
 
-// Parameters of a group from its extremes and the largest |x| bits (bf16).  The
-// scale is formed in fp64: (hi - lo) / 15 rounded to fp16 is then the nearest.
-__device__ __forceinline__ Kv4Group kv4_group(float lo, float hi, uint32_t amax) {
-    Kv4Group g;
-    g.bad = amax > 0x477Fu;                                  // beyond 65280, the largest bf16 value in fp16
-    const f16 s = (f16)(float)(((double)hi - (double)lo) * (1.0 / 15.0));
-    g.s = (float)s;
-    g.lo = lo;
-    g.s_bits = g.bad ? (uint16_t)0x7E00u : __builtin_bit_cast(uint16_t, s);
-    g.lo_bits = g.bad ? (uint16_t)0x7E00u : __builtin_bit_cast(uint16_t, (f16)lo);
+__device__ __forceinline__ void kv4_group(Kv4Group& g, const u32x4 (&in)[4]) {
+#pragma unroll
+    for (int i = 0; i < 16; i++) {
+        const uint32_t w = in[i / 4][i % 4];
+        g.x[i] = f16x2{(f16)__uint_as_float(w << 16), (f16)__uint_as_float(w & 0xFFFF0000u)};
+    }
+    f16x2 mn = g.x[0], mx = g.x[0], nan = g.x[0] * (f16)0.f;
+#pragma unroll
+    for (int i = 1; i < 16; i++) {
+        mn = __builtin_elementwise_min(mn, g.x[i]);
+        mx = __builtin_elementwise_max(mx, g.x[i]);
+        nan = __builtin_elementwise_fma(g.x[i], f16x2{(f16)0.f, (f16)0.f}, nan);     // (NaN of an infinity or a NaN)
+    }
+    g.bad = !((float)nan[0] + (float)nan[1] == 0.f);
+    const f16 lo = mn[0] < mn[1] ? mn[0] : mn[1], hi = mx[0] > mx[1] ? mx[0] : mx[1];
+    // (in fp64 the quotient rounded to fp16 is the nearest)
+    const f16 s = (f16)(float)(((double)(float)hi - (double)(float)lo) * (1.0 / 15.0));
+    g.lo = g.bad ? 0.f : (float)lo;
+    g.s = g.bad ? 0.f : (float)s;
     g.r = g.s > 0.f ? __builtin_amdgcn_rcpf(g.s) : 0.f;
-    return g;
+    g.b = __builtin_fmaf(-g.lo, g.r, 0.5f);
+    // z's error: of the reciprocal (2^-22), of b's rounding and of the fma's
+    g.eps = (__builtin_fabsf(g.lo * g.r) + 16.f) * 0x1p-20f;
+    g.clamp = !g.bad && __builtin_fmaf((float)hi, g.r, g.b) >= 15.9f;                // (a scale among the subnormals)
+    g.params = g.bad ? 0x7E007E00u : (uint32_t)__builtin_bit_cast(uint16_t, s) | (uint32_t)__builtin_bit_cast(uint16_t, lo) << 16;
 }
 
-// Eight bf16 values as the fp32 values of their fp16 values.
-struct Kv4Vals {
-    float x[8];
-    float lo, hi;
-    uint32_t amax;
-};
-__device__ __forceinline__ Kv4Vals kv4_load8(u32x4 w) {
-    Kv4Vals v;
-    v.amax = 0;
+// Codes of values 8 w .. + 7 of the group; element e at nibble e (NAT) or at bits 4 (e / 2) + 16 (e % 2).
+template <bool NAT>
+__device__ __forceinline__ uint32_t kv4_word(const Kv4Group& g, int w) {
+    float c[8], fmn = 1.f, fmx = 0.f;
 #pragma unroll
-    for (int j = 0; j < 4; j++) {
-        v.x[2 * j] = (float)(f16)__uint_as_float(w[j] << 16);
-        v.x[2 * j + 1] = (float)(f16)__uint_as_float(w[j] & 0xFFFF0000u);
-        v.amax = max(v.amax, max(w[j] & 0x7FFFu, w[j] >> 16 & 0x7FFFu));
+    for (int e = 0; e < 8; e++) {
+        const float z = __builtin_fmaf((float)g.x[4 * w + e / 2][e % 2], g.r, g.b), f = __builtin_amdgcn_fractf(z);
+        c[e] = z - f;
+        fmn = fminf(fmn, f);
+        fmx = fmaxf(fmx, f);
     }
-    v.lo = v.x[0];
-    v.hi = v.x[0];
+    if (fmn < g.eps || fmx > 1.f - g.eps || g.clamp) {
 #pragma unroll
-    for (int j = 1; j < 8; j++) {
-        v.lo = fminf(v.lo, v.x[j]);
-        v.hi = fmaxf(v.hi, v.x[j]);
+        for (int e = 0; e < 8; e++) c[e] = (float)kv4_code((float)g.x[4 * w + e / 2][e % 2], g.lo, g.s, g.r);
+        if (g.s == 0.f)
+#pragma unroll
+            for (int e = 0; e < 8; e++) c[e] = 0.f;
     }
-    return v;
+    // four codes are summed up as one number below 2^16
+    const int o = NAT ? 1 : 2;
+    const float a0 = __builtin_fmaf(__builtin_fmaf(__builtin_fmaf(c[3 * o], 16.f, c[2 * o]), 16.f, c[o]), 16.f, c[0]);
+    const int h = NAT ? 4 : 1;
+    const float a1 = __builtin_fmaf(__builtin_fmaf(__builtin_fmaf(c[h + 3 * o], 16.f, c[h + 2 * o]), 16.f, c[h + o]), 16.f, c[h]);
+    return (uint32_t)a0 | (uint32_t)a1 << 16;
 }
 
-__device__ __forceinline__ uint32_t xor_lane(uint32_t v, int m) { return (uint32_t)__shfl_xor((int)v, m, 64); }
-
-// 8x8 nibble transpose over the lanes of an aligned group of eight: nibble j of
-// lane i becomes nibble i of lane j.
-__device__ __forceinline__ uint32_t nibble_transpose(uint32_t w, int lane) {
-    uint32_t p = xor_lane(w, 4);
-    w = lane & 4 ? (w & 0xFFFF0000u) | p >> 16 : (w & 0x0000FFFFu) | p << 16;
-    p = xor_lane(w, 2);
-    w = lane & 2 ? (w & 0xFF00FF00u) | (p >> 8 & 0x00FF00FFu) : (w & 0x00FF00FFu) | (p & 0x00FF00FFu) << 8;
-    p = xor_lane(w, 1);
-    return lane & 1 ? (w & 0xF0F0F0F0u) | (p >> 4 & 0x0F0F0F0Fu) : (w & 0x0F0F0F0Fu) | (p & 0x0F0F0F0Fu) << 4;
-}
-
-// Token (of eight) whose code is nibble n of a V word, and the bit position of element e of a word.
-__device__ __forceinline__ int nibble_elem(int n) { return 2 * (n & 3) + (n >> 2); }
-__host__ __device__ constexpr int elem_bit(int e) { return 4 * (e / 2) + 16 * (e % 2); }
-
-// What a block works on: tile `tile` of row b, its tokens lo .. hi - 1 (of 32) in the row's run.
+// A wave's work: K or V of 64 / NS tokens (from tok0 of a tile) of a (row, kv head).
 struct Kv4Work {
-    int b, g, tile, lo, hi;
-    int t0;                  // token of the run at the tile's first slot (may be negative)
+    int b, g, tile, lo, hi;      // tokens lo .. hi - 1 of the tile's 32 are in the row's run
+    int t0;                      // token of the run at the tile's first slot (may be negative)
+    int tok0;
+    bool v;
 };
+template <int D>
 __device__ __forceinline__ bool kv4_work(const Kv4StoreArgs& a, Kv4Work& w) {
+    constexpr int WPT = D / 64;                              // waves per tile of K (or V)
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), item = wave / (2 * WPT);
     w.b = blockIdx.z;
     w.g = blockIdx.y;
+    w.v = wave / WPT % 2;
+    w.tok0 = wave % WPT * (KV4_TILE / WPT);
     const int s0 = a.slots_dev ? a.slots_dev[w.b] : a.slots.v[w.b];
     if (s0 < 0 || s0 > a.max_seq - a.T) return false;
-    w.tile = s0 / KV4_TILE + blockIdx.x;
+    w.tile = s0 / KV4_TILE + blockIdx.x * (2 / WPT) + item;
     w.t0 = w.tile * KV4_TILE - s0;
     w.lo = max(0, -w.t0);
     w.hi = min(KV4_TILE, a.T - w.t0);
-    return w.lo < w.hi;
+    return max(w.lo, w.tok0) < min(w.hi, w.tok0 + KV4_TILE / WPT);
 }
+
+// Lane (token, group lane % NS): tokens in order for K, for V in nibble order in blocks of 8.
+template <int D>
+struct Kv4Lane {
+    static constexpr int NS = D / 32;
+    int tok, s, j, blk;
+    __device__ __forceinline__ Kv4Lane(const Kv4Work& w) {
+        const int lane = threadIdx.x & 63;
+        s = lane % NS;
+        j = lane / NS % 8;
+        blk = w.tok0 / 8 + lane / (8 * NS);
+        tok = w.v ? 8 * blk + nibble_elem(j) : w.tok0 + lane / NS;
+    }
+    // K: first word of lane (n16, q4) of the token
+    __device__ __forceinline__ int k_word(int q4) const {
+        return ((tok >> 2 & 1) * 64 + q4 * 16 + ((tok >> 3) << 2 | (tok & 3))) * NS;
+    }
+    // V: words of dim blocks 2 s, 2 s + 1 (two in a row) of lane (j, q4 = blk), and 8 lanes on
+    __device__ __forceinline__ int v_word() const { return ((s >> 1) * 64 + blk * 16 + j) * 4 + 2 * (s & 1); }
+};
 
 template <int D>
 __global__ void __launch_bounds__(256) kv4_append_kernel(Kv4StoreArgs a) {
     constexpr int NS = D / 32;
     Kv4Work w;
-    if (!kv4_work(a, w)) return;
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const long long xrow = (long long)w.b * a.x_b + (long long)w.t0 * a.x_t + (long long)w.g * a.x_h;
-    const long long base = (long long)w.b * a.stride_b + (long long)w.g * a.stride_h + (long long)w.tile * kv4_tile_bytes(D);
-    bool bad = false;
-    if (wave < 2) {          // K: lane (token, q4)
-        const int q4 = lane & 3, tok = 16 * wave + (lane >> 2);
-        const bool on = tok >= w.lo && tok < w.hi;
-        u32x4 in[NS];
+    if (!kv4_work<D>(a, w)) return;
+    const int lane = threadIdx.x & 63;
+    const Kv4Lane<D> at(w);
+    const bool on = at.tok >= w.lo && at.tok < w.hi;
+    const uint16_t* const x = (w.v ? a.v_x : a.k_x) + ((long long)w.b * a.x_b + (long long)w.g * a.x_h +
+                                                       (long long)(w.t0 + at.tok) * a.x_t);
+    uint8_t* const tile = (w.v ? a.v : a.k) + ((long long)w.b * a.stride_b + (long long)w.g * a.stride_h +
+                                               (long long)w.tile * kv4_tile_bytes(D));
+    u32x4 in[4];
 #pragma unroll
-        for (int s = 0; s < NS; s++)
-            in[s] = on ? *reinterpret_cast<const u32x4*>(a.k_x + xrow + tok * a.x_t + 32 * s + 8 * q4) : u32x4{0u, 0u, 0u, 0u};
-        uint32_t word[NS];
-        uint16_t* const par = reinterpret_cast<uint16_t*>(a.k + base + kv4_code_bytes(D));
-#pragma unroll
-        for (int s = 0; s < NS; s++) {
-            Kv4Vals x = kv4_load8(in[s]);
-#pragma unroll
-            for (int m = 1; m < 4; m *= 2) {
-                x.lo = fminf(x.lo, __shfl_xor(x.lo, m, 64));
-                x.hi = fmaxf(x.hi, __shfl_xor(x.hi, m, 64));
-                x.amax = max(x.amax, xor_lane(x.amax, m));
-            }
-            const Kv4Group g = kv4_group(x.lo, x.hi, x.amax);
-            word[s] = 0;
-#pragma unroll
-            for (int e = 0; e < 8; e++) word[s] |= kv4_code(x.x[e], g.lo, g.s, g.r) << elem_bit(e);
-            if (g.s == 0.f || g.bad) word[s] = 0;
-            bad |= g.bad;
-            if (on && q4 == s) {
-                par[s * 64 + tok] = g.s_bits;
-                par[s * 64 + 32 + tok] = g.lo_bits;
-            }
-        }
-        const int t = tok >> 2 & 1, n16 = (tok >> 3) << 2 | (tok & 3);
-        uint32_t* const dst = reinterpret_cast<uint32_t*>(a.k + base) + (t * 64 + q4 * 16 + n16) * NS;
-        if (on) {
-#pragma unroll
-            for (int s = 0; s < NS; s++) dst[s] = word[s];
-        }
-    } else {                 // V: lane (token of a block of 8 in nibble order, dims' upper half of 16, half of D or token block)
-        const int j = lane & 7, nhi = lane >> 3 & 1;
-        const int hf = NS == 4 ? lane >> 4 & 1 : 0;
-        const int blk = NS == 4 ? 2 * (wave - 2) + (lane >> 5) : lane >> 4;    // block of 8 tokens
-        if (NS == 2 && wave == 3) return;
-        const int tok = 8 * blk + nibble_elem(j);
-        const bool on = tok >= w.lo && tok < w.hi;
-        u32x4 in[4];
-#pragma unroll
-        for (int i = 0; i < 4; i++)
-            in[i] = on ? *reinterpret_cast<const u32x4*>(a.v_x + xrow + tok * a.x_t + 16 * (4 * hf + i) + 8 * nhi)
-                       : u32x4{0u, 0u, 0u, 0u};
-        u32x4 word;
-        uint16_t* const par = reinterpret_cast<uint16_t*>(a.v + base + kv4_code_bytes(D));
-#pragma unroll
-        for (int p = 0; p < 2; p++) {          // a group: dim blocks 2 p and 2 p + 1, this lane and its neighbour
-            const Kv4Vals x0 = kv4_load8(in[2 * p]), x1 = kv4_load8(in[2 * p + 1]);
-            float lo = fminf(x0.lo, x1.lo), hi = fmaxf(x0.hi, x1.hi);
-            uint32_t amax = max(x0.amax, x1.amax);
-            lo = fminf(lo, __shfl_xor(lo, 8, 64));
-            hi = fmaxf(hi, __shfl_xor(hi, 8, 64));
-            amax = max(amax, xor_lane(amax, 8));
-            const Kv4Group g = kv4_group(lo, hi, amax);
-            uint32_t w0 = 0, w1 = 0;
-#pragma unroll
-            for (int e = 0; e < 8; e++) {
-                w0 |= kv4_code(x0.x[e], g.lo, g.s, g.r) << (4 * e);
-                w1 |= kv4_code(x1.x[e], g.lo, g.s, g.r) << (4 * e);
-            }
-            if (g.s == 0.f || g.bad) w0 = w1 = 0;
-            bad |= g.bad;
-            if (on && nhi == 0) {
-                par[(2 * hf + p) * 64 + tok] = g.s_bits;
-                par[(2 * hf + p) * 64 + 32 + tok] = g.lo_bits;
-            }
-            word[2 * p] = nibble_transpose(w0, lane);
-            word[2 * p + 1] = nibble_transpose(w1, lane);
-        }
-        // tokens of the block that are written, as nibbles
-        uint32_t keep = 0;
+    for (int i = 0; i < 4; i++) in[i] = on ? *reinterpret_cast<const u32x4*>(x + chunk_dim<NS>(at.s, i)) : u32x4{0u, 0u, 0u, 0u};
+    // V: nibbles (tokens) of this block's words that stay as they are
+    uint32_t keep = 0;
+    u32x2 old[2] = {u32x2{0u, 0u}, u32x2{0u, 0u}};
+    uint32_t* const vw = reinterpret_cast<uint32_t*>(tile) + at.v_word();
+    if (w.v) {
 #pragma unroll
         for (int n = 0; n < 8; n++) {
-            const int tk = 8 * blk + nibble_elem(n);
+            const int tk = 8 * at.blk + nibble_elem(n);
             if (tk < w.lo || tk >= w.hi) keep |= 0xFu << (4 * n);
         }
-        u32x4* const dst = reinterpret_cast<u32x4*>(a.v + base) + (hf * 64 + blk * 16 + 8 * nhi + j);
-        if (keep != 0xFFFFFFFFu) {
-            if (keep) word = (*dst & keep) | (word & ~keep);
-            *dst = word;
+        if (keep != 0 && keep != 0xFFFFFFFFu) {
+            old[0] = *reinterpret_cast<const u32x2*>(vw);
+            old[1] = *reinterpret_cast<const u32x2*>(vw + 32);
         }
     }
-    flag_range(a.err, bad);
+    group_transpose<NS>(in, lane);
+    Kv4Group g;
+    kv4_group(g, in);
+    if (on) {
+        uint16_t* const par = reinterpret_cast<uint16_t*>(tile + kv4_code_bytes(D)) + at.s * 64 + at.tok;
+        par[0] = (uint16_t)g.params;
+        par[32] = (uint16_t)(g.params >> 16);
+    }
+    if (w.v) {
+        uint32_t c[4];
+#pragma unroll
+        for (int i = 0; i < 4; i++) c[i] = nibble_transpose<NS>(kv4_word<true>(g, i), lane);  // dim 32 s + 8 i + j
+        if (keep != 0xFFFFFFFFu) {
+            *reinterpret_cast<u32x2*>(vw) = u32x2{(old[0][0] & keep) | (c[0] & ~keep), (old[0][1] & keep) | (c[2] & ~keep)};
+            *reinterpret_cast<u32x2*>(vw + 32) = u32x2{(old[1][0] & keep) | (c[1] & ~keep), (old[1][1] & keep) | (c[3] & ~keep)};
+        }
+    } else {
+        uint32_t c[4];
+#pragma unroll
+        for (int i = 0; i < 4; i++) c[i] = kv4_word<false>(g, i);       // q4 = i of group s
+        uint32_t* const kw = reinterpret_cast<uint32_t*>(tile);
+        if constexpr (NS == 4) {
+            group_transpose<4>(c, lane);                                // group i of q4 = s
+            if (on) *reinterpret_cast<u32x4*>(kw + at.k_word(at.s)) = u32x4{c[0], c[1], c[2], c[3]};
+        } else {
+            group_transpose<2>(c, lane);                                // group i % 2 of q4 = 2 s + i / 2
+            if (on) {
+                *reinterpret_cast<u32x2*>(kw + at.k_word(2 * at.s)) = u32x2{c[0], c[1]};
+                *reinterpret_cast<u32x2*>(kw + at.k_word(2 * at.s + 1)) = u32x2{c[2], c[3]};
+            }
+        }
+    }
+    flag_range(a.err, g.bad);
 }
 
 __device__ __forceinline__ uint32_t kv4_pair(uint32_t c0, uint32_t c1, float s, float lo) {
@@ -221,45 +290,47 @@ template <int D>
 __global__ void __launch_bounds__(256) kv4_read_kernel(Kv4StoreArgs a) {
     constexpr int NS = D / 32;
     Kv4Work w;
-    if (!kv4_work(a, w)) return;
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const long long xrow = (long long)w.b * a.x_b + (long long)w.t0 * a.x_t + (long long)w.g * a.x_h;
-    const long long base = (long long)w.b * a.stride_b + (long long)w.g * a.stride_h + (long long)w.tile * kv4_tile_bytes(D);
-    if (wave < 2) {
-        const int q4 = lane & 3, tok = 16 * wave + (lane >> 2);
-        if (tok < w.lo || tok >= w.hi) return;
-        const int t = tok >> 2 & 1, n16 = (tok >> 3) << 2 | (tok & 3);
-        const uint32_t* const src = reinterpret_cast<const uint32_t*>(a.k + base) + (t * 64 + q4 * 16 + n16) * NS;
-        const uint16_t* const par = reinterpret_cast<const uint16_t*>(a.k + base + kv4_code_bytes(D));
-#pragma unroll
-        for (int s = 0; s < NS; s++) {
-            const uint32_t c = src[s];
-            const float sc = kv4_param(par + s * 64 + tok), lo = kv4_param(par + s * 64 + 32 + tok);
-            u32x4 o;
-#pragma unroll
-            for (int p = 0; p < 4; p++) o[p] = kv4_pair(c >> (4 * p) & 15u, c >> (4 * p + 16) & 15u, sc, lo);
-            *reinterpret_cast<u32x4*>(a.k_x + xrow + tok * a.x_t + 32 * s + 8 * q4) = o;
-        }
+    if (!kv4_work<D>(a, w)) return;
+    const int lane = threadIdx.x & 63;
+    const Kv4Lane<D> at(w);
+    const bool on = at.tok >= w.lo && at.tok < w.hi;
+    uint16_t* const x = (w.v ? a.v_x : a.k_x) + ((long long)w.b * a.x_b + (long long)w.g * a.x_h +
+                                                 (long long)(w.t0 + at.tok) * a.x_t);
+    const uint8_t* const tile = (w.v ? a.v : a.k) + ((long long)w.b * a.stride_b + (long long)w.g * a.stride_h +
+                                                     (long long)w.tile * kv4_tile_bytes(D));
+    const uint16_t* const par = reinterpret_cast<const uint16_t*>(tile + kv4_code_bytes(D)) + at.s * 64 + at.tok;
+    const float s = kv4_param(par), lo = kv4_param(par + 32);
+    uint32_t c[4];                                           // natural nibble order (K: the cache's order)
+    if (w.v) {
+        const uint32_t* const vw = reinterpret_cast<const uint32_t*>(tile) + at.v_word();
+        const u32x2 p = *reinterpret_cast<const u32x2*>(vw), q = *reinterpret_cast<const u32x2*>(vw + 32);
+        c[0] = nibble_transpose<NS>(p[0], lane);
+        c[1] = nibble_transpose<NS>(q[0], lane);
+        c[2] = nibble_transpose<NS>(p[1], lane);
+        c[3] = nibble_transpose<NS>(q[1], lane);
     } else {
-        const int j = lane & 7, nhi = lane >> 3 & 1;
-        const int hf = NS == 4 ? lane >> 4 & 1 : 0;
-        const int blk = NS == 4 ? 2 * (wave - 2) + (lane >> 5) : lane >> 4;
-        if (NS == 2 && wave == 3) return;
-        const int tok = 8 * blk + nibble_elem(j);
-        const bool on = tok >= w.lo && tok < w.hi;
-        const uint16_t* const par = reinterpret_cast<const uint16_t*>(a.v + base + kv4_code_bytes(D));
-        const u32x4 word = reinterpret_cast<const u32x4*>(a.v + base)[hf * 64 + blk * 16 + 8 * nhi + j];
+        const uint32_t* const kw = reinterpret_cast<const uint32_t*>(tile);
+        if constexpr (NS == 4) {
+            const u32x4 p = *reinterpret_cast<const u32x4*>(kw + at.k_word(at.s));
 #pragma unroll
-        for (int i = 0; i < 4; i++) {
-            const uint32_t c = nibble_transpose(word[i], lane);
-            if (!on) continue;
-            const int g = 2 * hf + i / 2;
-            const float sc = kv4_param(par + g * 64 + tok), lo = kv4_param(par + g * 64 + 32 + tok);
-            u32x4 o;
-#pragma unroll
-            for (int p = 0; p < 4; p++) o[p] = kv4_pair(c >> (8 * p) & 15u, c >> (8 * p + 4) & 15u, sc, lo);
-            *reinterpret_cast<u32x4*>(a.v_x + xrow + tok * a.x_t + 16 * (4 * hf + i) + 8 * nhi) = o;
+            for (int i = 0; i < 4; i++) c[i] = p[i];
+        } else {
+            const u32x2 p = *reinterpret_cast<const u32x2*>(kw + at.k_word(2 * at.s));
+            const u32x2 q = *reinterpret_cast<const u32x2*>(kw + at.k_word(2 * at.s + 1));
+            c[0] = p[0]; c[1] = p[1]; c[2] = q[0]; c[3] = q[1];
         }
+        group_transpose<NS>(c, lane, true);
+    }
+    const int d0 = w.v ? 8 : 4, d1 = w.v ? 4 : 16;           // bits from pair to pair, between a pair's codes
+    u32x4 o[4];
+#pragma unroll
+    for (int i = 0; i < 4; i++)
+#pragma unroll
+        for (int p = 0; p < 4; p++) o[i][p] = kv4_pair(c[i] >> (d0 * p) & 15u, c[i] >> (d0 * p + d1) & 15u, s, lo);
+    group_transpose<NS>(o, lane, true);
+    if (on) {
+#pragma unroll
+        for (int i = 0; i < 4; i++) *reinterpret_cast<u32x4*>(x + chunk_dim<NS>(at.s, i)) = o[i];
     }
 }
 
@@ -278,7 +349,8 @@ int kv4_run_tiles(const Kv4StoreArgs& a) {
 }  // namespace
 
 int launch_kv4_append(const Kv4StoreArgs& a, hipStream_t stream) {
-    const dim3 grid(kv4_run_tiles(a), a.nkv, a.B);
+    const int per = a.d == 64 ? 2 : 1;                       // tiles per block
+    const dim3 grid((kv4_run_tiles(a) + per - 1) / per, a.nkv, a.B);
     if (a.d == 128) hipLaunchKernelGGL(kv4_append_kernel<128>, grid, dim3(256), 0, stream, a);
     else if (a.d == 64) hipLaunchKernelGGL(kv4_append_kernel<64>, grid, dim3(256), 0, stream, a);
     else return -1;
@@ -286,7 +358,8 @@ int launch_kv4_append(const Kv4StoreArgs& a, hipStream_t stream) {
 }
 
 int launch_kv4_read(const Kv4StoreArgs& a, hipStream_t stream) {
-    const dim3 grid(kv4_run_tiles(a), a.nkv, a.B);
+    const int per = a.d == 64 ? 2 : 1;                       // tiles per block
+    const dim3 grid((kv4_run_tiles(a) + per - 1) / per, a.nkv, a.B);
     if (a.d == 128) hipLaunchKernelGGL(kv4_read_kernel<128>, grid, dim3(256), 0, stream, a);
     else if (a.d == 64) hipLaunchKernelGGL(kv4_read_kernel<64>, grid, dim3(256), 0, stream, a);
     else return -1;
