@@ -15,6 +15,7 @@
 
 namespace {
 
+typedef float f32x2 __attribute__((ext_vector_type(2)));
 typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 
 template <int CTRL>
@@ -88,40 +89,19 @@ __device__ __forceinline__ int chunk_dim(int s, int i) { return NS == 4 ? 32 * i
 // Token (of eight) whose code is nibble n of a V word.
 __device__ __forceinline__ int nibble_elem(int n) { return 2 * (n & 3) + (n >> 2); }
 
-// The code of x in a group (lo, s), r = 1 / s roughly: exact.  floor((x - lo) / s)
-// by the reciprocal may be one off next to a whole number, where the border
-// (k + 1/2) s decides alike from either side.  That border has 16 bits and the
-// fma one rounding, so the sign of t - (k + 1/2) s is exact; where it is 0 the part that
-// the subtraction t = x - lo lost decides.
-__device__ __forceinline__ uint32_t kv4_code(float x, float lo, float s, float r) {
-    const float t = x - lo;
-    const float kf = __builtin_floorf(t * r);
-    const float d = __builtin_fmaf(-(kf + 0.5f), s, t);
-    int c = (int)kf;
-    if (d > 0.f) {
-        c++;
-    } else if (d == 0.f) {
-        const float z = t - x;                               // (two-sum: x - lo = t + rest)
-        const float rest = (x - (t - z)) + (-lo - z);
-        c += rest >= 0.f;
-    }
-    return (uint32_t)(c < 15 ? c : 15);
-}
-
-// A group: its values as fp16 pairs, parameters, and the line z = x r + b whose
-// whole part is the code, but for values within eps of a border.
+// A group: its values as fp16 pairs, its parameters, and what the codes need.
 struct Kv4Group {
     f16x2 x[16];
-    float lo, s, r, b, eps;
+    float lo, s, r, zb, half;    // r = 1 / s roughly, zb = - lo r, half = lo + s / 2
     uint32_t params;             // scale bits | offset bits << 16
-    bool bad, clamp;
+    bool bad, rare;
 };
 
 __device__ __forceinline__ void kv4_group(Kv4Group& g, const u32x4 (&in)[4]) {
 #pragma unroll
     for (int i = 0; i < 16; i++) {
         const uint32_t w = in[i / 4][i % 4];
-        g.x[i] = f16x2{(f16)__uint_as_float(w << 16), (f16)__uint_as_float(w & 0xFFFF0000u)};
+        g.x[i] = __builtin_convertvector(f32x2{__uint_as_float(w << 16), __uint_as_float(w & 0xFFFF0000u)}, f16x2);
     }
     f16x2 mn = g.x[0], mx = g.x[0], nan = g.x[0] * (f16)0.f;
 #pragma unroll
@@ -137,37 +117,50 @@ __device__ __forceinline__ void kv4_group(Kv4Group& g, const u32x4 (&in)[4]) {
     g.lo = g.bad ? 0.f : (float)lo;
     g.s = g.bad ? 0.f : (float)s;
     g.r = g.s > 0.f ? __builtin_amdgcn_rcpf(g.s) : 0.f;
-    g.b = __builtin_fmaf(-g.lo, g.r, 0.5f);
-    // z's error: of the reciprocal (2^-22), of b's rounding and of the fma's
-    g.eps = (__builtin_fabsf(g.lo * g.r) + 16.f) * 0x1p-20f;
-    g.clamp = !g.bad && __builtin_fmaf((float)hi, g.r, g.b) >= 15.9f;                // (a scale among the subnormals)
+    g.zb = -g.lo * g.r;
+    g.half = __builtin_fmaf(0.5f, g.s, g.lo);
+    // The borders lo + (k + 1/2) s have to be fp32 numbers: multiples of half the scale's last place (2^-12 s at least) and
+    // of the offset's (2^-11 |lo|), of magnitude up to the values'.  And a scale rounded among fp16's subnormals can ask for
+    // codes above 15.
+    const float top = fmaxf(__builtin_fabsf(g.lo), __builtin_fabsf((float)hi));
+    g.rare = !g.bad && (top > 2048.f * g.s || (g.lo != 0.f && __builtin_fabsf(g.lo) < 0x1p-11f * top) || g.s < 0x1p-14f);
     g.params = g.bad ? 0x7E007E00u : (uint32_t)__builtin_bit_cast(uint16_t, s) | (uint32_t)__builtin_bit_cast(uint16_t, lo) << 16;
 }
 
-// Codes of values 8 w .. + 7 of the group; element e at nibble e (NAT) or at bits 4 (e / 2) + 16 (e % 2).
-template <bool NAT>
+// The code of x, exact for every group.  floor((x - lo) / s) by the reciprocal may be one off
+// next to a whole number, where the border (k + 1/2) s decides alike from either
+// side.  That border has 16 bits and the fma one rounding, so the sign of t - (k + 1/2) s is
+// exact; where it is 0 the part that the subtraction t = x - lo lost decides.
+__device__ __forceinline__ float kv4_code_rare(float x, float lo, float s) {
+    if (s == 0.f) return 0.f;
+    const float t = x - lo, r = __builtin_amdgcn_rcpf(s);
+    const float kf = __builtin_floorf(t * r), d = __builtin_fmaf(-(kf + 0.5f), s, t);
+    const float z = t - x;                                   // (two-sum: x - lo = t + rest)
+    const float rest = (x - (t - z)) + (-lo - z);
+    return fminf(kf + (d > 0.f || (d == 0.f && rest >= 0.f) ? 1.f : 0.f), 15.f);
+}
+
+// Codes of values 8 w .. + 7 of the group, value e at nibble e.  The same idea as kv4_code_rare with the border as a value:
+// k = floor of about (x - lo) / s, and k + 1 from lo + (k + 1/2) s on.
 __device__ __forceinline__ uint32_t kv4_word(const Kv4Group& g, int w) {
-    float c[8], fmn = 1.f, fmx = 0.f;
+    float c[8];
+    float one = 1.f;                                         // (opaque: x - .. widens x in the same operation)
+    asm("" : "+v"(one));
 #pragma unroll
     for (int e = 0; e < 8; e++) {
-        const float z = __builtin_fmaf((float)g.x[4 * w + e / 2][e % 2], g.r, g.b), f = __builtin_amdgcn_fractf(z);
-        c[e] = z - f;
-        fmn = fminf(fmn, f);
-        fmx = fmaxf(fmx, f);
+        const f16 x = g.x[4 * w + e / 2][e % 2];
+        const float k = __builtin_floorf(__builtin_fmaf((float)x, g.r, g.zb));
+        const float d = __builtin_fmaf((float)x, one, -__builtin_fmaf(k, g.s, g.half));
+        c[e] = k + __builtin_amdgcn_fmed3f(__builtin_fmaf(d, 0x1p40f, 1.f), 0.f, 1.f);        // (1 if d >= 0, else 0)
     }
-    if (fmn < g.eps || fmx > 1.f - g.eps || g.clamp) {
+    if (g.rare) {
 #pragma unroll
-        for (int e = 0; e < 8; e++) c[e] = (float)kv4_code((float)g.x[4 * w + e / 2][e % 2], g.lo, g.s, g.r);
-        if (g.s == 0.f)
-#pragma unroll
-            for (int e = 0; e < 8; e++) c[e] = 0.f;
+        for (int e = 0; e < 8; e++) c[e] = kv4_code_rare((float)g.x[4 * w + e / 2][e % 2], g.lo, g.s);
     }
     // four codes are summed up as one number below 2^16
-    const int o = NAT ? 1 : 2;
-    const float a0 = __builtin_fmaf(__builtin_fmaf(__builtin_fmaf(c[3 * o], 16.f, c[2 * o]), 16.f, c[o]), 16.f, c[0]);
-    const int h = NAT ? 4 : 1;
-    const float a1 = __builtin_fmaf(__builtin_fmaf(__builtin_fmaf(c[h + 3 * o], 16.f, c[h + 2 * o]), 16.f, c[h + o]), 16.f, c[h]);
-    return (uint32_t)a0 | (uint32_t)a1 << 16;
+    const float a0 = __builtin_fmaf(__builtin_fmaf(__builtin_fmaf(c[3], 16.f, c[2]), 16.f, c[1]), 16.f, c[0]);
+    const float a1 = __builtin_fmaf(__builtin_fmaf(__builtin_fmaf(c[7], 16.f, c[6]), 16.f, c[5]), 16.f, c[4]);
+    return g.bad ? 0u : (uint32_t)a0 | (uint32_t)a1 << 16;
 }
 
 // A wave's work: K or V of 64 / NS tokens (from tok0 of a tile) of a (row, kv head).
@@ -185,7 +178,14 @@ __device__ __forceinline__ bool kv4_work(const Kv4StoreArgs& a, Kv4Work& w) {
     w.g = blockIdx.y;
     w.v = wave / WPT % 2;
     w.tok0 = wave % WPT * (KV4_TILE / WPT);
-    const int s0 = a.slots_dev ? a.slots_dev[w.b] : a.slots.v[w.b];
+    int s0;
+    if (a.slots_dev) {
+        s0 = a.slots_dev[w.b];
+        asm volatile("" : "+v"(s0));                         // (two loads, not one from a chosen address)
+    } else {
+        s0 = a.slots.v[w.b];
+    }
+    s0 = __builtin_amdgcn_readfirstlane(s0);
     if (s0 < 0 || s0 > a.max_seq - a.T) return false;
     w.tile = s0 / KV4_TILE + blockIdx.x * (2 / WPT) + item;
     w.t0 = w.tile * KV4_TILE - s0;
@@ -233,7 +233,7 @@ __global__ void __launch_bounds__(256) kv4_append_kernel(Kv4StoreArgs a) {
     uint32_t keep = 0;
     u32x2 old[2] = {u32x2{0u, 0u}, u32x2{0u, 0u}};
     uint32_t* const vw = reinterpret_cast<uint32_t*>(tile) + at.v_word();
-    if (w.v) {
+    if (w.v && (w.lo > w.tok0 || w.hi < w.tok0 + 64 / NS)) {
 #pragma unroll
         for (int n = 0; n < 8; n++) {
             const int tk = 8 * at.blk + nibble_elem(n);
@@ -252,19 +252,28 @@ __global__ void __launch_bounds__(256) kv4_append_kernel(Kv4StoreArgs a) {
         par[0] = (uint16_t)g.params;
         par[32] = (uint16_t)(g.params >> 16);
     }
-    if (w.v) {
-        uint32_t c[4];
+    if (!w.v) {              // K words hold values 0, 2, 4, 6 in their lower half: values 8 i .. + 7 in that order
 #pragma unroll
-        for (int i = 0; i < 4; i++) c[i] = nibble_transpose<NS>(kv4_word<true>(g, i), lane);  // dim 32 s + 8 i + j
+        for (int i = 0; i < 16; i += 4) {
+            const f16x2 p0 = g.x[i], p1 = g.x[i + 1], p2 = g.x[i + 2], p3 = g.x[i + 3];
+            g.x[i] = f16x2{p0[0], p1[0]};
+            g.x[i + 1] = f16x2{p2[0], p3[0]};
+            g.x[i + 2] = f16x2{p0[1], p1[1]};
+            g.x[i + 3] = f16x2{p2[1], p3[1]};
+        }
+    }
+    uint32_t c[4];
+#pragma unroll
+    for (int i = 0; i < 4; i++) c[i] = kv4_word(g, i);
+    if (w.v) {
+#pragma unroll
+        for (int i = 0; i < 4; i++) c[i] = nibble_transpose<NS>(c[i], lane);           // dim 32 s + 8 i + j
         if (keep != 0xFFFFFFFFu) {
             *reinterpret_cast<u32x2*>(vw) = u32x2{(old[0][0] & keep) | (c[0] & ~keep), (old[0][1] & keep) | (c[2] & ~keep)};
             *reinterpret_cast<u32x2*>(vw + 32) = u32x2{(old[1][0] & keep) | (c[1] & ~keep), (old[1][1] & keep) | (c[3] & ~keep)};
         }
     } else {
-        uint32_t c[4];
-#pragma unroll
-        for (int i = 0; i < 4; i++) c[i] = kv4_word<false>(g, i);       // q4 = i of group s
-        uint32_t* const kw = reinterpret_cast<uint32_t*>(tile);
+        uint32_t* const kw = reinterpret_cast<uint32_t*>(tile);        // (word i: q4 = i of group s)
         if constexpr (NS == 4) {
             group_transpose<4>(c, lane);                                // group i of q4 = s
             if (on) *reinterpret_cast<u32x4*>(kw + at.k_word(at.s)) = u32x4{c[0], c[1], c[2], c[3]};
