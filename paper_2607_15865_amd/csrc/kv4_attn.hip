@@ -573,7 +573,7 @@ __global__ void __launch_bounds__(64 * PF_W) kv4_prefill_kernel(Kv4AttnArgs a) {
     extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
     unsigned char* const Ks = smem;                          // [2 buffers][2 tiles][NF][64 lanes][16]
     unsigned char* const Vs = smem + 4 * FB;                 // [2][2][NS][2][64][16]
-    unsigned long long* const vbad = reinterpret_cast<unsigned long long*>(smem + 8 * FB);   // [3][NS + 1] NaN keys of V, by stage % 3
+    unsigned long long* const vbad = reinterpret_cast<unsigned long long*>(smem + 8 * FB);   // [4][NS + 1] NaN keys of V, by stage % 4
     const int tid = threadIdx.x, lane = tid & 63;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int h = lane >> 5, c = lane & 31;
@@ -594,19 +594,14 @@ __global__ void __launch_bounds__(64 * PF_W) kv4_prefill_kernel(Kv4AttnArgs a) {
     uint16_t ksc[NW], klo[NW];
     u32x4 vsc, vlo;
     const uint8_t *kb = nullptr, *vb = nullptr;
-    auto load_raw = [&](int st) __attribute__((always_inline)) {
-        // (a tile past the last key's repeats that one: its keys are never seen)
-        const int tile = min(2 * st + tt, (nkeys - 1) / KV4_TILE);
-        const uint8_t* kt = kb + (long long)tile * TB;
-        const uint8_t* vt = vb + (long long)tile * TB;
+    // (a tile past the last key's repeats that one: its keys are never seen)
+    auto load_k = [&](int st) __attribute__((always_inline)) {
+        const uint8_t* kt = kb + (long long)min(2 * st + tt, (nkeys - 1) / KV4_TILE) * TB;
         if constexpr (NW == 2) {
             const u32x2 x = *reinterpret_cast<const u32x2*>(kt + kL * 16 + ksub * 8);
-            const u32x2 y = *reinterpret_cast<const u32x2*>(vt + vL * 16 + vsub * 8);
             kw[0] = x[0]; kw[1] = x[1];
-            vw[0] = y[0]; vw[1] = y[1];
         } else {
             kw[0] = *reinterpret_cast<const uint32_t*>(kt + kL * 8 + ksub * 4);
-            vw[0] = *reinterpret_cast<const uint32_t*>(vt + vL * 16 + vsub * 4);
         }
 #pragma unroll
         for (int i = 0; i < NW; i++) {
@@ -614,14 +609,22 @@ __global__ void __launch_bounds__(64 * PF_W) kv4_prefill_kernel(Kv4AttnArgs a) {
             ksc[i] = *reinterpret_cast<const uint16_t*>(pp);
             klo[i] = *reinterpret_cast<const uint16_t*>(pp + 64);
         }
+    };
+    auto load_v = [&](int st) __attribute__((always_inline)) {
+        const uint8_t* vt = vb + (long long)min(2 * st + tt, (nkeys - 1) / KV4_TILE) * TB;
+        if constexpr (NW == 2) {
+            const u32x2 y = *reinterpret_cast<const u32x2*>(vt + vL * 16 + vsub * 8);
+            vw[0] = y[0]; vw[1] = y[1];
+        } else {
+            vw[0] = *reinterpret_cast<const uint32_t*>(vt + vL * 16 + vsub * 4);
+        }
         vsc = *reinterpret_cast<const u32x4*>(vt + CB + vg * 128 + vq4 * 16);
         vlo = *reinterpret_cast<const u32x4*>(vt + CB + vg * 128 + 64 + vq4 * 16);
     };
     const DqConst dq = dq_const();
     const ZeroOff zo = zero_off(0.f);
-    auto unpack = [&](int st, int buf, int nb) __attribute__((always_inline)) {
+    auto unpack_k = [&](int buf) __attribute__((always_inline)) {
         unsigned char* const kd = Ks + (buf * 2 + tt) * FB;
-        unsigned char* const vd = Vs + (buf * 2 + tt) * FB;
         const int row = key_perm(kkey);                      // of the score tile (its chunks rotated: fewer bank conflicts)
         const int kch = (row & 16) | ((row ^ (row >> 1 & 8)) & 15);
 #pragma unroll
@@ -632,13 +635,17 @@ __global__ void __launch_bounds__(64 * PF_W) kv4_prefill_kernel(Kv4AttnArgs a) {
             const int f = 2 * (NW * ksub + i) + (kq4 >> 1);
             *reinterpret_cast<f16x8*>(kd + (f * 64 + (kq4 & 1) * 32 + kch) * 16) = y;
         }
+    };
+    auto unpack_v = [&](int st, int buf, int nb) __attribute__((always_inline)) {
+        unsigned char* const vd = Vs + (buf * 2 + tt) * FB;
         f16x8 s = __builtin_bit_cast(f16x8, vsc), lo = __builtin_bit_cast(f16x8, vlo);
         const int key0 = st * PF_KST + tt * 32 + 8 * vq4;    // of the words' eight
-        if (key0 + 8 > nkeys) {                              // what lies behind the last key may be anything
+        const int left = nkeys - key0;
+        if (left < 8) {                                      // what lies behind the last key may be anything
 #pragma unroll
             for (int e = 0; e < 8; e++) {
-                s[e] = key0 + e < nkeys ? s[e] : (f16)0.f;
-                lo[e] = key0 + e < nkeys ? lo[e] : (f16)0.f;
+                s[e] = e < left ? s[e] : (f16)0.f;
+                lo[e] = e < left ? lo[e] : (f16)0.f;
             }
         }
         // A NaN value would reach the rows that do not see its key as 0 * NaN: it is 0 here, and the rows that do see it
@@ -646,13 +653,14 @@ __global__ void __launch_bounds__(64 * PF_W) kv4_prefill_kernel(Kv4AttnArgs a) {
         const f16x2 l0{lo[0], lo[1]}, l1{lo[2], lo[3]}, l2{lo[4], lo[5]}, l3{lo[6], lo[7]};
         const f16x2 any = (l0 * (f16)0.f + l1 * (f16)0.f) + (l2 * (f16)0.f + l3 * (f16)0.f);
         if (!(any[0] + any[1] == (f16)0.f)) {
-            unsigned long long m = 0;
+            uint32_t bits = 0;
 #pragma unroll
             for (int e = 0; e < 8; e++)
                 if (lo[e] != lo[e]) {
-                    m |= 1ull << (tt * 32 + 8 * vq4 + e);
+                    bits |= 1u << e;
                     s[e] = lo[e] = (f16)0.f;
                 }
+            const unsigned long long m = (unsigned long long)bits << (tt * 32 + 8 * vq4);
             if (vn == 0) {
                 atomicOr(vbad + nb * (NS + 1) + vg, m);
                 atomicOr(vbad + nb * (NS + 1) + NS, m);
@@ -679,7 +687,7 @@ __global__ void __launch_bounds__(64 * PF_W) kv4_prefill_kernel(Kv4AttnArgs a) {
         u = first + st1;
         kb = a.k + (long long)hk * a.stride_h;
         vb = a.v + (long long)hk * a.stride_h;
-        load_raw(st0);
+        load_k(st0);
 
         // ---- queries: this lane's row, dims 16 f + 8 h .. + 7 of every fragment f, times 2^qe
         const int row = q * PF_ROWS + wave * 32 + c;
@@ -716,28 +724,34 @@ __global__ void __launch_bounds__(64 * PF_W) kv4_prefill_kernel(Kv4AttnArgs a) {
 #pragma unroll
         for (int i = 0; i < NS; i++) o[i] = f32x16{};
         float m = -INFINITY, l = 0.f;
+        const int n = st1 - st0;
+        const int non = active ? min(n, lim_hi / PF_KST + 1 - st0) : 0;      // stages that the wave's rows see keys of
 
         __syncthreads();                                     // (the last tile's readers are done)
-        if (tid < 3 * (NS + 1)) vbad[tid] = 0;
+        if (tid < 4 * (NS + 1)) vbad[tid] = 0;
+        unpack_k(0);
+        if (n > 1) load_k(st0 + 1);
+        load_v(st0);
         __syncthreads();
-        unpack(st0, 0, 0);
-        if (st0 + 1 < st1) load_raw(st0 + 1);
-        __syncthreads();
-        int nb = 0;
-        for (int st = st0; st < st1; st++) {
-            const int buf = (st - st0) & 1;
-            const int nb1 = nb == 2 ? 0 : nb + 1, nb2 = nb1 == 2 ? 0 : nb1 + 1;
-            // (the list of stage st + 2 was last read in stage st - 1)
-            if (tid <= NS) vbad[nb2 * (NS + 1) + tid] = 0;
-            if (st + 1 < st1) {
-                unpack(st + 1, buf ^ 1, nb1);
-                if (st + 2 < st1) load_raw(st + 2);
-            }
-            const int kbase = st * PF_KST;
-            if (active && kbase <= lim_hi) {
-                const unsigned char* K = Ks + buf * 2 * FB;
-                const unsigned char* V = Vs + buf * 2 * FB;
-                f32x16 sc[2];
+        int next = 0;                                        // K of stage next + 1 and V of stage next are to be unpacked
+        auto unpack_next = [&]() __attribute__((always_inline)) {
+            if (next + 1 < n) unpack_k(next + 1 & 1);
+            if (next < n) unpack_v(st0 + next, next & 1, next & 3);
+            if (next + 2 < n) load_k(st0 + next + 2);
+            if (next + 1 < n) load_v(st0 + next + 1);
+            next++;
+        };
+        if (wave >= PF_W / 2) {                              // half a stage behind: vector work where the others multiply
+            unpack_next();
+            __syncthreads();
+        }
+        f32x16 sc[2];
+        f16x8 pf[4];
+#pragma clang loop unroll(disable)
+        for (int s = 0; s <= n; s++) {
+            // ---- matrix half: scores of stage s, output of stage s - 1
+            if (s < non) {
+                const unsigned char* K = Ks + (s & 1) * 2 * FB;
                 sc[0] = f32x16{};
                 sc[1] = f32x16{};
 #pragma unroll
@@ -747,15 +761,40 @@ __global__ void __launch_bounds__(64 * PF_W) kv4_prefill_kernel(Kv4AttnArgs a) {
                         const f16x8 kf = *reinterpret_cast<const f16x8*>(K + t * FB + (f * 64 + h * 32 + kch) * 16);
                         sc[t] = __builtin_amdgcn_mfma_f32_32x32x16_f16(kf, qf[f], sc[t], 0, 0, 0);
                     }
+            }
+            if (s > 0 && s <= non) {
+                const unsigned char* V = Vs + (s - 1 & 1) * 2 * FB;
+#pragma unroll
+                for (int ks = 0; ks < 4; ks++)
+#pragma unroll
+                    for (int i = 0; i < NS; i++) {
+                        const f16x8 vf = *reinterpret_cast<const f16x8*>(V + (ks >> 1) * FB + ((i * 2 + (ks & 1)) * 64 + lane) * 16);
+                        o[i] = __builtin_amdgcn_mfma_f32_32x32x16_f16(vf, pf[ks], o[i], 0, 0, 0);
+                    }
+                const unsigned long long* const bl = vbad + (s - 1 & 3) * (NS + 1);
+                if (bl[NS] != 0) {                           // NaN for the rows that see one of the keys, in its group
+                    const long long left = lim - (st0 + s - 1) * PF_KST;
+                    const unsigned long long see = left >= 63 ? ~0ull : left < 0 ? 0ull : (2ull << left) - 1;
+#pragma unroll
+                    for (int i = 0; i < NS; i++)
+                        if (bl[i] & see)
+#pragma unroll
+                            for (int e = 0; e < 16; e++) o[i][e] = __builtin_nanf("");
+                }
+            }
+            if (s == n) break;
+            __syncthreads();
+            // ---- vector half: weights of stage s, the next tiles
+            if (tid <= NS) vbad[(s + 1 & 3) * (NS + 1) + tid] = 0;       // (the list of stage s - 3)
+            if (s < non) {
+                const int kbase = (st0 + s) * PF_KST;
                 float p[32];
 #pragma unroll
                 for (int e = 0; e < 32; e++) p[e] = sc[e / 16][e % 16];
                 if (kbase + PF_KST - 1 > lim_lo) {
+                    const int left = lim - kbase - 8 * h;
 #pragma unroll
-                    for (int e = 0; e < 32; e++) {
-                        const int key = kbase + 32 * (e / 16) + 16 * ((e % 16) / 8) + 8 * h + e % 8;
-                        p[e] = key <= lim ? p[e] : -INFINITY;
-                    }
+                    for (int e = 0; e < 32; e++) p[e] = 32 * (e / 16) + 16 * (e % 16 / 8) + e % 8 <= left ? p[e] : -INFINITY;
                 }
                 float mt = fmaxf(p[0], p[1]);
 #pragma unroll
@@ -773,39 +812,20 @@ __global__ void __launch_bounds__(64 * PF_W) kv4_prefill_kernel(Kv4AttnArgs a) {
                 const float mb = m == -INFINITY ? 0.f : m;
                 float ls[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-                for (int e = 0; e < 32; e++) {
-                    p[e] = exp2_hw(__builtin_fmaf(p[e], sl, -mb));
-                    ls[e % 4] += p[e];
+                for (int e = 0; e < 32; e += 2) {
+                    const float x = exp2_hw(__builtin_fmaf(p[e], sl, -mb)), y = exp2_hw(__builtin_fmaf(p[e + 1], sl, -mb));
+                    ls[e / 2 % 2] += x;
+                    ls[2 + e / 2 % 2] += y;
+                    const f16x2 w = __builtin_convertvector(f32x2{x, y}, f16x2);
+                    pf[e / 8][e % 8] = w[0];
+                    pf[e / 8][e % 8 + 1] = w[1];
                 }
                 l += (ls[0] + ls[1]) + (ls[2] + ls[3]);
-#pragma unroll
-                for (int ks = 0; ks < 4; ks++) {
-                    f16x8 pf;
-#pragma unroll
-                    for (int e = 0; e < 8; e += 2) {
-                        const f16x2 x = __builtin_convertvector(f32x2{p[8 * ks + e], p[8 * ks + e + 1]}, f16x2);
-                        pf[e] = x[0];
-                        pf[e + 1] = x[1];
-                    }
-#pragma unroll
-                    for (int i = 0; i < NS; i++) {
-                        const f16x8 vf = *reinterpret_cast<const f16x8*>(V + (ks >> 1) * FB + ((i * 2 + (ks & 1)) * 64 + lane) * 16);
-                        o[i] = __builtin_amdgcn_mfma_f32_32x32x16_f16(vf, pf, o[i], 0, 0, 0);
-                    }
-                }
-                if (vbad[nb * (NS + 1) + NS] != 0) {         // NaN for the rows that see one of the keys, in its group
-                    const long long left = lim - kbase;
-                    const unsigned long long see = left >= 63 ? ~0ull : left < 0 ? 0ull : (2ull << left) - 1;
-#pragma unroll
-                    for (int i = 0; i < NS; i++)
-                        if (vbad[nb * (NS + 1) + i] & see)
-#pragma unroll
-                            for (int e = 0; e < 16; e++) o[i][e] = __builtin_nanf("");
-                }
             }
+            unpack_next();
             __syncthreads();
-            nb = nb1;
         }
+        if (wave < PF_W / 2) __syncthreads();
         const bool whole = st0 == 0 && st1 == nst;
         const float lt = l + __shfl_xor(l, 32, 64);
         if (whole && row < R) {
@@ -958,7 +978,7 @@ Kv4PrefillPlan kv4_prefill_plan(int T, int hist, int nkv, int r, int d) {
 
 template <int D>
 static int launch_prefill(const Kv4AttnArgs& a, int blocks, hipStream_t stream) {
-    const size_t lds = (size_t)8 * 32 * D * 2 + 3 * (D / 32 + 1) * 8;
+    const size_t lds = (size_t)8 * 32 * D * 2 + 4 * (D / 32 + 1) * 8;
     static LdsLimit lim;
     if (ensure_lds_limit(lim, (const void*)kv4_prefill_kernel<D>, lds)) return -1;
     hipLaunchKernelGGL(kv4_prefill_kernel<D>, dim3(blocks), dim3(64 * PF_W), lds, stream, a);
