@@ -446,7 +446,7 @@ int kv_append(const kv_desc* desc, void* k_cache, void* v_cache,
 typedef struct kv4_desc {
     int32_t batch;
     int32_t n_kv_heads;
-    int32_t max_seq;
+    int32_t max_seq;      /* at most 2^27 */
     int32_t head_dim;     /* 64 or 128 */
     int64_t stride_b;     /* bytes between sequences */
     int64_t stride_h;     /* bytes between kv heads */
@@ -488,8 +488,8 @@ int kv4_read(const kv4_desc* desc, const void* k_cache, const void* v_cache,
  *   out[r][h] = sum_j softmax_j(q[r][h] . K_j / sqrt(head_dim) [+ mask_j]) V_j
  * with K, V the values lo + s c.  q and out are bf16 [rows][n_heads][head_dim],
  * out rounded once; softmax statistics and sums are fp32, a product's operands
- * fp16 (codes and q exact, weights and, in the prefill, keys and values
- * within 2^-11).  Deterministic.
+ * fp16 (codes and q exact, weights and, in a prefill of many queries, keys and
+ * values within 2^-11).  Deterministic.
  *
  * kv4_attn_decode: one query for each of B sequences, row b attends to slots
  * 0 .. ctx_lens[b] (int32 [B] device, every one <= max_ctx), which are

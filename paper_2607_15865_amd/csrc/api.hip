@@ -1398,6 +1398,7 @@ static bool aligned16(std::initializer_list<const void*> ps) {
 
 static int check_kv4(const kv4_desc* d, int32_t B) {
     if (d->batch < 1 || d->n_kv_heads < 1 || d->max_seq < 1) return fail(W4_EINVAL, "bad kv4_desc");
+    if (d->max_seq > 1 << 27) return fail(W4_EUNSUPPORTED, "max_seq must be at most 2^27");   // (rows of queries fit 31 bits)
     if (d->head_dim != 64 && d->head_dim != 128) return fail(W4_EUNSUPPORTED, "head_dim must be 64 or 128");
     const int64_t tiles = ((int64_t)d->max_seq + KV4_TILE - 1) / KV4_TILE;
     if (d->stride_h % 16 || d->stride_b % 16 || d->stride_h < tiles * kv4_tile_bytes(d->head_dim) ||
@@ -1508,7 +1509,7 @@ size_t kv4_attn_workspace_size(const kv4_desc* d, int32_t n_heads, int32_t stage
     if (stage == 2)          // (for the plan of any batch up to B and context up to max_ctx; never 0)
         return std::max((size_t)256, kv4_decode_part_bound(B, d->n_kv_heads, n_heads / d->n_kv_heads, d->head_dim, max_ctx));
     if (T < 1) return 0;
-    return kv4_prefill_plan(T, max_ctx, d->n_kv_heads, n_heads / d->n_kv_heads, d->head_dim).part_bytes;
+    return kv4_prefill_plan(std::min(T, d->max_seq), std::min(max_ctx, d->max_seq), d->n_kv_heads, n_heads / d->n_kv_heads, d->head_dim).part_bytes;
 }
 
 // The parts of an attention call that both forms share.

@@ -66,7 +66,8 @@ struct Kv4AttnArgs {
     float scale;             // of the scores
     int nsplit;              // decode: shares of a (row, kv head)'s tiles
     float* part;             // decode: share states (nsplit > 1), [rows nkv][nsplit] of r (d + 2) floats; prefill: plan.part_bytes
-    long long pf_units;      // prefill: set by the launcher
+    long long pf_units;      // prefill, set by the launcher: stages of one kv head's row tiles; stages of a part
+    int pf_chunk;            // (0: equal runs)
     int r, per;              // set by the launcher: nq / nkv; decode: tiles per share
     int* err;                // raised with W4_FLAG_F16_RANGE (out_f16), or null
 };
@@ -79,7 +80,9 @@ int launch_kv4_decode(const Kv4AttnArgs& a, int waves, hipStream_t stream);
 // Prefill: rows queries of one sequence after ctx_base tokens (part: part_bytes).
 struct Kv4PrefillPlan {
     long long units = 0;     // stages of one kv head's row tiles
-    int blocks = 0;
+    int blocks = 0, chunk = 0;   // chunk: parts of so many stages at most, a block each; 0: equal runs
+    bool merge = false;
+    bool single = false;     // the queries are rows of the decode kernel (then nothing above)
     size_t part_bytes = 0;   // grows with T and hist
 };
 Kv4PrefillPlan kv4_prefill_plan(int T, int hist, int nkv, int r, int d);

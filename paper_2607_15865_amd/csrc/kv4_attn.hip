@@ -503,10 +503,12 @@ __global__ void __launch_bounds__(256) kv4_decode_merge_kernel(Kv4AttnArgs a) {
 // online softmax needs a lane exchange only when a maximum moves, which it does when a
 // score passes it by more than 8 (log2 units; weights stay below 2^8, in fp16).
 //
-// The stages of all row tiles of all kv heads form one line of work that the
-// blocks cut into equal runs, so that the blocks end together whatever the
-// causal lengths; a row tile that a cut parts leaves its pieces' states in the
-// workspace, and a second launch merges them in order.
+// Work is dealt out in one of two ways (kv4_prefill_plan).  In pieces (a.pf_chunk):
+// every row tile's stages are cut into as many equal parts as it has runs of pf_chunk, one
+// block each, the longest tiles first.  Or in a line: the stages of all row tiles of
+// all kv heads follow each other and the blocks cut them into equal runs, so that
+// long work ends everywhere at once.  A row tile with more than one part leaves their states in
+// the workspace, and a second launch merges them in order.
 constexpr int PF_W = 8;                      // waves per block
 constexpr int PF_ROWS = 32 * PF_W;
 constexpr int PF_KST = 64;                   // keys per stage
@@ -516,13 +518,26 @@ __host__ __device__ inline int pf_stages(int q, int R, int r, int hist) {     //
     return (hist + last / r) / PF_KST + 1;
 }
 
-// Row tile and first unit of the tile that holds unit u of a kv head (u below the
-// head's sum); whole waves call it.
-__device__ __forceinline__ void pf_find(const Kv4AttnArgs& a, int R, int r, long long u, int& q, long long& first) {
+// A kv head's row tiles in the order in which work is dealt out, with their shares of it: parts, last tile first
+// (a.pf_chunk), or stages.
+__device__ __forceinline__ int pf_tile(const Kv4AttnArgs& a, int i, int nqt) { return a.pf_chunk ? nqt - 1 - i : i; }
+__device__ __forceinline__ int pf_weight(const Kv4AttnArgs& a, int i, int nqt, int R, int r) {
+    const int st = pf_stages(pf_tile(a, i, nqt), R, r, a.ctx_base);
+    return a.pf_chunk ? (st + a.pf_chunk - 1) / a.pf_chunk : st;
+}
+
+// x, the same in all lanes, in scalar registers.
+__device__ __forceinline__ long long scalar(long long x) {
+    return (long long)((uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((int)(x >> 32)) << 32 |
+                       (uint32_t)__builtin_amdgcn_readfirstlane((int)x));
+}
+
+// The entry i that has unit u of a kv head (u below the head's sum), and its first; whole waves call it.
+__device__ __forceinline__ void pf_find(const Kv4AttnArgs& a, int R, int r, long long u, int& i, long long& first) {
     const int lane = threadIdx.x & 63, nqt = (R + PF_ROWS - 1) / PF_ROWS;
     first = 0;
-    for (int q0 = 0;; q0 += 64) {
-        int x = q0 + lane < nqt ? pf_stages(q0 + lane, R, r, a.ctx_base) : 0;
+    for (int i0 = 0;; i0 += 64) {
+        int x = i0 + lane < nqt ? pf_weight(a, i0 + lane, nqt, R, r) : 0;
         const int own = x;
 #pragma unroll
         for (int off = 1; off < 64; off *= 2) {              // inclusive sums over the lanes
@@ -530,13 +545,13 @@ __device__ __forceinline__ void pf_find(const Kv4AttnArgs& a, int R, int r, long
             x += lane >= off ? y : 0;
         }
         const unsigned long long past = __builtin_amdgcn_ballot_w64(first + x > u);
-        if (past != 0 || q0 + 64 >= nqt) {
+        if (past != 0 || i0 + 64 >= nqt) {
             const int l = past != 0 ? __builtin_ctzll(past) : 0;
-            q = q0 + l;
-            first += __shfl(x - own, l, 64);
+            i = i0 + l;
+            first += __builtin_amdgcn_readlane(x - own, l);
             return;
         }
-        first += __shfl(x, 63, 64);
+        first += __builtin_amdgcn_readlane(x, 63);
     }
 }
 
@@ -565,7 +580,7 @@ __device__ __forceinline__ void pf_put(const Kv4AttnArgs& a, size_t off, const f
     *reinterpret_cast<uint2*>(static_cast<uint16_t*>(a.out) + off) = w;
 }
 
-template <int D>
+template <int D, bool PIECES>
 __global__ void __launch_bounds__(64 * PF_W) kv4_prefill_kernel(Kv4AttnArgs a) {
     constexpr int NS = D / 32, NF = D / 16, NW = D / 64;     // groups, K fragments, words per thread
     constexpr int TB = kv4_tile_bytes(D), CB = kv4_code_bytes(D);
@@ -579,17 +594,17 @@ __global__ void __launch_bounds__(64 * PF_W) kv4_prefill_kernel(Kv4AttnArgs a) {
     const int h = lane >> 5, c = lane & 31;
     const int r = a.nq / a.nkv, R = a.rows * r, nkeys = a.ctx_base + a.rows;
     const int nqt = (R + PF_ROWS - 1) / PF_ROWS;
-    // this block's run of units
+    // this block's part, or its run of units
     const long long total = a.pf_units * a.nkv;
-    long long u = total * blockIdx.x / gridDim.x;
-    const long long u1 = total * (blockIdx.x + 1) / gridDim.x;
+    long long u = PIECES ? blockIdx.x / a.nkv : scalar(total * blockIdx.x / gridDim.x);
+    const long long u1 = PIECES ? u + 1 : scalar(total * (blockIdx.x + 1) / gridDim.x);
 
-    // words of this thread: tile tt of the stage
-    const int tt = tid >> 8, w = tid & 255;
-    const int kL = w & 127, ksub = w >> 7;                   // K: lane slot t 64 + q4 16 + n16, words NW ksub ..
-    const int kkey = 8 * ((kL & 15) >> 2) + 4 * (kL >> 6) + (kL & 3), kq4 = kL >> 4 & 3;
-    const int vL = D == 128 ? w & 127 : w & 63, vsub = D == 128 ? w >> 7 : w >> 6;   // V: lane slot, words NW vsub ..
-    const int vn = vL & 15, vq4 = vL >> 4 & 3, vdb = D == 128 ? 4 * (vL >> 6) + 2 * vsub : vsub, vg = vdb >> 1;
+    // words of this thread: tile tt of the stage (of a wave, as most that places them)
+    const int tt = wave >> 2, khi = wave & 1;
+    const int ksub = wave >> 1 & 1;                          // K: lane slot khi 64 + lane, words NW ksub ..
+    const int vhi = D == 128 ? khi : 0, vsub = D == 128 ? ksub : wave & 3;   // V: lane slot vhi 64 + lane, words NW vsub ..
+    const int vdb = D == 128 ? 4 * khi + 2 * ksub : vsub, vg = vdb >> 1;
+    const int kkey = 8 * ((lane & 15) >> 2) + 4 * khi + (lane & 3);
     uint32_t kw[NW], vw[NW];
     uint16_t ksc[NW], klo[NW];
     u32x4 vsc, vlo;
@@ -597,35 +612,39 @@ __global__ void __launch_bounds__(64 * PF_W) kv4_prefill_kernel(Kv4AttnArgs a) {
     // (a tile past the last key's repeats that one: its keys are never seen)
     auto load_k = [&](int st) __attribute__((always_inline)) {
         const uint8_t* kt = kb + (long long)min(2 * st + tt, (nkeys - 1) / KV4_TILE) * TB;
+        const uint8_t* kc = kt + khi * 64 * NW * 8 + ksub * NW * 4;
         if constexpr (NW == 2) {
-            const u32x2 x = *reinterpret_cast<const u32x2*>(kt + kL * 16 + ksub * 8);
+            const u32x2 x = *reinterpret_cast<const u32x2*>(kc + (uint32_t)lane * 16);
             kw[0] = x[0]; kw[1] = x[1];
         } else {
-            kw[0] = *reinterpret_cast<const uint32_t*>(kt + kL * 8 + ksub * 4);
+            kw[0] = *reinterpret_cast<const uint32_t*>(kc + (uint32_t)lane * 8);
         }
 #pragma unroll
         for (int i = 0; i < NW; i++) {
-            const uint8_t* pp = kt + CB + (NW * ksub + i) * 128 + 2 * kkey;
+            const uint8_t* pp = kt + CB + (NW * ksub + i) * 128 + (uint32_t)(2 * kkey);
             ksc[i] = *reinterpret_cast<const uint16_t*>(pp);
             klo[i] = *reinterpret_cast<const uint16_t*>(pp + 64);
         }
     };
     auto load_v = [&](int st) __attribute__((always_inline)) {
         const uint8_t* vt = vb + (long long)min(2 * st + tt, (nkeys - 1) / KV4_TILE) * TB;
+        const uint8_t* vc = vt + vhi * 1024 + vsub * NW * 4;
         if constexpr (NW == 2) {
-            const u32x2 y = *reinterpret_cast<const u32x2*>(vt + vL * 16 + vsub * 8);
+            const u32x2 y = *reinterpret_cast<const u32x2*>(vc + (uint32_t)lane * 16);
             vw[0] = y[0]; vw[1] = y[1];
         } else {
-            vw[0] = *reinterpret_cast<const uint32_t*>(vt + vL * 16 + vsub * 4);
+            vw[0] = *reinterpret_cast<const uint32_t*>(vc + (uint32_t)lane * 16);
         }
-        vsc = *reinterpret_cast<const u32x4*>(vt + CB + vg * 128 + vq4 * 16);
-        vlo = *reinterpret_cast<const u32x4*>(vt + CB + vg * 128 + 64 + vq4 * 16);
+        const uint8_t* vp = vt + CB + vg * 128;
+        vsc = *reinterpret_cast<const u32x4*>(vp + (uint32_t)(lane >> 4) * 16);
+        vlo = *reinterpret_cast<const u32x4*>(vp + 64 + (uint32_t)(lane >> 4) * 16);
     };
     const DqConst dq = dq_const();
     const ZeroOff zo = zero_off(0.f);
     auto unpack_k = [&](int buf) __attribute__((always_inline)) {
         unsigned char* const kd = Ks + (buf * 2 + tt) * FB;
-        const int row = key_perm(kkey);                      // of the score tile (its chunks rotated: fewer bank conflicts)
+        const int kq4 = lane >> 4;
+        const int row = key_perm(kkey);                 // of the score tile (its chunks rotated: fewer bank conflicts)
         const int kch = (row & 16) | ((row ^ (row >> 1 & 8)) & 15);
 #pragma unroll
         for (int i = 0; i < NW; i++) {
@@ -639,6 +658,7 @@ __global__ void __launch_bounds__(64 * PF_W) kv4_prefill_kernel(Kv4AttnArgs a) {
     auto unpack_v = [&](int st, int buf, int nb) __attribute__((always_inline)) {
         unsigned char* const vd = Vs + (buf * 2 + tt) * FB;
         f16x8 s = __builtin_bit_cast(f16x8, vsc), lo = __builtin_bit_cast(f16x8, vlo);
+        const int vn = lane & 15, vq4 = lane >> 4;
         const int key0 = st * PF_KST + tt * 32 + 8 * vq4;    // of the words' eight
         const int left = nkeys - key0;
         if (left < 8) {                                      // what lies behind the last key may be anything
@@ -677,14 +697,25 @@ __global__ void __launch_bounds__(64 * PF_W) kv4_prefill_kernel(Kv4AttnArgs a) {
     bool bad = false;
 
     while (u < u1) {
-        const int hk = (int)(u / a.pf_units);
-        int q;
+        const int hk = PIECES ? blockIdx.x % a.nkv : (int)scalar(u / a.pf_units);
+        const long long head0 = PIECES ? 0 : (long long)hk * a.pf_units;
+        int e;
         long long first;
-        pf_find(a, R, r, u - (long long)hk * a.pf_units, q, first);
-        first += (long long)hk * a.pf_units;
+        pf_find(a, R, r, u - head0, e, first);
+        first += head0;
+        const int q = pf_tile(a, e, nqt);
         const int nst = pf_stages(q, R, r, a.ctx_base);      // stages of the tile
-        const int st0 = (int)(u - first), st1 = (int)min((long long)nst, u1 - first);
-        u = first + st1;
+        int st0, st1;
+        if constexpr (PIECES) {
+            const long long n = (nst + a.pf_chunk - 1) / a.pf_chunk, j = u - first;
+            st0 = (int)(nst * j / n);
+            st1 = (int)(nst * (j + 1) / n);
+            u = u1;
+        } else {
+            st0 = (int)(u - first);
+            st1 = (int)min((long long)nst, u1 - first);
+            u = first + st1;
+        }
         kb = a.k + (long long)hk * a.stride_h;
         vb = a.v + (long long)hk * a.stride_h;
         load_k(st0);
@@ -745,11 +776,11 @@ __global__ void __launch_bounds__(64 * PF_W) kv4_prefill_kernel(Kv4AttnArgs a) {
             unpack_next();
             __syncthreads();
         }
-        f32x16 sc[2];
         f16x8 pf[4];
 #pragma clang loop unroll(disable)
         for (int s = 0; s <= n; s++) {
             // ---- matrix half: scores of stage s, output of stage s - 1
+            f32x16 sc[2];
             if (s < non) {
                 const unsigned char* K = Ks + (s & 1) * 2 * FB;
                 sc[0] = f32x16{};
@@ -828,9 +859,11 @@ __global__ void __launch_bounds__(64 * PF_W) kv4_prefill_kernel(Kv4AttnArgs a) {
         if (wave < PF_W / 2) __syncthreads();
         const bool whole = st0 == 0 && st1 == nst;
         const float lt = l + __shfl_xor(l, 32, 64);
-        if (whole && row < R) {
+        int row_o = q * PF_ROWS + wave * 32 + c;             // (worked out again: not kept in registers all along)
+        asm volatile("" : "+v"(row_o));
+        if (whole && row_o < R) {
             const float inv = lt == 0.f ? 0.f : 1.f / lt;
-            const size_t orow = ((size_t)tok * a.nq + hd) * D;
+            const size_t orow = ((size_t)(row_o / r) * a.nq + hk * r + row_o % r) * D;
 #pragma unroll
             for (int i = 0; i < NS; i++)
 #pragma unroll
@@ -840,8 +873,9 @@ __global__ void __launch_bounds__(64 * PF_W) kv4_prefill_kernel(Kv4AttnArgs a) {
                 }
         }
         if (!whole && active) {
-            // state of this piece: slot 0 of the block if it does not begin the tile, else 1
-            float* pp = a.part + (((size_t)blockIdx.x * 2 + (st0 == 0)) * PF_W + wave) * PF_NREG<D> * 64 + lane;
+            // state of this part: the block's slot; in a line slot 0 of two if it does not begin the tile, else 1
+            const size_t slot = PIECES ? blockIdx.x : (size_t)blockIdx.x * 2 + (st0 == 0);
+            float* pp = a.part + (slot * PF_W + wave) * PF_NREG<D> * 64 + lane;
             pp[0] = m;
             pp[64] = l;
 #pragma unroll
@@ -861,18 +895,24 @@ __global__ void __launch_bounds__(64 * PF_W) kv4_prefill_merge_kernel(Kv4AttnArg
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, h = lane >> 5, c = lane & 31;
     const int q = blockIdx.x, hk = blockIdx.y, i = blockIdx.z;
     const int r = a.nq / a.nkv, R = a.rows * r;
-    const long long total = a.pf_units * a.nkv;
-    long long before = 0;                                    // units of the head's tiles before q
-    for (int q0 = 0; q0 < q; q0 += 64) {
-        int x = q0 + lane < q ? pf_stages(q0 + lane, R, r, a.ctx_base) : 0;
+    const int nqt = (R + PF_ROWS - 1) / PF_ROWS, i0 = pf_tile(a, q, nqt);        // (its own inverse)
+    long long before = 0;                                    // shares of the head's tiles before this one
+    for (int k = 0; k < i0; k += 64) {
+        int x = k + lane < i0 ? pf_weight(a, k + lane, nqt, R, r) : 0;
 #pragma unroll
         for (int off = 32; off > 0; off >>= 1) x += __shfl_xor(x, off, 64);
         before += x;
     }
-    const long long first = hk * a.pf_units + before, last = first + pf_stages(q, R, r, a.ctx_base) - 1;
-    // block that has unit u: the largest b with total * b / nblocks <= u
-    auto block_of = [&](long long x) { return (int)(((x + 1) * nblocks - 1) / total); };
-    const int b0 = block_of(first), b1 = block_of(last);
+    const int own = pf_weight(a, i0, nqt, R, r);
+    int b0 = 0, b1 = own - 1;                                // its parts; in a line the blocks from its first unit's to its last's
+    if (!a.pf_chunk) {
+        const long long total = a.pf_units * a.nkv, first = hk * a.pf_units + before;
+        // block that has unit x: the largest b with total * b / nblocks <= x
+        auto block_of = [&](long long x) { return (int)(((x + 1) * nblocks - 1) / total); };
+        b0 = block_of(first);
+        b1 = block_of(first + own - 1);
+    }
+    auto slot_of = [&](int b) { return a.pf_chunk ? (size_t)(before + b) * a.nkv + hk : (size_t)b * 2 + (b == b0); };
     if (b0 == b1 || q * PF_ROWS + wave * 32 >= R) return;
     constexpr int CB = 4;                                    // pieces requested together
     float M = -INFINITY, L = 0.f, acc[16] = {};
@@ -881,7 +921,7 @@ __global__ void __launch_bounds__(64 * PF_W) kv4_prefill_merge_kernel(Kv4AttnArg
 #pragma unroll
         for (int j = 0; j < CB; j++) {
             const int b = min(p0 + j, b1);
-            const float* pp = a.part + (((size_t)b * 2 + (b == b0)) * PF_W + wave) * PF_NREG<D> * 64 + lane;
+            const float* pp = a.part + (slot_of(b) * PF_W + wave) * PF_NREG<D> * 64 + lane;
             mc[j] = pp[0];
             lc[j] = pp[64];
 #pragma unroll
@@ -965,27 +1005,81 @@ int launch_kv4_decode(const Kv4AttnArgs& args, int waves, hipStream_t stream) {
     return a.d == 64 ? launch_decode<64, 1>(a, waves, stream) : -1;
 }
 
+constexpr int kMaxParts = 512;       // states of parts in the workspace
+
+// Few queries or keys are left to the decode kernel, a row for each (p.single): it has no fixed cost to speak of, but
+// reads the keys once for every query.  The two take the same time at about 2^21 tiles x dims: heads of 128, 8 kv heads,
+// 8 / 64 queries of 1000 keys 7.7 / 15.0 us and 12.2 / 19.5 with the prefill kernel, 8 / 12 of 16000 27 / 38 and 28 / 32,
+// 24 of 3000 21 and 18; 2 kv heads of 64, 61 of 250 5 and 13.5, 64 of 16000 32 and 48.
+//
+// For the prefill kernel the way of dealing out the work with the least estimated time, in us.  Pieces waste less on starts and on states;
+// the line ends everywhere at once, and takes any number of stages with two states per block.  Measured (pieces, line):
+// 128 wide, 32 heads of 8, 1000 tokens from nothing 37 and 51, 64 behind 4000 26.5 and 41, 512 behind 4096 71 and 69,
+// 5000 from nothing 265 and 346; 28 heads of 4, 2000 behind 2000 137 and 148, and in parts that fill the chip badly 172.
 Kv4PrefillPlan kv4_prefill_plan(int T, int hist, int nkv, int r, int d) {
     const int R = T * r, nqt = (R + PF_ROWS - 1) / PF_ROWS;
     Kv4PrefillPlan p;
-    for (int q = 0; q < nqt; q++) p.units += pf_stages(q, R, r, hist);
+    int most = 0;
+    for (int q = 0; q < nqt; q++) {
+        const int st = pf_stages(q, R, r, hist);
+        p.units += st;
+        most = std::max(most, st);
+    }
+    const size_t state = (size_t)PF_W * (2 + 16 * (d / 32)) * 64 * 4;
     const long long total = p.units * nkv;
+    // of either kernel (grows with T and hist)
+    const int few = std::min(T, 1024);                       // (more see too many keys)
+    const long long tiles = ((long long)hist + few + KV4_TILE - 1) / KV4_TILE, pairs = (long long)few * nkv;
+    p.part_bytes = std::max((size_t)std::min<long long>(kMaxParts, 2 * total) * state,
+                            (size_t)std::min<long long>(2 * kCus, pairs * tiles) * r * (d + 2) * 4);
+    p.single = T == few && pairs * tiles * d <= 1 << 21;
+    if (p.single) return p;
+    // a stage of one block alone and with all others (the clock falls), a part's start and end, its state written and read
+    // back (of its waves that have rows), the merge launch
+    const double t = d == 128 ? 2.2 : 1.9, tf = 1.1 * t, start = 5.0, merge = 3.0;
+    const double part = std::min(1.0, (R + 31) / 32 / (double)PF_W) * state * 2 / 5.4e6;
     p.blocks = (int)std::min<long long>(kCus, total);
-    // (of as many blocks as there may be: grows with T and hist)
-    p.part_bytes = (size_t)std::min<long long>(kCus, total) * 2 * PF_W * (2 + 16 * (d / 32)) * 64 * 4;
+    const long long run = (total + p.blocks - 1) / p.blocks;
+    int starts = 0;                                          // of the block that has the shortest tiles
+    for (long long sum = 0; starts < nqt && sum < run; starts++) sum += pf_stages(starts, R, r, hist);
+    double best = run * tf + (starts + 0.5) * start + 2 * p.blocks * part + merge;
+    for (int c = (int)std::min<long long>(most, std::max<long long>(1, total / kMaxParts));; c += c < 8 ? 1 : c / 5) {
+        c = std::min(c, most);
+        long long items = 0;
+        double longest = 0, work = 0, end = 0;               // us of a part, of all so far; end of one that has to wait for another's
+        for (int q = nqt - 1; q >= 0; q--) {
+            const int st = pf_stages(q, R, r, hist), n = (st + c - 1) / c, len = (st + n - 1) / n;
+            items += (long long)n * nkv;
+            work += (double)n * nkv * (len * tf + start);
+            longest = std::max(longest, len * t + start);
+            if (items > kCus) end = std::max(end, work / kCus + len * t + start);
+        }
+        const bool split = c < most;
+        if (!split || items <= kMaxParts) {
+            double us = std::max(longest, std::min(end, (double)((items + kCus - 1) / kCus) * longest));
+            if (split) us += items * part + merge;
+            if (us < best) {
+                best = us;
+                p.chunk = c;
+                p.blocks = (int)items;
+            }
+        }
+        if (c >= most) break;
+    }
+    p.merge = p.chunk ? p.chunk < most : p.blocks > 1;
     return p;
 }
 
-template <int D>
-static int launch_prefill(const Kv4AttnArgs& a, int blocks, hipStream_t stream) {
+template <int D, bool PIECES>
+static int launch_prefill(const Kv4AttnArgs& a, const Kv4PrefillPlan& p, hipStream_t stream) {
     const size_t lds = (size_t)8 * 32 * D * 2 + 4 * (D / 32 + 1) * 8;
     static LdsLimit lim;
-    if (ensure_lds_limit(lim, (const void*)kv4_prefill_kernel<D>, lds)) return -1;
-    hipLaunchKernelGGL(kv4_prefill_kernel<D>, dim3(blocks), dim3(64 * PF_W), lds, stream, a);
+    if (ensure_lds_limit(lim, (const void*)kv4_prefill_kernel<D, PIECES>, lds)) return -1;
+    hipLaunchKernelGGL((kv4_prefill_kernel<D, PIECES>), dim3(p.blocks), dim3(64 * PF_W), lds, stream, a);
     const int R = a.rows * (a.nq / a.nkv);
-    if (blocks > 1)
+    if (p.merge)
         hipLaunchKernelGGL(kv4_prefill_merge_kernel<D>, dim3((R + PF_ROWS - 1) / PF_ROWS, a.nkv, D / 32), dim3(64 * PF_W), 0,
-                           stream, a, blocks);
+                           stream, a, p.blocks);
     return hipGetLastError() == hipSuccess ? 0 : -1;
 }
 
@@ -993,8 +1087,21 @@ int launch_kv4_prefill(const Kv4AttnArgs& a, hipStream_t stream) {
     if (a.rows < 1 || !a.part) return -1;
     const Kv4PrefillPlan p = kv4_prefill_plan(a.rows, a.ctx_base, a.nkv, a.nq / a.nkv, a.d);
     Kv4AttnArgs b = a;
+    if (p.single) {
+        b.max_ctx = a.ctx_base + a.rows - 1;
+        const Kv4DecodePlan dp = kv4_decode_plan(a.rows, a.nkv, a.nq / a.nkv, a.d, b.max_ctx);
+        b.nsplit = dp.nsplit;
+        return launch_kv4_decode(b, dp.waves, stream);
+    }
+    // every block has a part, every state a slot
+    if (p.blocks < 1 || (!p.chunk && p.blocks > std::min<long long>(kCus, p.units * a.nkv)) ||
+        (p.chunk && p.merge && p.blocks > kMaxParts))
+        return -1;
     b.pf_units = p.units;
-    return a.d == 128 ? launch_prefill<128>(b, p.blocks, stream) : a.d == 64 ? launch_prefill<64>(b, p.blocks, stream) : -1;
+    b.pf_chunk = p.chunk;
+    if (a.d == 128) return p.chunk ? launch_prefill<128, true>(b, p, stream) : launch_prefill<128, false>(b, p, stream);
+    if (a.d == 64) return p.chunk ? launch_prefill<64, true>(b, p, stream) : launch_prefill<64, false>(b, p, stream);
+    return -1;
 }
 
 int load_kv4_attn() { return load_code((const void*)kv4_decode_kernel<128, 1>); }

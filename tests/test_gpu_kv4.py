@@ -598,3 +598,104 @@ def test_prefill_nan_values_reach_the_rows_that_see_them():
             # (the other dims of a group with a NaN were quantised with it: not compared)
             if ok.any():
                 check(np.where(ok, got[t], ref), ref, tol, f"query {t}")
+
+
+# ------------------------------------------------- prefills of many queries
+#
+# A prefill of few queries or keys runs as rows of the decode kernel (T kv heads ceil(keys / 32) head_dim up to 2^21);
+# these are beyond, in every way of dealing out the work: whole row tiles, parts of them, equal runs.
+
+@pytest.mark.parametrize("nq,nkv,d,T,hist", [
+    (64, 64, 64, 129, 0), (64, 64, 64, 33, 500), (64, 64, 64, 2, 8200), (32, 16, 128, 100, 333), (32, 16, 128, 257, 0),
+    (32, 16, 128, 31, 1055), (56, 8, 128, 65, 1000), (56, 8, 128, 300, 0), (14, 2, 64, 511, 700), (24, 8, 64, 401, 31),
+    (8, 1, 128, 1025, 0), (7, 1, 128, 900, 4000), (64, 8, 128, 1500, 1), (40, 8, 64, 2049, 63)])
+def test_prefill_many_queries(nq, nkv, d, T, hist):
+    log(f"prefill heads {nq}/{nkv} d {d} T {T} hist {hist}")
+    n = hist + T
+    assert T * nkv * -(-n // 32) * d > 2 ** 21
+    c, kh, vh, rng = filled(nq, nkv, d, 1, n, seed=T, max_seq=n + 5)
+    q = bf16_values(rng, (T, nq, d))
+    got = prefill(c, q, hist)
+    assert np.isfinite(got).all()
+    for t in sorted({0, 1, T // 3, T // 2, T - 2, T - 1}):
+        ref, tol = O.attend(q[t].astype(np.float64), kh[0], vh[0], np.arange(n) <= hist + t, key_eps=2.0 ** -11)
+        check(got[t], ref, tol, f"query {t}")
+
+
+def test_prefill_forms_agree_at_their_border():
+    """The same queries as one call of the prefill kernel and as calls of a few each, which the decode kernel takes."""
+    nq, nkv, d, T, hist = 32, 16, 128, 120, 300
+    c, kh, vh, rng = filled(nq, nkv, d, 1, hist + T, seed=30)
+    q = bf16_values(rng, (T, nq, d))
+    whole = prefill(c, q, hist)
+    for at, n in ((0, 1), (1, 8), (9, 40), (49, 71)):
+        part = prefill(c, q[at:at + n], hist + at)
+        for t in {0, n // 2, n - 1}:
+            _, tol = O.attend(q[at + t].astype(np.float64), kh[0], vh[0], np.arange(hist + T) <= hist + at + t, key_eps=2.0 ** -11)
+            a, z = part[t], whole[at + t]
+            assert (np.abs(a - z) <= 2 * tol * 1.01 + 2.0 ** -7 * np.abs(a)).all()
+
+
+@pytest.mark.parametrize("qscale,vscale", [(1e-6, 1.0), (30.0, 1.0), (1e4, 300.0), (1.0, 15000.0), (1.0, 1e-4)])
+def test_prefill_many_ranges(qscale, vscale):
+    rng = np.random.default_rng(31)
+    n, T, nkv = 333, 120, 16
+    c = new_cache(config(32, nkv, 128, n), 1)
+    k = bf16_values(rng, (1, n, nkv, 128))
+    v = round_bf16(np.clip(bf16_values(rng, (1, n, nkv, 128), vscale), -65280, 65280)).astype(np.float32)
+    c.append(dev(k), dev(v), [0])
+    kh, vh = (np.swapaxes(O.held(x), 1, 2) for x in (k, v))
+    q = round_bf16(bf16_values(rng, (T, 32, 128)) * qscale).astype(np.float32)
+    got = prefill(c, q, n - T)
+    for t in (0, 13, T - 1):
+        ref, tol = O.attend(q[t].astype(np.float64), kh[0], vh[0], np.arange(n) <= n - T + t, key_eps=2.0 ** -11)
+        check(got[t], ref, tol, f"query {t}")
+
+
+@pytest.mark.parametrize("T,n", [(210, 210), (90, 400)])
+def test_prefill_many_nan_values_reach_the_rows_that_see_them(T, n):
+    """As for few queries; slots after the last query hold NaN, too."""
+    nq, nkv, d = 32, 16, 128
+    t0 = n - T
+    rng = np.random.default_rng(32)
+    k, v = bf16_values(rng, (1, n, nkv, d)), bf16_values(rng, (1, n, nkv, d))
+    at = [n - 60, n - 20, n - 10]
+    v[0, at[0], 0, 40], v[0, at[1], 9, 127], k[0, at[2], 9, 3] = np.nan, np.inf, np.nan
+    c = new_cache(config(nq, nkv, d, n + 70), 1)
+    c.append(dev(k), dev(v), [0])
+    junk = torch.full((1, 70, nkv, d), float("nan"), dtype=torch.bfloat16, device="cuda")
+    c.append(junk, junk, [n])
+    q = bf16_values(rng, (T, nq, d))
+    got = prefill(c, q, t0)
+    want = np.zeros(got.shape, bool)
+    want[at[0] - t0:, 0:2, 32:64] = True
+    want[at[1] - t0:, 18:20, 96:128] = True
+    want[at[2] - t0:, 18:20, :] = True
+    assert np.array_equal(np.isnan(got), want)
+    for x in (k, v):
+        x[~np.isfinite(x)] = 0.0
+    kh, vh = (np.swapaxes(O.held(x), 1, 2) for x in (k, v))
+    for t in (0, at[0] - t0 - 1, at[0] - t0, T - 1):
+        ref, tol = O.attend(q[t].astype(np.float64), kh[0], vh[0], np.arange(n) <= t0 + t, key_eps=2.0 ** -11)
+        check(np.where(want[t], ref, got[t]), ref, tol, f"query {t}")
+
+
+def test_prefill_many_captured_on_another_stream():
+    nq, nkv, d, n, T = 32, 16, 128, 900, 200
+    c, kh, vh, rng = filled(nq, nkv, d, 1, n, seed=33)
+    q = dev(bf16_values(rng, (T, nq, d)))
+    out, ref = torch.zeros_like(q), torch.zeros_like(q)
+    c.attn_prefill(q, n - T, ref)
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        c.attn_prefill(q, n - T, out)
+    side = torch.cuda.Stream()
+    for _ in range(4):
+        q.copy_(dev(bf16_values(rng, (T, nq, d))))
+        torch.cuda.synchronize()
+        with torch.cuda.stream(side):
+            g.replay()
+        side.synchronize()
+        c.attn_prefill(q, n - T, ref)
+        torch.cuda.synchronize()
+        assert torch.equal(out, ref)

@@ -126,3 +126,12 @@ def test_struct_matches_the_header():
 
 def test_set_kv_format_refusals():
     assert B.layer_set_kv_format(None, B.W4_KV_INT4) == B.W4_EINVAL
+
+
+def test_longest_cache():
+    """2^27 slots at most: rows of queries are counted in 31 bits."""
+    for n, rc in ((2 ** 27, B.W4_ECAPACITY), (2 ** 27 + 1, B.W4_EUNSUPPORTED)):
+        d = desc(max_seq=n, stride_h=(n + 31) // 32 * 32 * 80, stride_b=(n + 31) // 32 * 32 * 80 * 8)
+        assert B.kv4_append(d, P, P, P, P, 1, 2, [n - 1], stream=0) == rc
+        assert B.kv4_attn_prefill(d, P, 5, n, 32, P, P, 2 * P, P, 1 << 40, stream=0) == rc
+        assert (B.kv4_attn_workspace_size(d, 32, 1, 1, 2 ** 31 - 1, 2 ** 31 - 1) > 0) == (rc == B.W4_ECAPACITY)
