@@ -475,7 +475,7 @@ PrefillWs plan_prefill(const layer_s* L, int T, int hist) {
     return w;
 }
 
-struct DecodeWs { size_t q, part, attn, h, g, xn, kv, total; int nsplit, waves; };
+struct DecodeWs { size_t q, part, attn, h, g, xn, kv, total; int nsplit; };
 DecodeWs plan_decode(const layer_s* L, int B, int max_ctx) {
     const layer_config& c = L->cfg;
     const size_t qd = (size_t)c.n_heads * c.head_dim;
@@ -485,11 +485,7 @@ DecodeWs plan_decode(const layer_s* L, int B, int max_ctx) {
     // attention shares; their arrival counters live in g, which is written
     // only after the attention (a layer whose g is too small takes one share)
     w.nsplit = c.n_kv_heads * 4 <= L->F_pad * 2 ? attn_decode_splits(B, c.n_kv_heads, max_ctx, L->num_cus) : 1;
-    if (kv4) {
-        const Kv4DecodePlan p = kv4_decode_plan(B, c.n_kv_heads, r, c.head_dim, max_ctx);
-        w.nsplit = p.nsplit;
-        w.waves = p.waves;
-    }
+    if (kv4) w.nsplit = kv4_decode_shares(B, c.n_kv_heads, r, c.head_dim, max_ctx);
     // (sized for a share per 64 keys, at least as many as there are)
     const int nchunks = (max_ctx + 64) / 64;
     Carve cv;
@@ -851,7 +847,7 @@ int run_decode_seq(layer_s* L, const float* x, const int32_t* pos, const int32_t
         ka.nsplit = w.nsplit;
         ka.part = part;
         ProfScope ps(L, ps_stage, ps_stage == 2 ? 1 : 2, st);
-        rc |= launch_kv4_decode(ka, w.waves, st);
+        rc |= launch_kv4_decode(ka, st);
     }
     AttnDecodeArgs ad{};
     ad.q = q;
@@ -1548,10 +1544,9 @@ int kv4_attn_decode(const kv4_desc* d, const void* q, const int32_t* ctx_lens, i
     a.max_ctx = max_ctx;
     a.mask = attn_mask;
     a.rows = B;
-    const Kv4DecodePlan plan = kv4_decode_plan(B, d->n_kv_heads, n_heads / d->n_kv_heads, d->head_dim, max_ctx);
-    a.nsplit = plan.nsplit;
+    a.nsplit = kv4_decode_shares(B, d->n_kv_heads, n_heads / d->n_kv_heads, d->head_dim, max_ctx);
     a.part = (float*)ws;
-    if (launch_kv4_decode(a, plan.waves, (hipStream_t)stream))
+    if (launch_kv4_decode(a, (hipStream_t)stream))
         return fail(W4_EHIP, "kernel launch failed: %s", hipGetErrorString(hipGetLastError()));
     return W4_OK;
 }

@@ -71,12 +71,9 @@ struct Kv4AttnArgs {
     int r, per;              // set by the launcher: nq / nkv; decode: tiles per share
     int* err;                // raised with W4_FLAG_F16_RANGE (out_f16), or null
 };
-struct Kv4DecodePlan {
-    int waves = 8, nsplit = 1;
-};
-Kv4DecodePlan kv4_decode_plan(int rows, int nkv, int r, int d, int max_ctx);
+int kv4_decode_shares(int rows, int nkv, int r, int d, int max_ctx);      // nsplit
 size_t kv4_decode_part_bound(int rows, int nkv, int r, int d, int max_ctx);
-int launch_kv4_decode(const Kv4AttnArgs& a, int waves, hipStream_t stream);
+int launch_kv4_decode(const Kv4AttnArgs& a, hipStream_t stream);
 // Prefill: rows queries of one sequence after ctx_base tokens (part: part_bytes).
 struct Kv4PrefillPlan {
     long long units = 0;     // stages of one kv head's row tiles

@@ -28,7 +28,7 @@ constexpr float LOG2E = 1.4426950408889634f;
 
 // ---------------------------------------------------------------- decode
 
-constexpr int MAXW = 8;          // waves per block
+constexpr int DW = 8;            // waves per block
 constexpr long long kMaxShares = 1024;   // beyond one per (row, kv head), of a launch
 constexpr int kCus = 256;
 constexpr int MAXR = 8;          // query heads per kv head
@@ -85,7 +85,7 @@ __device__ __forceinline__ void put_pair(const Kv4AttnArgs& a, size_t off, float
 }
 
 // One block: a share (a.per tiles) of one (row, kv head), all r query heads of the
-// group.  Wave w of W takes tiles w, w + W, .. of the share on its own; the next
+// group.  Wave w of 8 takes tiles w, w + 8, .. of the share on its own; the next
 // tile's K is requested when this one's scores are formed and its V when its
 // output is, into the same registers, so that two blocks fit a CU (CT 1).  The first
 // tile's requests do not wait for the context length: a share's place is fixed by
@@ -98,12 +98,12 @@ __device__ __forceinline__ void put_pair(const Kv4AttnArgs& a, size_t off, float
 // passes the fp16 range after all (a scale above 8), ef drops to 1 for the rest of
 // the share: e^2 times the largest scale (8734) is 64536.
 template <int D, int CT>
-__global__ void __launch_bounds__(64 * MAXW, CT == 1 ? 4 : 2) kv4_decode_kernel(Kv4AttnArgs a) {
+__global__ void __launch_bounds__(64 * DW, CT == 1 ? 4 : 2) kv4_decode_kernel(Kv4AttnArgs a) {
     constexpr int NS = D / 32, NDB = D / 16, HC = 16 / NS, PS = 8 / NS;
     constexpr int TB = kv4_tile_bytes(D), CB = kv4_code_bytes(D);
-    extern __shared__ __attribute__((aligned(16))) float ored[];          // [W][r][D]
-    __shared__ float gst[MAXW][MAXR][2], glo[MAXW][MAXR][NS];
-    const int tid = threadIdx.x, lane = tid & 63, NT = blockDim.x, W = NT >> 6;
+    extern __shared__ __attribute__((aligned(16))) float ored[];          // [DW][r][D]
+    __shared__ float gst[DW][MAXR][2], glo[DW][MAXR][NS];
+    const int tid = threadIdx.x, lane = tid & 63;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int hk = blockIdx.x, part = blockIdx.y, b = blockIdx.z, r = a.r;
     const int n16 = lane & 15, q4 = lane >> 4, g = n16 % NS;
@@ -211,7 +211,7 @@ __global__ void __launch_bounds__(64 * MAXW, CT == 1 ? 4 : 2) kv4_decode_kernel(
     }
     float ef = 1024.f;
 
-    for (; tile < tile1; tile += W) {
+    for (; tile < tile1; tile += DW) {
         f32x4 acc[CT][2];
 #pragma unroll
         for (int ct = 0; ct < CT; ct++) acc[ct][0] = acc[ct][1] = f32x4{0.f, 0.f, 0.f, 0.f};
@@ -259,7 +259,7 @@ __global__ void __launch_bounds__(64 * MAXW, CT == 1 ? 4 : 2) kv4_decode_kernel(
                 }
             }
         }
-        if (tile + W < tile1) load_k(tile + W);
+        if (tile + DW < tile1) load_k(tile + DW);
         f16x8 pf[CT], pl[CT];
 #pragma unroll
         for (int ct = 0; ct < CT; ct++) {
@@ -364,7 +364,7 @@ __global__ void __launch_bounds__(64 * MAXW, CT == 1 ? 4 : 2) kv4_decode_kernel(
                 o[ct][i] = __builtin_amdgcn_mfma_f32_16x16x32_f16(pl[ct], vf, o[ct][i], 0, 0, 0);
             }
         }
-        if (tile + W < tile1) load_v(tile + W);
+        if (tile + DW < tile1) load_v(tile + DW);
     }
 
     // ---- the waves' states meet in LDS
@@ -393,12 +393,12 @@ __global__ void __launch_bounds__(64 * MAXW, CT == 1 ? 4 : 2) kv4_decode_kernel(
     // one share: the output; more: its state, [row, kv head][share][r heads][D] outputs, then [..][r] (max, sum)
     float* const po = a.part + slot * D;
     bool bad = false;
-    for (int idx = tid; idx < r * (D / 2); idx += NT) {
+    for (int idx = tid; idx < r * (D / 2); idx += 64 * DW) {
         const int i = idx / (D / 2), d = 2 * (idx % (D / 2));
         float M = -INFINITY;
-        for (int w = 0; w < W; w++) M = fmaxf(M, gst[w][i][0]);
+        for (int w = 0; w < DW; w++) M = fmaxf(M, gst[w][i][0]);
         float x = 0.f, y = 0.f, lt = 0.f;
-        for (int w = 0; w < W; w++) {
+        for (int w = 0; w < DW; w++) {
             const float sc = gst[w][i][0] == -INFINITY ? 0.f : exp2_hw((gst[w][i][0] - M) * LOG2E);
             const float2 v = *reinterpret_cast<const float2*>(ored + (w * r + i) * D + d);
             x += sc * (v.x + glo[w][i][d / 32]);
@@ -599,10 +599,11 @@ __global__ void __launch_bounds__(64 * PF_W) kv4_prefill_kernel(Kv4AttnArgs a) {
     long long u = PIECES ? blockIdx.x / a.nkv : scalar(total * blockIdx.x / gridDim.x);
     const long long u1 = PIECES ? u + 1 : scalar(total * (blockIdx.x + 1) / gridDim.x);
 
-    // words of this thread: tile tt of the stage (of a wave, as most that places them)
-    const int tt = wave >> 2, khi = wave & 1;
-    const int ksub = wave >> 1 & 1;                          // K: lane slot khi 64 + lane, words NW ksub ..
-    const int vhi = D == 128 ? khi : 0, vsub = D == 128 ? ksub : wave & 3;   // V: lane slot vhi 64 + lane, words NW vsub ..
+    // Words of this thread: tile tt of the stage (not in scalar registers: their 64-bit products hold up the stage; 2011
+    // queries of 28 heads of 4 behind 14001 tokens 485 us and 513)
+    const int wv = tid >> 6, tt = wv >> 2, khi = wv & 1;
+    const int ksub = wv >> 1 & 1;                            // K: lane slot khi 64 + lane, words NW ksub ..
+    const int vhi = D == 128 ? khi : 0, vsub = D == 128 ? ksub : wv & 3;   // V: lane slot vhi 64 + lane, words NW vsub ..
     const int vdb = D == 128 ? 4 * khi + 2 * ksub : vsub, vg = vdb >> 1;
     const int kkey = 8 * ((lane & 15) >> 2) + 4 * khi + (lane & 3);
     uint32_t kw[NW], vw[NW];
@@ -961,21 +962,22 @@ __global__ void __launch_bounds__(64 * PF_W) kv4_prefill_merge_kernel(Kv4AttnArg
 
 }  // namespace
 
-// Waves per block and shares per (row, kv head).  A block costs about 5 us to begin
-// and end and 0.12 us a tile (eight waves to a CU; d = 128), a second share the clearing launch and the
-// hand-off, about 3.5 us: below 32 tiles one block is the faster.  Else a tile per
-// wave, as long as the blocks fit the CUs at once (two to a CU; one of more than 4 heads
-// of d = 128).  Llama-8B shape, 1 row of 2048 keys: 1 share 13.3 us, 2 12.4, 4
-// 10.4, 8 9.7, 16 10.5; 16 rows of up to 32768: 1 192, 2 114, 4 105, 8 109; Qwen-0.5B,
-// 512 keys: 1 5.7, 2 8.2; Qwen-7B, 8 rows of up to 8192: 4 26.5, 8 20.1, 16 29.3.
-Kv4DecodePlan kv4_decode_plan(int rows, int nkv, int r, int d, int max_ctx) {
+// Shares per (row, kv head).  A block costs about 5 us to begin and end and a wave 0.35
+// us a tile, a second share the merge launch, about 2.5 us: below 32 tiles one block is the
+// faster.  Else a tile per wave, as long as the blocks fit the CUs at once (two to a
+// CU; one of more than 4 heads of d = 128).  32 heads of 8, d = 128, 1 row of 2048 keys: 1
+// share 13.3 us, 2 12.4, 4 10.4, 8 9.7, 16 10.5; 16 rows of up to 32768: 1 192, 2
+// 114, 4 105, 8 109; 14 heads of 2, d = 64, 512 keys: 1 5.7, 2 8.2; 28 heads of 4, d = 128, 8 rows
+// of up to 8192: 4 26.5, 8 20.1, 16 29.3.
+//
+// The wide kernel (CT 2) is bound by the vector units, 0.55 us a tile of a SIMD; waves of four heads each,
+// twice as many, took 8.7 and 8.0 us for 1 row of 500 and 2000 keys of 28 heads of 4 instead of 9.2 and 9.4, but 88 instead
+// of 81 for 16 of up to 32000.
+int kv4_decode_shares(int rows, int nkv, int r, int d, int max_ctx) {
     const long long tiles = ((long long)max_ctx + KV4_TILE) / KV4_TILE, pairs = (long long)rows * nkv;
     const bool wide = d == 128 && r > 4;
-    Kv4DecodePlan p;
-    p.waves = 8;
-    const long long n = tiles < 32 ? 1 : std::min((wide ? 1 : 2) * kCus / pairs, (tiles + p.waves - 1) / p.waves);
-    p.nsplit = (int)std::max(1ll, std::min({n, tiles, kMaxShares / pairs + 1}));
-    return p;
+    const long long n = tiles < 32 ? 1 : std::min((wide ? 1 : 2) * kCus / pairs, (tiles + DW - 1) / DW);
+    return (int)std::max(1ll, std::min({n, tiles, kMaxShares / pairs + 1}));
 }
 
 // Share states of any plan up to `rows` and max_ctx (grows with both).
@@ -985,24 +987,23 @@ size_t kv4_decode_part_bound(int rows, int nkv, int r, int d, int max_ctx) {
 }
 
 template <int D, int CT>
-static int launch_decode(const Kv4AttnArgs& a, int waves, hipStream_t stream) {
-    const size_t lds = (size_t)waves * a.r * D * 4;       // the waves' outputs (at most 32 KB)
-    hipLaunchKernelGGL((kv4_decode_kernel<D, CT>), dim3(a.nkv, a.nsplit, a.rows), dim3(64 * waves), lds, stream, a);
+static int launch_decode(const Kv4AttnArgs& a, hipStream_t stream) {
+    const size_t lds = (size_t)DW * a.r * D * 4;       // the waves' outputs (at most 32 KB)
+    hipLaunchKernelGGL((kv4_decode_kernel<D, CT>), dim3(a.nkv, a.nsplit, a.rows), dim3(64 * DW), lds, stream, a);
     if (a.nsplit > 1) hipLaunchKernelGGL(kv4_decode_merge_kernel<D>, dim3(a.nkv, a.r, a.rows), dim3(256), 0, stream, a);
     return hipGetLastError() == hipSuccess ? 0 : -1;
 }
 
-int launch_kv4_decode(const Kv4AttnArgs& args, int waves, hipStream_t stream) {
+int launch_kv4_decode(const Kv4AttnArgs& args, hipStream_t stream) {
     Kv4AttnArgs a = args;
     const int r = a.r = a.nq / a.nkv;
     const int tiles = (int)(((long long)a.max_ctx + KV4_TILE) / KV4_TILE);
-    if (r < 1 || r > MAXR || waves < 1 || waves > MAXW || a.nsplit < 1 || a.nsplit > tiles) return -1;
+    if (r < 1 || r > MAXR || a.nsplit < 1 || a.nsplit > tiles) return -1;
     if (a.nsplit > 1 && !a.part) return -1;
     a.per = (tiles + a.nsplit - 1) / a.nsplit;
     a.nsplit = (tiles + a.per - 1) / a.per;              // (no share beyond the longest context)
-    if (a.d == 128 && r <= 4) return launch_decode<128, 1>(a, waves, stream);
-    if (a.d == 128) return waves <= 8 ? launch_decode<128, 2>(a, waves, stream) : -1;
-    return a.d == 64 ? launch_decode<64, 1>(a, waves, stream) : -1;
+    if (a.d == 128) return r <= 4 ? launch_decode<128, 1>(a, stream) : launch_decode<128, 2>(a, stream);
+    return a.d == 64 ? launch_decode<64, 1>(a, stream) : -1;
 }
 
 constexpr int kMaxParts = 512;       // states of parts in the workspace
@@ -1089,9 +1090,8 @@ int launch_kv4_prefill(const Kv4AttnArgs& a, hipStream_t stream) {
     Kv4AttnArgs b = a;
     if (p.single) {
         b.max_ctx = a.ctx_base + a.rows - 1;
-        const Kv4DecodePlan dp = kv4_decode_plan(a.rows, a.nkv, a.nq / a.nkv, a.d, b.max_ctx);
-        b.nsplit = dp.nsplit;
-        return launch_kv4_decode(b, dp.waves, stream);
+        b.nsplit = kv4_decode_shares(a.rows, a.nkv, a.nq / a.nkv, a.d, b.max_ctx);
+        return launch_kv4_decode(b, stream);
     }
     // every block has a part, every state a slot
     if (p.blocks < 1 || (!p.chunk && p.blocks > std::min<long long>(kCus, p.units * a.nkv)) ||
