@@ -437,8 +437,8 @@ int kv_append(const kv_desc* desc, void* k_cache, void* v_cache,
  * written may hold anything.
  *
  * Every kv4_ call takes cache, key / value, query and output pointers that are
- * 16-byte aligned, and checks its arguments on the host before anything is
- * launched.  Calls are asynchronous on the stream, allocate nothing and may be
+ * 16-byte aligned, K's and V's apart where they are written, and checks its arguments on the host
+ * before anything is launched.  Calls are asynchronous on the stream, allocate nothing and may be
  * captured into a graph (the host's slot_start is then part of the graph).  Two
  * calls that write the same sequence's cache, or one that writes what another
  * reads, must be ordered by the caller; different sequences of a cache may be
@@ -455,7 +455,7 @@ typedef struct kv4_desc {
 
 /* The layout for a batch of sequences (pure host computation; of cfg it reads
  * n_kv_heads, head_dim and max_seq).  Errors: W4_EINVAL, W4_EUNSUPPORTED
- * (head_dim). */
+ * (head_dim, max_seq). */
 int kv4_layout(const layer_config* cfg, int32_t batch, kv4_desc* out);
 
 /* Quantise new keys / values k_new, v_new (bf16 [B][T][n_kv_heads][head_dim],
@@ -527,7 +527,8 @@ int kv4_attn_prefill(const kv4_desc* desc, const void* q, int32_t T, int32_t his
  * and a whole prefill see the same keys.  A key or value without fp16 value
  * raises W4_FLAG_F16_RANGE.  Workspace sizes depend on the format: set it
  * first.  Such a layer decodes as the kernel sequence; with decode path 2 its
- * decode calls are refused (W4_EUNSUPPORTED).  Errors: W4_EINVAL. */
+ * decode calls are refused (W4_EUNSUPPORTED).  Errors: W4_EINVAL,
+ * W4_EUNSUPPORTED (max_seq). */
 int layer_set_kv_format(layer_t layer, int32_t format);
 
 /* ---- diagnostics ------------------------------------------------------- */

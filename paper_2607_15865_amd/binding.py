@@ -679,21 +679,21 @@ class KV4Cache:
     integers holding the bits) on the cache's device, which must be the current
     one.  Calls run on ``stream`` (default: torch's current stream).  A call's
     workspace is kept per stream; under graph capture it is allocated in the
-    capture, so that every graph has its own."""
+    capture, so that every graph has its own.  The caches k and v stay the same tensors."""
 
     def __init__(self, cfg, batch: int):
         import torch
         rc, self.desc = kv4_layout(cfg, batch)
         check(rc)
         self.n_heads = cfg.n_heads
-        self.k = torch.empty(self.desc.bytes, dtype=torch.uint8, device="cuda")
-        self.v = torch.empty(self.desc.bytes, dtype=torch.uint8, device="cuda")
+        self._k = torch.empty(self.desc.bytes, dtype=torch.uint8, device="cuda")
+        self._v = torch.empty(self.desc.bytes, dtype=torch.uint8, device="cuda")
         self._ws = {}
-        self._grown = []                 # outgrown workspaces: work in flight may still use them
+        self._grown = []                 # workspaces that work in flight may still use after their call
         # what every call needs, in the form that costs a call least
         self._desc_ref = ctypes.byref(self.desc)
-        self._dev = self.k.device.index
-        self._kp, self._vp = self.k.data_ptr(), self.v.data_ptr()
+        self._dev = self._k.device.index
+        self._kp, self._vp = self._k.data_ptr(), self._v.data_ptr()
         self._head = (self.desc.n_kv_heads, self.desc.head_dim)
         self._q_head = (cfg.n_heads, self.desc.head_dim)
         self._torch = torch
@@ -701,6 +701,14 @@ class KV4Cache:
         # (torch.cuda.current_stream() builds a Stream object, 2.7 us; its handle alone takes 0.1)
         self._raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream",
                                    lambda dev: torch.cuda.current_stream(dev).cuda_stream)
+
+    @property
+    def k(self):
+        return self._k
+
+    @property
+    def v(self):
+        return self._v
 
     def _refuse(self, t, shape, what, dtypes):
         """The reason why a tensor does not fit."""
@@ -734,13 +742,23 @@ class KV4Cache:
     def _slots(self, slot_start, B):
         if len(slot_start) != B:
             raise ValueError(f"{len(slot_start)} slots for {B} sequences")
-        return (ctypes.c_int32 * B)(*[int(s) for s in slot_start])
+        return (ctypes.c_int32 * B)(*[self._i32(s, "slot") for s in slot_start])
+
+    @staticmethod
+    def _i32(x, what):
+        """An integer that ctypes would cut to 32 bits without a word."""
+        x = int(x)
+        if not -2 ** 31 <= x < 2 ** 31:
+            raise ValueError(f"{what} {x}")
+        return x
 
     def _attend(self, call, size, stream):
         """Runs call(workspace address, bytes) on the stream's workspace; one that is too small is replaced."""
         if self._torch.cuda.is_current_stream_capturing():
             n = size()
             ws = self._torch.empty(n, dtype=self._torch.uint8, device=self.k.device)
+            if stream != self._raw_stream(self._dev):        # (a fork of the capture: not for later calls to take)
+                self._grown.append(ws)
             check(call(ws.data_ptr(), n))
             return
         ws = self._ws.get(stream)
@@ -791,7 +809,7 @@ class KV4Cache:
                     not attn_mask.is_contiguous():
                 self._refuse(attn_mask, mshape, "attn_mask", (f32,))
             mp = attn_mask.data_ptr()
-        st = self._on(stream)
+        max_ctx, st = self._i32(max_ctx, "max_ctx"), self._on(stream)
         self._attend(lambda ws, n: _lib.kv4_attn_decode(self._desc_ref, qp, cp, max_ctx, mp, B, self.n_heads, self._kp,
                                                         self._vp, op, ws, n, st),
                      lambda: kv4_attn_workspace_size(self.desc, self.n_heads, STAGE_DECODE, B, 1, max_ctx), st)
@@ -803,7 +821,7 @@ class KV4Cache:
         qp, op = self._tensor(q, shape, "q"), self._tensor(out, shape, "out")
         if not 0 <= row < self.desc.batch:
             raise ValueError(f"row {row} of a cache of {self.desc.batch} sequences")
-        off, st = row * self.desc.stride_b, self._on(stream)
+        hist_len, off, st = self._i32(hist_len, "hist_len"), row * self.desc.stride_b, self._on(stream)
         self._attend(lambda ws, n: _lib.kv4_attn_prefill(self._desc_ref, qp, T, hist_len, self.n_heads, self._kp + off,
                                                          self._vp + off, op, ws, n, st),
                      lambda: kv4_attn_workspace_size(self.desc, self.n_heads, STAGE_PREFILL_KV, 1, T, hist_len), st)

@@ -1392,13 +1392,15 @@ static bool aligned16(std::initializer_list<const void*> ps) {
     return true;
 }
 
+constexpr int kKv4MaxSeq = 1 << 27;      // (rows of queries, 8 a token, fit 31 bits)
+
 static int check_kv4(const kv4_desc* d, int32_t B) {
     if (d->batch < 1 || d->n_kv_heads < 1 || d->max_seq < 1) return fail(W4_EINVAL, "bad kv4_desc");
-    if (d->max_seq > 1 << 27) return fail(W4_EUNSUPPORTED, "max_seq must be at most 2^27");   // (rows of queries fit 31 bits)
+    if (d->max_seq > kKv4MaxSeq) return fail(W4_EUNSUPPORTED, "max_seq must be at most 2^27");
     if (d->head_dim != 64 && d->head_dim != 128) return fail(W4_EUNSUPPORTED, "head_dim must be 64 or 128");
     const int64_t tiles = ((int64_t)d->max_seq + KV4_TILE - 1) / KV4_TILE;
     if (d->stride_h % 16 || d->stride_b % 16 || d->stride_h < tiles * kv4_tile_bytes(d->head_dim) ||
-        d->stride_b < d->stride_h * d->n_kv_heads)
+        d->stride_b / d->n_kv_heads < d->stride_h)
         return fail(W4_EINVAL, "bad kv4_desc strides");
     if (B < 1) return fail(W4_EINVAL, "B must be >= 1");
     if (B > d->batch || B > 65535 || d->n_kv_heads > 65535) return fail(W4_ECAPACITY, "B = %d exceeds the cache batch", B);
@@ -1417,6 +1419,7 @@ static int kv4_store(const kv4_desc* d, const void* kc, const void* vc, const vo
         if (slot_start[b] < 0 || (long long)slot_start[b] + T > d->max_seq)
             return fail(W4_ECAPACITY, "slots %d..%lld of sequence %d outside max_seq %d", slot_start[b],
                         (long long)slot_start[b] + T - 1, b, d->max_seq);
+    if (read ? kx == vx : kc == vc) return fail(W4_EINVAL, "K and V must not alias");
     Kv4StoreArgs a{};
     a.stride_b = d->stride_b;
     a.stride_h = d->stride_h;
@@ -1445,6 +1448,7 @@ int kv4_layout(const layer_config* cfg, int32_t batch, kv4_desc* out) {
     if (batch < 1) return fail(W4_EINVAL, "batch must be >= 1");
     if (cfg->n_kv_heads <= 0 || cfg->max_seq <= 0) return fail(W4_EINVAL, "bad config");
     if (cfg->head_dim != 64 && cfg->head_dim != 128) return fail(W4_EUNSUPPORTED, "head_dim must be 64 or 128");
+    if (cfg->max_seq > kKv4MaxSeq) return fail(W4_EUNSUPPORTED, "max_seq must be at most 2^27");
     out->batch = batch;
     out->n_kv_heads = cfg->n_kv_heads;
     out->max_seq = cfg->max_seq;
@@ -1471,6 +1475,7 @@ int kv4_append_step(const kv4_desc* d, void* kc, void* vc, const void* k_new, co
     int rc;
     if ((rc = check_kv4(d, B))) return rc;
     if (!aligned16({kc, vc, k_new, v_new})) return fail(W4_EINVAL, "pointers must be 16-byte aligned");
+    if (kc == vc) return fail(W4_EINVAL, "K and V must not alias");
     Kv4StoreArgs a{};
     a.k = (uint8_t*)kc;
     a.v = (uint8_t*)vc;
@@ -1720,6 +1725,8 @@ int layer_set_decode_path(layer_t L, int32_t path) {
 int layer_set_kv_format(layer_t L, int32_t format) {
     if (!L) return fail(W4_EINVAL, "null layer");
     if (format != W4_KV_BF16 && format != W4_KV_INT4) return fail(W4_EINVAL, "unknown cache format %d", format);
+    if (format == W4_KV_INT4 && L->cfg.max_seq > kKv4MaxSeq)
+        return fail(W4_EUNSUPPORTED, "max_seq must be at most 2^27 for a 4-bit cache");
     L->kv_format = format;
     return W4_OK;
 }

@@ -699,3 +699,46 @@ def test_prefill_many_captured_on_another_stream():
         c.attn_prefill(q, n - T, ref)
         torch.cuda.synchronize()
         assert torch.equal(out, ref)
+
+
+def test_class_refuses_integers_beyond_32_bits():
+    c, _, _, rng = filled(8, 2, 128, 2, 50, seed=34)
+    k = dev(bf16_values(rng, (2, 3, 2, 128)))
+    q = dev(bf16_values(rng, (2, 8, 128)))
+    ctx = torch.tensor([4, 5], dtype=torch.int32, device="cuda")
+    for call in (lambda: c.append(k, k, [0, 2 ** 32]), lambda: c.read([2 ** 32, 0], 3, torch.empty_like(k), torch.empty_like(k)),
+                 lambda: c.attn_decode(q, ctx, 2 ** 32 + 5, torch.empty_like(q)),
+                 lambda: c.attn_prefill(q, 2 ** 32 + 4, torch.empty_like(q))):
+        with pytest.raises(ValueError):
+            call()
+    with pytest.raises(AttributeError):
+        c.k = c.v
+
+
+def test_captured_on_forks():
+    """Two calls on two streams of one capture, a third behind them, each with a workspace: replays equal the eager calls."""
+    nq, nkv, d, n = 8, 2, 128, 3000
+    c, _, _, rng = filled(nq, nkv, d, 2, n, seed=35)
+    qs = [dev(bf16_values(rng, (2, nq, d))) for _ in range(3)]
+    outs, refs = ([torch.zeros_like(qs[0]) for _ in range(3)] for _ in range(2))
+    ctx = torch.tensor([n - 1, 1700], dtype=torch.int32, device="cuda")
+    for q, ref in zip(qs, refs):
+        c.attn_decode(q, ctx, n - 1, ref)
+    side = torch.cuda.Stream()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        main = torch.cuda.current_stream()
+        side.wait_stream(main)
+        c.attn_decode(qs[0], ctx, n - 1, outs[0], stream=side)
+        c.attn_decode(qs[1], ctx, n - 1, outs[1])
+        c.attn_decode(qs[2], ctx, n - 1, outs[2])
+        main.wait_stream(side)
+    for _ in range(4):
+        for q in qs:
+            q.copy_(dev(bf16_values(rng, (2, nq, d))))
+        g.replay()
+        for q, ref in zip(qs, refs):
+            c.attn_decode(q, ctx, n - 1, ref)
+        torch.cuda.synchronize()
+        for out, ref in zip(outs, refs):
+            assert torch.equal(out, ref)

@@ -135,3 +135,19 @@ def test_longest_cache():
         assert B.kv4_append(d, P, P, P, P, 1, 2, [n - 1], stream=0) == rc
         assert B.kv4_attn_prefill(d, P, 5, n, 32, P, P, 2 * P, P, 1 << 40, stream=0) == rc
         assert (B.kv4_attn_workspace_size(d, 32, 1, 1, 2 ** 31 - 1, 2 ** 31 - 1) > 0) == (rc == B.W4_ECAPACITY)
+    cfg = synth.replace(CFG, max_seq=2 ** 27)
+    assert B.kv4_layout(cfg, 1)[0] == 0
+    assert B.kv4_layout(synth.replace(cfg, max_seq=2 ** 27 + 1), 1)[0] == B.W4_EUNSUPPORTED
+
+
+def test_keys_and_values_apart():
+    """Caches that are written, and outputs, may not be one; sources may."""
+    d = desc()
+    assert B.kv4_append(d, P, P, P, 2 * P, 1, 2, [0], stream=0) == B.W4_EINVAL and "alias" in B.layer_last_error()
+    assert B.kv4_append_step(d, P, P, P, 2 * P, 1, P, stream=0) == B.W4_EINVAL and "alias" in B.layer_last_error()
+    assert B.kv4_read(d, P, 2 * P, 1, 2, [0], P, P, stream=0) == B.W4_EINVAL and "alias" in B.layer_last_error()
+
+
+def test_strides_that_overflow():
+    assert B.kv4_append(desc(stride_h=2 ** 62, stride_b=2 ** 62), P, P, P, P, 1, 2, [0], stream=0) == B.W4_EINVAL
+    assert "strides" in B.layer_last_error()
