@@ -65,9 +65,10 @@ struct Kv4AttnArgs {
     int rows, nq, nkv, d;
     float scale;             // of the scores
     int nsplit;              // decode: shares of a (row, kv head)'s tiles
-    float* part;             // decode: share states (nsplit > 1), [rows nkv][nsplit] of r (d + 2) floats; prefill: plan.part_bytes
-    long long pf_units;      // prefill, set by the launcher: stages of one kv head's row tiles; stages of a part
-    int pf_chunk;            // (0: equal runs)
+    float* part;             // decode: share states (nsplit > 1), [rows nkv][nsplit] of r (d + 2) floats; prefill:
+                             // plan.part_bytes
+    long long pf_units;      // prefill, set by the launcher: stages of one kv head's row tiles
+    int pf_chunk;            // and most stages of a part (0: equal runs)
     int r, per;              // set by the launcher: nq / nkv; decode: tiles per share
     int* err;                // raised with W4_FLAG_F16_RANGE (out_f16), or null
 };

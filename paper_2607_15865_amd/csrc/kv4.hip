@@ -9,6 +9,10 @@
 // 11 us of 47).  V, whose words span 8 tokens: the eight lanes of a token block
 // transpose their 8x8 nibbles, one word of dims each for one word of tokens, in
 // three exchanges; a run that ends inside a block replaces its nibbles alone.
+//
+// Measured, 2 sequences of 16384 tokens, 8 heads of 128 (134 MB of bf16, 42 of cache): append 39 us in a row of
+// appends, 35 without the codes' arithmetic (of about 15 operations a value), and 47 in turn with reads; read 38 and 31.
+// One token of two heads of 64: 4.3 and 2.8, a kernel's start, chain of loads, exchanges and stores, and end.
 #include <type_traits>
 
 #include "kv4.h"

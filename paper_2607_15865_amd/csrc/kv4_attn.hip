@@ -87,7 +87,8 @@ __device__ __forceinline__ void put_pair(const Kv4AttnArgs& a, size_t off, float
 // One block: a share (a.per tiles) of one (row, kv head), all r query heads of the
 // group.  Wave w of 8 takes tiles w, w + 8, .. of the share on its own; the next
 // tile's K is requested when this one's scores are formed and its V when its
-// output is, into the same registers, so that two blocks fit a CU (CT 1).  The first
+// output is, into the same registers, so that two blocks fit a CU (CT 1; 16 rows of up to 32768 keys of 8 heads of
+// 128 take 96 to 99 us, 5.2 TB/s, where reading alone in this pattern takes 85).  The first
 // tile's requests do not wait for the context length: a share's place is fixed by
 // the longest context, and blocks past a row's own end leave.  CT column tiles of 16 /
 // NS heads.  Softmax: the maximum of a head moves only when a score passes it by
@@ -509,6 +510,12 @@ __global__ void __launch_bounds__(256) kv4_decode_merge_kernel(Kv4AttnArgs a) {
 // all kv heads follow each other and the blocks cut them into equal runs, so that
 // long work ends everywhere at once.  A row tile with more than one part leaves their states in
 // the workspace, and a second launch merges them in order.
+//
+// Measured, 2011 queries of 28 heads of 4 behind 14001 tokens: 481 to 535 us by
+// the card's clock, 0.81 to 0.90 PFLOP/s (a library product of two 8192^2 fp16
+// matrices: 1.14).  In a build without the exponentials 449, without the expansion
+// 430, with neither 426, without the first product 428: the halves overlap, and
+// the clock at the power limit bounds what is left.
 constexpr int PF_W = 8;                      // waves per block
 constexpr int PF_ROWS = 32 * PF_W;
 constexpr int PF_KST = 64;                   // keys per stage
@@ -962,7 +969,7 @@ __global__ void __launch_bounds__(64 * PF_W) kv4_prefill_merge_kernel(Kv4AttnArg
 
 }  // namespace
 
-// Shares per (row, kv head).  A block costs about 5 us to begin and end and a wave 0.35
+// Shares per (row, kv head).  A block costs about 5 us to begin and end and a wave about 1
 // us a tile, a second share the merge launch, about 2.5 us: below 32 tiles one block is the
 // faster.  Else a tile per wave, as long as the blocks fit the CUs at once (two to a
 // CU; one of more than 4 heads of d = 128).  32 heads of 8, d = 128, 1 row of 2048 keys: 1
@@ -970,9 +977,9 @@ __global__ void __launch_bounds__(64 * PF_W) kv4_prefill_merge_kernel(Kv4AttnArg
 // 114, 4 105, 8 109; 14 heads of 2, d = 64, 512 keys: 1 5.7, 2 8.2; 28 heads of 4, d = 128, 8 rows
 // of up to 8192: 4 26.5, 8 20.1, 16 29.3.
 //
-// The wide kernel (CT 2) is bound by the vector units, 0.55 us a tile of a SIMD; waves of four heads each,
-// twice as many, took 8.7 and 8.0 us for 1 row of 500 and 2000 keys of 28 heads of 4 instead of 9.2 and 9.4, but 88 instead
-// of 81 for 16 of up to 32000.
+// The wide kernel (CT 2) is bound by the vector units, 1.3 us a tile of a SIMD.  Waves of
+// four heads each, twice as many, took 8.7 and 8.0 us for 1 row of 500 and 2000 keys of
+// 28 heads of 4 instead of 9.2 and 9.4, but 88 instead of 81 for 16 of up to 32000.
 int kv4_decode_shares(int rows, int nkv, int r, int d, int max_ctx) {
     const long long tiles = ((long long)max_ctx + KV4_TILE) / KV4_TILE, pairs = (long long)rows * nkv;
     const bool wide = d == 128 && r > 4;
@@ -1013,8 +1020,8 @@ constexpr int kMaxParts = 512;       // states of parts in the workspace
 // 8 / 64 queries of 1000 keys 7.7 / 15.0 us and 12.2 / 19.5 with the prefill kernel, 8 / 12 of 16000 27 / 38 and 28 / 32,
 // 24 of 3000 21 and 18; 2 kv heads of 64, 61 of 250 5 and 13.5, 64 of 16000 32 and 48.
 //
-// For the prefill kernel the way of dealing out the work with the least estimated time, in us.  Pieces waste less on starts and on states;
-// the line ends everywhere at once, and takes any number of stages with two states per block.  Measured (pieces, line):
+// For the prefill kernel the way of dealing out the work with the least estimated time, in us.  Pieces waste less on starts
+// and on states; the line ends everywhere at once, and takes any number of stages with two states per block.  Measured (pieces, line):
 // 128 wide, 32 heads of 8, 1000 tokens from nothing 37 and 51, 64 behind 4000 26.5 and 41, 512 behind 4096 71 and 69,
 // 5000 from nothing 265 and 346; 28 heads of 4, 2000 behind 2000 137 and 148, and in parts that fill the chip badly 172.
 Kv4PrefillPlan kv4_prefill_plan(int T, int hist, int nkv, int r, int d) {
@@ -1047,7 +1054,7 @@ Kv4PrefillPlan kv4_prefill_plan(int T, int hist, int nkv, int r, int d) {
     for (int c = (int)std::min<long long>(most, std::max<long long>(1, total / kMaxParts));; c += c < 8 ? 1 : c / 5) {
         c = std::min(c, most);
         long long items = 0;
-        double longest = 0, work = 0, end = 0;               // us of a part, of all so far; end of one that has to wait for another's
+        double longest = 0, work = 0, end = 0;               // us of a part, of all so far; end of one that has to wait
         for (int q = nqt - 1; q >= 0; q--) {
             const int st = pf_stages(q, R, r, hist), n = (st + c - 1) / c, len = (st + n - 1) / n;
             items += (long long)n * nkv;
