@@ -688,19 +688,23 @@ class KV4Cache:
         self.n_heads = cfg.n_heads
         self._k = torch.empty(self.desc.bytes, dtype=torch.uint8, device="cuda")
         self._v = torch.empty(self.desc.bytes, dtype=torch.uint8, device="cuda")
-        self._ws = {}
-        self._grown = []                 # workspaces that work in flight may still use after their call
+        self._ws = {}                    # stream: address and bytes
+        self._kept = []                  # workspaces' tensors
         # what every call needs, in the form that costs a call least
         self._desc_ref = ctypes.byref(self.desc)
         self._dev = self._k.device.index
         self._kp, self._vp = self._k.data_ptr(), self._v.data_ptr()
+        self._no_ws = (self._kp, 0)
+        self._slot_arrays = {}
         self._head = (self.desc.n_kv_heads, self.desc.head_dim)
         self._q_head = (cfg.n_heads, self.desc.head_dim)
         self._torch = torch
         self._bits16 = (torch.bfloat16, torch.int16, torch.uint16)
+        self._capturing = torch.cuda.is_current_stream_capturing
         # (torch.cuda.current_stream() builds a Stream object, 2.7 us; its handle alone takes 0.1)
         self._raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream",
                                    lambda dev: torch.cuda.current_stream(dev).cuda_stream)
+        self._current_device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
 
     @property
     def k(self):
@@ -733,16 +737,11 @@ class KV4Cache:
 
     def _on(self, stream):
         """The stream's handle; the cache's device has to be the current one."""
-        if self._torch.cuda.current_device() != self._dev:
-            raise ValueError(f"the cache is on {self.k.device}, the current device is {self._torch.cuda.current_device()}")
+        if self._current_device() != self._dev:
+            raise ValueError(f"the cache is on {self.k.device}, the current device is {self._current_device()}")
         if stream is None:
             return self._raw_stream(self._dev)
         return stream if isinstance(stream, int) else stream.cuda_stream
-
-    def _slots(self, slot_start, B):
-        if len(slot_start) != B:
-            raise ValueError(f"{len(slot_start)} slots for {B} sequences")
-        return (ctypes.c_int32 * B)(*[self._i32(s, "slot") for s in slot_start])
 
     @staticmethod
     def _i32(x, what):
@@ -752,26 +751,32 @@ class KV4Cache:
             raise ValueError(f"{what} {x}")
         return x
 
-    def _attend(self, call, size, stream):
-        """Runs call(workspace address, bytes) on the stream's workspace; one that is too small is replaced."""
-        if self._torch.cuda.is_current_stream_capturing():
-            n = size()
-            ws = self._torch.empty(n, dtype=self._torch.uint8, device=self.k.device)
-            if stream != self._raw_stream(self._dev):        # (a fork of the capture: not for later calls to take)
-                self._grown.append(ws)
-            check(call(ws.data_ptr(), n))
-            return
-        ws = self._ws.get(stream)
-        rc = W4_EWORKSPACE if ws is None else call(ws.data_ptr(), ws.numel())
+    def _slots(self, slot_start, B):
+        if len(slot_start) != B:
+            raise ValueError(f"{len(slot_start)} slots for {B} sequences")
+        kind = self._slot_arrays.get(B)
+        if kind is None:
+            kind = self._slot_arrays[B] = ctypes.c_int32 * B
+        s = [int(x) for x in slot_start]
+        if s and not (-2 ** 31 <= min(s) and max(s) < 2 ** 31):        # (ctypes would cut them to 32 bits without a word)
+            raise ValueError(f"slots {s}")
+        return kind(*s)
+
+    def _attend(self, fn, args, stage, B, T, ctx, stream):
+        """Calls fn(*args, workspace, its bytes, stream): the stream's, replaced if it is too small."""
+        capturing = self._capturing()
+        ws = self._no_ws if capturing else self._ws.get(stream, self._no_ws)
+        rc = fn(*args, ws[0], ws[1], stream)                 # (without a workspace: refuses the arguments, or asks for one)
         if rc == W4_EWORKSPACE:
-            n = size()
-            if n == 0:
-                raise W4Error(W4_EINVAL, layer_last_error())
-            if ws is not None:
-                self._grown.append(ws)
-                n = max(n, 2 * ws.numel())
-            ws = self._ws[stream] = self._torch.empty(n, dtype=self._torch.uint8, device=self.k.device)
-            rc = call(ws.data_ptr(), n)
+            n = max(kv4_attn_workspace_size(self.desc, self.n_heads, stage, B, T, ctx), 0 if capturing else 2 * ws[1])
+            new = self._torch.empty(n, dtype=self._torch.uint8, device=self._k.device)
+            if capturing:
+                if stream != self._raw_stream(self._dev):    # (a fork of the capture: not for later calls to take)
+                    self._kept.append(new)
+            else:
+                self._kept.append(new)                       # (work in flight may still use the one before)
+                self._ws[stream] = (new.data_ptr(), n)
+            rc = fn(*args, new.data_ptr(), n, stream)
         check(rc)
 
     def append(self, k_new, v_new, slot_start, stream=None):
@@ -810,9 +815,8 @@ class KV4Cache:
                 self._refuse(attn_mask, mshape, "attn_mask", (f32,))
             mp = attn_mask.data_ptr()
         max_ctx, st = self._i32(max_ctx, "max_ctx"), self._on(stream)
-        self._attend(lambda ws, n: _lib.kv4_attn_decode(self._desc_ref, qp, cp, max_ctx, mp, B, self.n_heads, self._kp,
-                                                        self._vp, op, ws, n, st),
-                     lambda: kv4_attn_workspace_size(self.desc, self.n_heads, STAGE_DECODE, B, 1, max_ctx), st)
+        self._attend(_lib.kv4_attn_decode, (self._desc_ref, qp, cp, max_ctx, mp, B, self.n_heads, self._kp, self._vp, op),
+                     STAGE_DECODE, B, 1, max_ctx, st)
 
     def attn_prefill(self, q, hist_len, out, row: int = 0, stream=None):
         """T queries of sequence `row` after hist_len tokens: q, out [T][n_heads][head_dim]."""
@@ -822,6 +826,5 @@ class KV4Cache:
         if not 0 <= row < self.desc.batch:
             raise ValueError(f"row {row} of a cache of {self.desc.batch} sequences")
         hist_len, off, st = self._i32(hist_len, "hist_len"), row * self.desc.stride_b, self._on(stream)
-        self._attend(lambda ws, n: _lib.kv4_attn_prefill(self._desc_ref, qp, T, hist_len, self.n_heads, self._kp + off,
-                                                         self._vp + off, op, ws, n, st),
-                     lambda: kv4_attn_workspace_size(self.desc, self.n_heads, STAGE_PREFILL_KV, 1, T, hist_len), st)
+        self._attend(_lib.kv4_attn_prefill, (self._desc_ref, qp, T, hist_len, self.n_heads, self._kp + off, self._vp + off, op),
+                     STAGE_PREFILL_KV, 1, T, hist_len, st)
