@@ -979,7 +979,9 @@ __global__ void __launch_bounds__(64 * PF_W) kv4_prefill_merge_kernel(Kv4AttnArg
 //
 // The wide kernel (CT 2) is bound by the vector units, 1.3 us a tile of a SIMD.  Waves of
 // four heads each, twice as many, took 8.7 and 8.0 us for 1 row of 500 and 2000 keys of
-// 28 heads of 4 instead of 9.2 and 9.4, but 88 instead of 81 for 16 of up to 32000.
+// 28 heads of 4 instead of 9.2 and 9.4, but 88 instead of 81 for 16 of up to 32000; three blocks
+// of four waves to a CU (the queries in shared memory, 168 registers) 79, but 20.9 for 8 of up to 8192 instead
+// of 18.4 and 27 for 1 of 30000 instead of 17: more shares to merge.
 int kv4_decode_shares(int rows, int nkv, int r, int d, int max_ctx) {
     const long long tiles = ((long long)max_ctx + KV4_TILE) / KV4_TILE, pairs = (long long)rows * nkv;
     const bool wide = d == 128 && r > 4;
