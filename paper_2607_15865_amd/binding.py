@@ -678,8 +678,9 @@ class KV4Cache:
     Keys, values, queries and outputs are contiguous bf16 tensors (or 16-bit
     integers holding the bits) on the cache's device, which must be the current
     one.  Calls run on ``stream`` (default: torch's current stream).  A call's
-    workspace is kept per stream; under graph capture it is allocated in the
-    capture, so that every graph has its own.  The caches k and v stay the same tensors."""
+    workspace is allocated on that stream and kept per stream; under graph capture
+    (torch.cuda.graph) it is allocated in the capture, so that every graph, and
+    every branch of one, has its own.  The caches k and v stay the same tensors."""
 
     def __init__(self, cfg, batch: int):
         import torch
@@ -688,8 +689,7 @@ class KV4Cache:
         self.n_heads = cfg.n_heads
         self._k = torch.empty(self.desc.bytes, dtype=torch.uint8, device="cuda")
         self._v = torch.empty(self.desc.bytes, dtype=torch.uint8, device="cuda")
-        self._ws = {}                    # stream: address and bytes
-        self._kept = []                  # workspaces' tensors
+        self._ws = {}                    # stream: address, bytes and tensor
         # what every call needs, in the form that costs a call least
         self._desc_ref = ctypes.byref(self.desc)
         self._dev = self._k.device.index
@@ -762,20 +762,29 @@ class KV4Cache:
             raise ValueError(f"slots {s}")
         return kind(*s)
 
+    def _stream_context(self, stream):
+        """Makes the stream torch's current one (ExternalStream has no form for the default stream)."""
+        cuda = self._torch.cuda
+        return cuda.stream(cuda.ExternalStream(stream, self._dev) if stream > 1 else cuda.default_stream(self._dev))
+
     def _attend(self, fn, args, stage, B, T, ctx, stream):
-        """Calls fn(*args, workspace, its bytes, stream): the stream's, replaced if it is too small."""
+        """Calls fn(*args, workspace, its bytes, stream).  The workspace is allocated with `stream` as torch's current one:
+        what the allocator hands out for a stream has no work of others pending on it, and freed, it goes to that stream's
+        later work alone (or, in a capture, the graph's)."""
         capturing = self._capturing()
+        if stream != self._raw_stream(self._dev):
+            with self._stream_context(stream):
+                return self._attend_here(fn, args, stage, B, T, ctx, stream, capturing)
+        return self._attend_here(fn, args, stage, B, T, ctx, stream, capturing)
+
+    def _attend_here(self, fn, args, stage, B, T, ctx, stream, capturing):
         ws = self._no_ws if capturing else self._ws.get(stream, self._no_ws)
         rc = fn(*args, ws[0], ws[1], stream)                 # (without a workspace: refuses the arguments, or asks for one)
         if rc == W4_EWORKSPACE:
             n = max(kv4_attn_workspace_size(self.desc, self.n_heads, stage, B, T, ctx), 0 if capturing else 2 * ws[1])
             new = self._torch.empty(n, dtype=self._torch.uint8, device=self._k.device)
-            if capturing:
-                if stream != self._raw_stream(self._dev):    # (a fork of the capture: not for later calls to take)
-                    self._kept.append(new)
-            else:
-                self._kept.append(new)                       # (work in flight may still use the one before)
-                self._ws[stream] = (new.data_ptr(), n)
+            if not capturing:
+                self._ws[stream] = (new.data_ptr(), n, new)
             rc = fn(*args, new.data_ptr(), n, stream)
         check(rc)
 
