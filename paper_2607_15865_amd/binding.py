@@ -678,9 +678,9 @@ class KV4Cache:
     Keys, values, queries and outputs are contiguous bf16 tensors (or 16-bit
     integers holding the bits) on the cache's device, which must be the current
     one.  Calls run on ``stream`` (default: torch's current stream).  A call's
-    workspace is allocated on that stream and kept per stream; under graph capture
-    (torch.cuda.graph) it is allocated in the capture, so that every graph, and
-    every branch of one, has its own.  The caches k and v stay the same tensors."""
+    workspace is allocated on that stream and kept per stream; where that stream is
+    being captured (torch.cuda.graph), it is allocated in the capture, so that
+    every graph, and every branch of one, has its own.  The caches k and v stay the same tensors."""
 
     def __init__(self, cfg, batch: int):
         import torch
@@ -771,13 +771,13 @@ class KV4Cache:
         """Calls fn(*args, workspace, its bytes, stream).  The workspace is allocated with `stream` as torch's current one:
         what the allocator hands out for a stream has no work of others pending on it, and freed, it goes to that stream's
         later work alone (or, in a capture, the graph's)."""
-        capturing = self._capturing()
         if stream != self._raw_stream(self._dev):
             with self._stream_context(stream):
-                return self._attend_here(fn, args, stage, B, T, ctx, stream, capturing)
-        return self._attend_here(fn, args, stage, B, T, ctx, stream, capturing)
+                return self._attend_here(fn, args, stage, B, T, ctx, stream)
+        return self._attend_here(fn, args, stage, B, T, ctx, stream)
 
-    def _attend_here(self, fn, args, stage, B, T, ctx, stream, capturing):
+    def _attend_here(self, fn, args, stage, B, T, ctx, stream):
+        capturing = self._capturing()
         ws = self._no_ws if capturing else self._ws.get(stream, self._no_ws)
         rc = fn(*args, ws[0], ws[1], stream)                 # (without a workspace: refuses the arguments, or asks for one)
         if rc == W4_EWORKSPACE:

@@ -134,3 +134,30 @@ def test_one_cache_on_several_streams_at_once():
         for got, ref in zip(outs, refs):
             assert all(torch.equal(a, b) for a, b in zip(got, ref))
     assert np.isfinite(refs[0][0].float().cpu().numpy()).all()
+
+
+def test_captured_stream_that_is_not_current():
+    """A call on the captured stream while another one is current: the graph has a workspace of its own, replayed while
+    eager calls on the same stream use theirs."""
+    c, g = filled(5)
+    ctx, side = i32(N - 1, 1500), torch.cuda.Stream()
+    qs = [rand(g, (2, NQ, D)) for _ in range(2)]
+    outs, refs = ([torch.zeros_like(q) for q in qs] for _ in range(2))
+    torch.cuda.synchronize()
+    c.attn_decode(qs[0], ctx, N - 1, refs[0], stream=side)
+    torch.cuda.synchronize()
+    graph, idle = torch.cuda.CUDAGraph(), torch.cuda.Stream()
+    with torch.cuda.graph(graph, stream=side):
+        with torch.cuda.stream(idle):
+            c.attn_decode(qs[0], ctx, N - 1, outs[0], stream=side)
+    for r in range(5):
+        for q in qs:
+            q.copy_(rand(g, q.shape))
+        torch.cuda.synchronize()
+        graph.replay()                                       # (on the default stream, beside the eager call on side)
+        c.attn_decode(qs[1], ctx, N - 1, outs[1], stream=side)
+        torch.cuda.synchronize()
+        for q, ref in zip(qs, refs):
+            c.attn_decode(q, ctx, N - 1, ref)
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(outs, refs)), r

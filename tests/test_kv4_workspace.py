@@ -172,3 +172,19 @@ def test_nothing_is_kept_of_captured_calls(fake):
             decode(c, SIDE)
     assert len({ws for ws, _ in fake.calls}) == 2
     assert sum(len(torch.free[s]) for s in (MAIN, SIDE)) == 2
+
+
+def test_capture_of_a_stream_that_is_not_current(fake):
+    """The state that counts is that of the stream which the call runs on, whatever the current one does: a captured call
+    does not take the workspace of the stream's eager calls, and an eager call beside a capture not one of the capture's."""
+    torch, c = fake.torch, fake.cache
+    decode(c, SIDE)
+    eager = fake.calls[0][0]
+    torch.captured.add(SIDE)
+    decode(c, SIDE)
+    prefill(c, SIDE)
+    assert all(ws != eager and torch.blocks[ws] == SIDE for ws, _ in fake.calls[1:])
+    torch.captured = {MAIN}
+    with torch.use(Stream(MAIN)):
+        decode(c, SIDE)
+    assert fake.calls[3] == (eager, SIDE)
