@@ -87,6 +87,76 @@ def attend(q, k, v, seen, add=None, key_eps: float = 0.0):
     return out, tol
 
 
+def fp16_operands(x):
+    """Values held, as the prefill kernel multiplies them: lo + s c rounded once to fp16 (still fp64)."""
+    return np.asarray(x, dtype=F64).astype(np.float16).astype(F64)
+
+
+def attend_heads(q, k, v, first, kparts=None, vparts=None, w_eps=2.0 ** -11, drop=None):
+    """Causal attention of all queries, head by head: q [T][nq][d], k, v [nkv][n][d] torch fp64 tensors, the very
+    operands that a computation multiplies (fp16_operands for the prefill kernel); query t sees keys 0 .. first + t.
+    kparts, vparts: where a key or value is multiplied in parts (scale times code, offset), the sum of the parts'
+    magnitudes; w_eps: the rounding of a weight; drop(t0, t1) for a planted mistake: [t1 - t0][n] bool, keys left out.
+    Yields (head, out [T][d], tol [T][d]); tol bounds the error of fp32 sums of exact products, before the result is
+    rounded:
+
+      A score's d products are exact in fp32 and summed there; with an addition off by at most 2^-23, in whatever
+      order, and a few operations on the sum, the argument of the exponential is off by at most
+          e = (d + 16) 2^-23 max_j (|q| . |k_j|) / sqrt(d) + 2^-21 max_j |z_j|.
+      Scores off by at most e either way change the weight w_j by a factor 1 + f, |f| <= (1 - w_j) expm1(2 e): with
+      every other score moved against it w' / w = 1 / (w + (1 - w) exp(-+2 e)), for which that holds.
+      Rounded to 2^-11 (w_eps), or, in fp16's subnormals, by at most 2^-25 of the largest weight's unit, and never by
+      more than itself.  n additions to the output and to the weights' sum in fp32, of which a matrix instruction does
+      16 and more at a time: (n / 2 + 96) 2^-24.  2^-20: the exponential, the final division, the joining of parts."""
+    import torch
+    T, nq, d = q.shape
+    nkv, n, _ = k.shape
+    r = nq // nkv
+    kparts = k.abs() if kparts is None else kparts
+    vparts = v.abs() if vparts is None else vparts
+    seen = torch.arange(n, device=q.device)[None] <= torch.arange(T, device=q.device)[:, None] + first
+    if drop is not None:
+        seen = seen & ~drop
+    scale = float(d) ** -0.5
+    for h in range(nq):
+        qh, kh = q[:, h].contiguous(), k[h // r].t().contiguous()
+        z = (qh @ kh) * scale
+        z = torch.where(seen, z, -torch.inf)
+        zmax = z.amax(-1, keepdim=True)
+        mag = (qh.abs() @ kparts[h // r].t().contiguous()) * scale
+        e = (d + 16) * 2.0 ** -23 * torch.where(seen, mag, 0.0).amax(-1, keepdim=True)
+        e += 2.0 ** -21 * torch.where(seen, z.abs(), 0.0).amax(-1, keepdim=True)
+        p = torch.exp(z - zmax)
+        total = p.sum(-1, keepdim=True)
+        w = p / total
+        out = w @ v[h // r]
+        rel = (1 - w) * torch.expm1(2 * e.clamp(max=50)) + (w_eps + (n / 2 + 96) * 2.0 ** -24 + 2.0 ** -20)
+        tol = (w * rel) @ vparts[h // r] + (p.clamp(max=2.0 ** -25) / total) @ vparts[h // r]
+        yield h, out, tol
+
+
+def probing_queries(rng, k, nq, T, first):
+    """Queries [T][nq][d] whose outputs show every key: rows (query, head) of a kv head in order, every other one near
+    one key of a stage of 64 after another (its first, last or some key), of the rest each fourth near the last key seen,
+    the first one hidden, key 0, and nowhere in particular.  "Near" a key: six times its difference from the
+    keys' mean, which puts nearly all the weight on it.  k [nkv][n][d]."""
+    nkv, n, d = k.shape
+    r = nq // nkv
+    mean = k.mean(1)
+    q = np.empty((T, nq, d))
+    for g in range(nkv):
+        for i in range(T * r):
+            t, h = divmod(i, r)
+            last, kind = first + t, i % 8
+            if kind % 2 == 0:
+                st = (i // 2) % (last // 64 + 1)
+                j = min(last, 64 * st + (0, 63, int(rng.integers(64)))[(i // 2 + i // 512) % 3])
+            else:
+                j = {1: last, 3: min(last + 1, n - 1), 5: 0, 7: -1}[kind]
+            q[t, g * r + h] = rng.standard_normal(d) if j < 0 else 6.0 * (k[g, j] - mean[g])
+    return _layer.round_bf16(q)
+
+
 def block(w: dict, cfg, x, pos, k_hist=None, v_hist=None, bias=None, rows=None, W=None):
     """oracle.layer.block for a layer whose cache is held in 4 bits: the new
     keys and values (bf16 after RoPE, as they are formed there) enter the cache,

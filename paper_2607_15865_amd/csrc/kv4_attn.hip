@@ -1080,6 +1080,15 @@ Kv4PrefillPlan kv4_prefill_plan(int T, int hist, int nkv, int r, int d) {
     return p;
 }
 
+// (for the host tests)
+extern "C" void w4_kv4_prefill_plan(int T, int hist, int nkv, int r, int d, int* single, int* chunk, int* blocks, int* merge) {
+    const Kv4PrefillPlan p = kv4_prefill_plan(T, hist, nkv, r, d);
+    *single = p.single;
+    *chunk = p.chunk;
+    *blocks = p.blocks;
+    *merge = p.merge;
+}
+
 template <int D, bool PIECES>
 static int launch_prefill(const Kv4AttnArgs& a, const Kv4PrefillPlan& p, hipStream_t stream) {
     const size_t lds = (size_t)8 * 32 * D * 2 + 4 * (D / 32 + 1) * 8;
