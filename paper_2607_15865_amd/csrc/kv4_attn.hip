@@ -1021,6 +1021,10 @@ constexpr int kMaxParts = 512;       // states of parts in the workspace
 // reads the keys once for every query.  The two take the same time at about 2^21 tiles x dims: heads of 128, 8 kv heads,
 // 8 / 64 queries of 1000 keys 7.7 / 15.0 us and 12.2 / 19.5 with the prefill kernel, 8 / 12 of 16000 27 / 38 and 28 / 32,
 // 24 of 3000 21 and 18; 2 kv heads of 64, 61 of 250 5 and 13.5, 64 of 16000 32 and 48.
+// Up to four queries are always the decode kernel's: it reads the keys four times at most, where the prefill kernel
+// unpacks and multiplies them for 256 rows.  32 heads of 8 of 128, 131000 keys, 1 / 2 / 4 / 6 queries 33 / 51 / 80 / 123 us
+// and 114 with the prefill kernel; 28 of 4, 29 / 42 / 71 / 106 and 86 to 91 (four of 260000
+// keys 130 and 124); 8 of 8 of 64, 23 / 33 / 56 / 85 and 109.
 //
 // For the prefill kernel the way of dealing out the work with the least estimated time, in us.  Pieces waste less on starts
 // and on states; the line ends everywhere at once, and takes any number of stages with two states per block.  Measured (pieces, line):
@@ -1042,7 +1046,7 @@ Kv4PrefillPlan kv4_prefill_plan(int T, int hist, int nkv, int r, int d) {
     const long long tiles = ((long long)hist + few + KV4_TILE - 1) / KV4_TILE, pairs = (long long)few * nkv;
     p.part_bytes = std::max((size_t)std::min<long long>(kMaxParts, 2 * total) * state,
                             (size_t)std::min<long long>(2 * kCus, pairs * tiles) * r * (d + 2) * 4);
-    p.single = T == few && pairs * tiles * d <= 1 << 21;
+    p.single = T <= 4 || (T == few && pairs * tiles * d <= 1 << 21);
     if (p.single) return p;
     // a stage of one block alone and with all others (the clock falls), a part's start and end, its state written and read
     // back (of its waves that have rows), the merge launch

@@ -25,7 +25,8 @@ CASES = [
     ("parts", 56, 8, 128, 65, 1000), ("parts", 7, 1, 128, 900, 4000), ("parts", 32, 16, 128, 31, 1055),
     ("parts", 64, 64, 64, 9, 2100), ("parts", 24, 8, 64, 401, 31),
     ("whole", 48, 12, 64, 292, 0), ("whole", 33, 11, 128, 225, 0), ("whole", 64, 8, 128, 1500, 1), ("whole", 40, 8, 64, 2049, 63),
-    ("rows", 8, 2, 128, 33, 300), ("rows", 14, 2, 64, 61, 250), ("rows", 7, 1, 128, 5, 4000), ("rows", 32, 8, 128, 1, 2100)]
+    ("rows", 8, 2, 128, 33, 300), ("rows", 14, 2, 64, 61, 250), ("rows", 7, 1, 128, 5, 4000), ("rows", 32, 8, 128, 1, 2100),
+    ("rows", 16, 8, 64, 4, 70000), ("rows", 16, 8, 128, 1, 70001), ("rows", 28, 4, 128, 2, 70002)]
 BIG = [("runs", 60, 12, 128, 530, 1911), ("parts", 32, 16, 128, 120, 213), ("rows", 8, 2, 128, 70, 263)]
 
 

@@ -116,3 +116,16 @@ def test_every_stage_once_and_every_state_a_slot(seed):
         forms.add("runs" if not chunk else "parts" if merge else "whole")
     if seed == 0:
         assert forms == {"runs", "parts", "whole"}
+
+
+@pytest.mark.parametrize("nkv,r,d", [(8, 4, 128), (4, 7, 128), (2, 7, 64), (1, 8, 128), (16, 1, 64)])
+def test_up_to_four_queries_run_as_rows_of_the_decode_kernel(nkv, r, d):
+    """Whatever the context: the prefill kernel would work on 256 rows.  The workspace holds that form's states too."""
+    for hist in (0, 5000, 65000, 131000, 1000000, 2 ** 26):
+        last = 0
+        for T in range(1, 9):
+            assert plan(T, hist, nkv, r, d)[0] or T > 4, (T, hist)
+            n = workspace(T, hist, nkv, r, d)
+            tiles = (hist + T + 31) // 32
+            assert n >= max(last, min(512, T * nkv * tiles) * r * (d + 2) * 4)
+            last = n
