@@ -614,7 +614,8 @@ int layer_debug_decode_stamps(layer_t layer, uint64_t* out, int32_t n);
  * 1, prefill and prefill_kv: 0 rmsnorm, 1 qkv GEMM, 2 attention, 3 o_proj
  * GEMM, 4 rmsnorm, 5 gate/up GEMM, 6 down GEMM; stage 2, decode: 0 qkv GEMV,
  * 1 attention, 3 o_proj GEMV, 4 gate/up GEMV, 5 down GEMV,
- * 6 the whole persistent decode launch);
+ * 6 the whole persistent decode launch; with a 4-bit cache the attention's
+ * time includes the launch that puts the new keys and values into the cache);
  * kernel < 0 switches timing of that stage off.  While selected, each stage
  * call records a HIP event pair around that launch on the call's stream (at
  * most 4096 pairs per stage until the next read).  Switching timing off and

@@ -841,12 +841,12 @@ int run_decode_seq(layer_s* L, const float* x, const int32_t* pos, const int32_t
     { ProfScope ps(L, ps_stage, ps_stage == 2 ? 0 : 1, st); rc |= launch_gemv_w4(EPI_QKV, !prenorm, a1, st); }
 
     if (kv4) {
-        rc |= launch_kv4_append(kv_stage_store(L, base + w.kv, B, shared, ctx_lens, ctx_base, kc, vc), st);
         Kv4AttnArgs ka = kv4_layer_attn(L, q, kc, vc, attn, B, shared, ctx_lens, ctx_base, max_ctx);
         ka.mask = attn_mask;
         ka.nsplit = w.nsplit;
         ka.part = part;
         ProfScope ps(L, ps_stage, ps_stage == 2 ? 1 : 2, st);
+        rc |= launch_kv4_append(kv_stage_store(L, base + w.kv, B, shared, ctx_lens, ctx_base, kc, vc), st);
         rc |= launch_kv4_decode(ka, st);
     }
     AttnDecodeArgs ad{};
@@ -1012,10 +1012,10 @@ int run_prefill(layer_s* L, const float* x, const int32_t* pos, int T, int hist,
     if (kv4) kv_stage_epi(L, e, base + w.kv, T);
     { ProfScope ps(L, stage, 1, st); rc |= launch_gemm_w4(EPI_QKV, xn1, H, L->qkv.d, e, w.qkv, T, part, cnt, st); }
     if (kv4) {
-        rc |= launch_kv4_append(kv_stage_store(L, base + w.kv, T, true, nullptr, hist, kc, vc), st);
         Kv4AttnArgs ka = kv4_layer_attn(L, q, kc, vc, attn, T, true, nullptr, hist, hist + T - 1);
         ka.part = part;
         ProfScope ps(L, stage, 2, st);
+        rc |= launch_kv4_append(kv_stage_store(L, base + w.kv, T, true, nullptr, hist, kc, vc), st);
         rc |= launch_kv4_prefill(ka, st);
     }
     AttnPrefillArgs aa{};
