@@ -458,6 +458,12 @@ typedef struct kv4_desc {
  * (head_dim, max_seq). */
 int kv4_layout(const layer_config* cfg, int32_t batch, kv4_desc* out);
 
+/* Loads the code of the kv4_ kernels on the current device, so that the first
+ * calls do not (0.5 ms for an append, 0.7 for an attention call).  layer_create
+ * and lm_create do it too; without any of them the calls load it themselves.
+ * Errors: W4_EUNSUPPORTED (device), W4_EHIP. */
+int kv4_load(void);
+
 /* Quantise new keys / values k_new, v_new (bf16 [B][T][n_kv_heads][head_dim],
  * device) into slots slot_start[b] .. slot_start[b]+T-1 of sequence b.
  * slot_start is a host array [B].  No other slot changes.  Deterministic.

@@ -104,6 +104,7 @@ _SIG = {
     "layer_decode_noalloc_max_bytes": (ctypes.c_size_t, []),
     "kv_append": (ctypes.c_int, [ctypes.POINTER(kv_desc), _P, _P, _P, _P, _I, _I, _P, _P]),
     "kv4_layout": (ctypes.c_int, [ctypes.POINTER(layer_config), _I, ctypes.POINTER(kv4_desc)]),
+    "kv4_load": (ctypes.c_int, []),
     "kv4_append": (ctypes.c_int, [ctypes.POINTER(kv4_desc), _P, _P, _P, _P, _I, _I, _P, _P]),
     "kv4_append_step": (ctypes.c_int, [ctypes.POINTER(kv4_desc), _P, _P, _P, _P, _I, _P, _P]),
     "kv4_read": (ctypes.c_int, [ctypes.POINTER(kv4_desc), _P, _P, _I, _I, _P, _P, _P, _P]),
@@ -316,6 +317,10 @@ def kv4_layout(cfg, batch: int):
     d = kv4_desc()
     rc = _lib.kv4_layout(ctypes.byref(make_config(cfg)), batch, ctypes.byref(d))
     return rc, d
+
+
+def kv4_load() -> int:
+    return _lib.kv4_load()
 
 
 def kv4_append(desc: kv4_desc, k_cache, v_cache, k_new, v_new, B, T, slot_start, stream=None) -> int:
@@ -686,6 +691,7 @@ class KV4Cache:
         import torch
         rc, self.desc = kv4_layout(cfg, batch)
         check(rc)
+        check(kv4_load())
         self.n_heads = cfg.n_heads
         self._k = torch.empty(self.desc.bytes, dtype=torch.uint8, device="cuda")
         self._v = torch.empty(self.desc.bytes, dtype=torch.uint8, device="cuda")

@@ -1459,6 +1459,12 @@ int kv4_layout(const layer_config* cfg, int32_t batch, kv4_desc* out) {
     return W4_OK;
 }
 
+int kv4_load(void) {
+    if (int rc = check_device()) return rc;
+    if (load_kv4() || load_kv4_attn()) return fail(W4_EHIP, "kernels not loaded: %s", hipGetErrorString(hipGetLastError()));
+    return W4_OK;
+}
+
 int kv4_append(const kv4_desc* desc, void* kc, void* vc, const void* k_new, const void* v_new, int32_t B, int32_t T,
                const int32_t* slot_start, void* stream) {
     return kv4_store(desc, kc, vc, k_new, v_new, B, T, slot_start, false, stream);

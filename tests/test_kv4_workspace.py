@@ -102,6 +102,7 @@ def fake(monkeypatch):
         calls.append((ws, stream))
         return 0
 
+    monkeypatch.setattr(binding._lib, "kv4_load", lambda: 0)
     monkeypatch.setattr(binding._lib, "kv4_attn_decode", attn)
     monkeypatch.setattr(binding._lib, "kv4_attn_prefill", attn)
     return types.SimpleNamespace(torch=torch, calls=calls, cache=binding.KV4Cache(CFG, 2))
