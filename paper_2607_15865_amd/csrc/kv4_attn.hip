@@ -88,7 +88,7 @@ __device__ __forceinline__ void put_pair(const Kv4AttnArgs& a, size_t off, float
 // group.  Wave w of 8 takes tiles w, w + 8, .. of the share on its own; the next
 // tile's K is requested when this one's scores are formed and its V when its
 // output is, into the same registers, so that two blocks fit a CU (CT 1; 16 rows of up to 32768 keys of 8 heads of
-// 128 take 96 to 99 us, 5.2 TB/s, where reading alone in this pattern takes 85).  The first
+// 128, 480 to 500 MB, take 96 to 100 us, 5.0 TB/s; the device reads at 5.9 at most).  The first
 // tile's requests do not wait for the context length: a share's place is fixed by
 // the longest context, and blocks past a row's own end leave.  CT column tiles of 16 /
 // NS heads.  Softmax: the maximum of a head moves only when a score passes it by
@@ -97,7 +97,8 @@ __device__ __forceinline__ void put_pair(const Kv4AttnArgs& a, size_t off, float
 // value near 0 cancel, so P' rounded once would leave 2^-12 of the group's range.
 // They are multiplied by ef = 2^10 so that small ones keep their digits; if one
 // passes the fp16 range after all (a scale above 8), ef drops to 1 for the rest of
-// the share: e^2 times the largest scale (8734) is 64536.
+// the share: e^2 times the largest scale (8704: bf16 values that fp16 has
+// end at 65280) is 64314.
 template <int D, int CT>
 __global__ void __launch_bounds__(64 * DW, CT == 1 ? 4 : 2) kv4_decode_kernel(Kv4AttnArgs a) {
     constexpr int NS = D / 32, NDB = D / 16, HC = 16 / NS, PS = 8 / NS;
@@ -503,6 +504,9 @@ __global__ void __launch_bounds__(256) kv4_decode_merge_kernel(Kv4AttnArgs a) {
 // unpacked, an operand of O^T = V^T P^T as it stands.  A lane owns one row: the
 // online softmax needs a lane exchange only when a maximum moves, which it does when a
 // score passes it by more than 8 (log2 units; weights stay below 2^8, in fp16).
+// Keys, values and weights rounded to fp16 (2^-11 each) are what lets the matrix units take a stage in one product each;
+// the rounding of the output to bf16 (2^-8) hides them: against 64 bits the outputs are off by 0.00170 in the mean, and
+// 0.00166 where those are fp32.
 //
 // Work is dealt out in one of two ways (kv4_prefill_plan).  In pieces (a.pf_chunk):
 // every row tile's stages are cut into as many equal parts as it has runs of pf_chunk, one
@@ -511,9 +515,9 @@ __global__ void __launch_bounds__(256) kv4_decode_merge_kernel(Kv4AttnArgs a) {
 // long work ends everywhere at once.  A row tile with more than one part leaves their states in
 // the workspace, and a second launch merges them in order.
 //
-// Measured, 2011 queries of 28 heads of 4 behind 14001 tokens: 481 to 535 us by
-// the card's clock, 0.81 to 0.90 PFLOP/s (a library product of two 8192^2 fp16
-// matrices: 1.14).  In a build without the exponentials 449, without the expansion
+// Measured, 2011 queries of 28 heads of 4 behind 14001 tokens: 475 to 540 us by
+// the card's clock; 522, 0.83 PFLOP/s, where a library product of two 8192^2 fp16
+// matrices ran at 1.13.  With all CUs at work a stage takes 2.4 us (d = 64: 2.1).  In a build without the exponentials 449, without the expansion
 // 430, with neither 426, without the first product 428: the halves overlap, and
 // the clock at the power limit bounds what is left.
 constexpr int PF_W = 8;                      // waves per block
