@@ -30,6 +30,7 @@ W4_WEIGHTS_INT4, W4_WEIGHTS_INT8, W4_WEIGHTS_BF16 = 0, 1, 2
 WEIGHT_FORMAT_CODE = {"int4": W4_WEIGHTS_INT4, "int8": W4_WEIGHTS_INT8, "bf16": W4_WEIGHTS_BF16}
 STAGE_PREFILL, STAGE_PREFILL_KV, STAGE_DECODE = 0, 1, 2
 W4_KV_BF16, W4_KV_INT4 = 0, 1
+_CAPTURE_RELAXED = 2                     # hipStreamCaptureModeRelaxed: memory may be allocated while a stream is captured
 KV_FORMAT_CODE = {"bf16": W4_KV_BF16, "int4": W4_KV_INT4}
 LINEAR_INDEX = {"q": 0, "k": 1, "v": 2, "o": 3, "gate": 4, "up": 5, "down": 6}
 
@@ -788,8 +789,15 @@ class KV4Cache:
         rc = fn(*args, ws[0], ws[1], stream)                 # (without a workspace: refuses the arguments, or asks for one)
         if rc == W4_EWORKSPACE:
             n = max(kv4_attn_workspace_size(self.desc, self.n_heads, stage, B, T, ctx), 0 if capturing else 2 * ws[1])
-            new = self._torch.empty(n, dtype=self._torch.uint8, device=self._k.device)
-            if not capturing:
+            if capturing:
+                new = self._torch.empty(n, dtype=self._torch.uint8, device=self._k.device)
+            else:
+                mode = _lib.w4_capture_mode(_CAPTURE_RELAXED)      # (some other stream may be in a capture)
+                try:
+                    new = self._torch.empty(n, dtype=self._torch.uint8, device=self._k.device)
+                finally:
+                    if mode >= 0:
+                        _lib.w4_capture_mode(mode)
                 self._ws[stream] = (new.data_ptr(), n, new)
             rc = fn(*args, new.data_ptr(), n, stream)
         check(rc)

@@ -1459,6 +1459,12 @@ int kv4_layout(const layer_config* cfg, int32_t batch, kv4_desc* out) {
     return W4_OK;
 }
 
+// (for the binding) Sets this thread's stream capture mode, returns the one before or -1.
+int w4_capture_mode(int mode) {
+    hipStreamCaptureMode m = (hipStreamCaptureMode)mode;
+    return hipThreadExchangeStreamCaptureMode(&m) == hipSuccess ? (int)m : -1;
+}
+
 int kv4_load(void) {
     if (int rc = check_device()) return rc;
     if (load_kv4() || load_kv4_attn()) return fail(W4_EHIP, "kernels not loaded: %s", hipGetErrorString(hipGetLastError()));

@@ -161,3 +161,50 @@ def test_captured_stream_that_is_not_current():
             c.attn_decode(q, ctx, N - 1, ref)
         torch.cuda.synchronize()
         assert all(torch.equal(a, b) for a, b in zip(outs, refs)), r
+
+
+def test_eager_call_beside_a_capture():
+    """While one stream is captured, a call on another one that is no part of the capture runs at once."""
+    c, g = filled(6)
+    q, ctx, idle = rand(g, (2, NQ, D)), i32(N - 1, 333), torch.cuda.Stream()
+    out, now, ref = (torch.zeros_like(q) for _ in range(3))
+    c.attn_decode(q, ctx, N - 1, ref)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        c.attn_decode(q, ctx, N - 1, out)
+        c.attn_decode(q, ctx, N - 1, now, stream=idle)
+    idle.synchronize()
+    assert torch.equal(now, ref)
+    now.zero_()
+    for _ in range(3):
+        out.zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(out, ref) and not now.any()
+
+
+def test_cache_made_in_a_capture():
+    """A cache made, filled and read in a captured graph: its memory is the graph's, every replay gives the same."""
+    _, g = filled(7)
+    cfg = synth.replace(synth.CONFIGS["llama8b"], n_heads=NQ, n_kv_heads=NKV, head_dim=D, max_seq=400)
+    k, v, q = rand(g, (1, 400, NKV, D)), rand(g, (1, 400, NKV, D)), rand(g, (300, NQ, D))
+    out, ref = torch.zeros_like(q), torch.zeros_like(q)
+    back = [torch.zeros_like(k) for _ in range(4)]
+    e = binding.KV4Cache(cfg, 1)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        c = binding.KV4Cache(cfg, 1)
+        c.append(k, v, [0])
+        c.attn_prefill(q, 100, out)
+    for _ in range(4):
+        for t in (k, v, q):
+            t.copy_(rand(g, t.shape))
+        graph.replay()
+        e.append(k, v, [0])
+        e.attn_prefill(q, 100, ref)
+        c.read([0], 400, *back[:2])                          # (400 slots end inside a tile, whose rest is anything)
+        e.read([0], 400, *back[2:])
+        torch.cuda.synchronize()
+        assert torch.equal(out, ref) and torch.equal(back[0], back[2]) and torch.equal(back[1], back[3])
