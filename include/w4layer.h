@@ -14,7 +14,8 @@
  *
  * plus the KV-cache calls kv_layout / kv_append (the in-place Concat of
  * Sec. 4.6.3), the same cache held in 4 bits with the attention that reads it
- * (kv4_*), layer stacks (stack_*), and the model ends around the layers
+ * (kv4_*), attention with a window and sinks and of drafted tokens over the bf16
+ * cache (kv_attn_*, tree_*), layer stacks (stack_*), and the model ends around the layers
  * (lm_*: embedding, LM head and greedy sampling of the runtime loop, Sec. 2).
  *
  * Conventions shared by every call
@@ -536,6 +537,114 @@ int kv4_attn_prefill(const kv4_desc* desc, const void* q, int32_t T, int32_t his
  * decode calls are refused (W4_EUNSUPPORTED).  Errors: W4_EINVAL,
  * W4_EUNSUPPORTED (max_seq). */
 int layer_set_kv_format(layer_t layer, int32_t format);
+
+/* ---- attention over the bf16 cache: window, sinks, draft trees ---------------- */
+
+/* Attention of queries that are already in place (after RoPE) over a bf16
+ * K and V cache, on its own, n_heads query heads on the cache's kv heads
+ * (n_heads a multiple of n_kv_heads), scores scaled by head_dim^-1/2:
+ *   out[r][h] = sum_j softmax_j(q[r][h] . K_j / sqrt(head_dim) [+ mask_j]) V_j
+ * over the slots j that the row sees.  window > 0: a row at position p sees
+ * the last `window` slots up to its own, p - window + 1 .. p, and the first
+ * `sinks` slots of the sequence (0: none); window 0: all slots up to its own.
+ * Slots that a row does not see may hold anything (NaN included); a value
+ * that it sees and that is not finite makes its output not finite in that dim,
+ * and may in others.
+ *
+ * q and out are bf16 [rows][n_heads][head_dim], out rounded once.  Scores,
+ * softmax statistics and sums are fp32; the weights are multiplied as bf16
+ * pairs (2^-16), or, where many rows share the keys, rounded to bf16 (2^-8).
+ * Deterministic.  *desc: head_dim 64 or 128, max_seq at most 2^27, strides that are multiples
+ * of 8 elements (any order: stride_s need not be head_dim), and that stay within `bytes`; cache, q and out pointers
+ * 16-byte aligned.  The calls check their arguments on the host before anything is
+ * launched, are asynchronous on the stream, allocate nothing and may be captured
+ * into a graph.
+ *
+ * kv_attn_decode: one query for each of B sequences; row b stands at position
+ * ctx_lens[b] (int32 [B] device, every one <= max_ctx), whose slot is
+ * already written.  ctx_lens[b] = -1 (a padded row) gives a zero row.
+ *   attn_mask  fp32 [B][max_seq] device, added to the scores (finite or
+ *              -inf: hidden), or NULL; a row whose slots are all hidden gives zeros;
+ *   ws         at least kv_attn_workspace_size(desc, n_heads, 2, B, 1, max_ctx).
+ *
+ * kv_attn_prefill: T >= 1 queries of one sequence (k_cache, v_cache: that
+ * sequence's part of the cache) behind hist_len >= 0 cached tokens; query t
+ * stands at position hist_len + t, whose slot is already written.
+ *   ws         at least kv_attn_workspace_size(desc, n_heads, 1, 1, T, hist_len).
+ *
+ * kv_attn_tree: N drafted tokens (1 .. W4_TREE_MAX) for each of B sequences, held as a
+ * tree: node i of sequence b has slot ctx_lens[b] + i (already written) and position pos[b][i].  It sees the context, slots
+ * 0 .. ctx_lens[b] - 1, within its window and the sinks, and those nodes whose bit
+ * is set in its mask.  Both come from tree_plan, with the same window and sinks.
+ * q and out are [B][N][n_heads][head_dim].
+ *   tree_mask  uint64 [B][N][ceil(N / 64)] device: bit a % 64 of word a / 64 of
+ *              node i is set if it sees node a (its own among them);
+ *   pos        int32 [B][N] device, every one >= ctx_lens[b]; may be NULL without a window;
+ *   ws         at least kv_attn_workspace_size(desc, n_heads, 3, B, N, max_ctx).
+ *
+ * The workspace may hold anything, and belongs to one call at a time.
+ * kv_attn_workspace_size: 0 for invalid arguments; it does not decrease with B, T
+ * or max_ctx, and serves every window.
+ * Errors: W4_EINVAL, W4_ECAPACITY (B > desc->batch, slots beyond max_seq, more rows than a launch
+ * takes), W4_EUNSUPPORTED (heads, head_dim, N), W4_EWORKSPACE, W4_EHIP. */
+#define W4_TREE_MAX 256
+size_t kv_attn_workspace_size(const kv_desc* desc, int32_t n_heads, int32_t stage, int32_t B, int32_t T,
+                              int32_t max_ctx);
+int kv_attn_decode(const kv_desc* desc, const void* q, const int32_t* ctx_lens, int32_t max_ctx,
+                   int32_t window, int32_t sinks, const float* attn_mask, int32_t B, int32_t n_heads,
+                   const void* k_cache, const void* v_cache, void* out, void* ws, size_t ws_bytes, void* stream);
+int kv_attn_prefill(const kv_desc* desc, const void* q, int32_t T, int32_t hist_len, int32_t window, int32_t sinks,
+                    int32_t n_heads, const void* k_cache, const void* v_cache, void* out, void* ws, size_t ws_bytes,
+                    void* stream);
+int kv_attn_tree(const kv_desc* desc, const void* q, const int32_t* ctx_lens, int32_t max_ctx,
+                 const uint64_t* tree_mask, const int32_t* pos, int32_t window, int32_t sinks, int32_t B, int32_t N,
+                 int32_t n_heads, const void* k_cache, const void* v_cache, void* out, void* ws, size_t ws_bytes,
+                 void* stream);
+
+/* Loads the code of these kernels and of the tree_ calls on the current
+ * device, so that the first calls do not (as kv4_load).  Errors: W4_EUNSUPPORTED (device), W4_EHIP. */
+int kv_attn_load(void);
+
+/* Copy new keys / values k_new, v_new (bf16 [B][T][n_kv_heads][head_dim],
+ * device, 16-byte aligned) into slots ctx_lens[b] .. ctx_lens[b]+T-1 (int32 [B], device): kv_append where the
+ * host does not know the slots.  Bit-exact.  A slot outside 0 .. max_seq-1, and
+ * every slot of a sequence with ctx_lens[b] < 0 (a padded row), is not written.
+ * *desc as for the attention calls.  Errors: W4_EINVAL, W4_EUNSUPPORTED, W4_ECAPACITY (B), W4_EHIP. */
+int kv_append_step(const kv_desc* desc, void* k_cache, void* v_cache, const void* k_new, const void* v_new,
+                   int32_t B, int32_t T, const int32_t* ctx_lens, void* stream);
+
+/* One step of decoding with drafted tokens, N per sequence, as a tree
+ * (parents int32 [B][N] device: node i hangs below node parents[b][i] < i;
+ * anything outside 0 .. i-1 makes it a root).  Node 0 is the sequence's last token, whose key and
+ * value are not in the cache yet; the others are guesses of what follows.
+ * 1 <= N <= W4_TREE_MAX.  All deterministic, on the device, capturable.
+ *
+ * tree_plan: what the model's layers need: pos[b][i] = ctx_lens[b] + depth of
+ * node i (0 for ctx_lens[b] < 0; int32 [B][N] out, also RoPE's positions) and
+ * tree_mask (out, as kv_attn_tree takes it): node i sees itself and those ancestors a
+ * with pos[a] > pos[i] - window (window 0: all) or pos[a] < sinks.
+ *
+ * tree_accept: picks[b][i] is the token that the model puts after node i (int32
+ * [B][N] device, e.g. lm_head's next_tokens).  From node 0 on, the
+ * path goes to the child whose token equals the pick of the node it hangs
+ * below, the one with the lowest index if several do, until there is none.
+ *   path         int32 [B][N] out: the path's nodes, then -1;
+ *   n_path       int32 [B] out: their number, 1 or more;
+ *   next_tokens  int32 [B] out: the pick of the last of them.
+ *
+ * kv_tree_keep: moves the keys and values of the path's nodes together, slot ctx_lens[b] +
+ * path[b][t] to ctx_lens[b] + t for t < n_path[b], in n_caches pairs of caches
+ * (host arrays, at most 1024; one pair per layer, all in the layout of *desc and none twice).  The context is then ctx_lens[b] +
+ * n_path[b] tokens.  The other slots keep what they held.  Sequences with ctx_lens[b] < 0 are left alone; so
+ * is a move whose slots are not below max_seq or whose node is not in t .. N-1.
+ * Errors: W4_EINVAL, W4_EUNSUPPORTED (N, *desc as for the attention calls), W4_ECAPACITY (B, n_caches), W4_EHIP. */
+int tree_plan(const int32_t* parents, const int32_t* ctx_lens, int32_t B, int32_t N, int32_t window, int32_t sinks,
+              uint64_t* tree_mask, int32_t* pos, void* stream);
+int tree_accept(const int32_t* parents, const int32_t* tokens, const int32_t* picks, int32_t B, int32_t N,
+                int32_t* path, int32_t* n_path, int32_t* next_tokens, void* stream);
+int kv_tree_keep(const kv_desc* desc, void* const* k_caches, void* const* v_caches, int32_t n_caches,
+                 const int32_t* ctx_lens, const int32_t* path, const int32_t* n_path, int32_t B, int32_t N,
+                 void* stream);
 
 /* ---- diagnostics ------------------------------------------------------- */
 

@@ -28,9 +28,10 @@ W4_OK, W4_EINVAL, W4_EUNSUPPORTED, W4_ECAPACITY, W4_EWORKSPACE, W4_EHIP = 0, -1,
 W4_FLAG_WAIT_TIMEOUT, W4_FLAG_F16_RANGE, W4_FLAG_TOKEN_ID = 1, 2, 4
 W4_WEIGHTS_INT4, W4_WEIGHTS_INT8, W4_WEIGHTS_BF16 = 0, 1, 2
 WEIGHT_FORMAT_CODE = {"int4": W4_WEIGHTS_INT4, "int8": W4_WEIGHTS_INT8, "bf16": W4_WEIGHTS_BF16}
-STAGE_PREFILL, STAGE_PREFILL_KV, STAGE_DECODE = 0, 1, 2
+STAGE_PREFILL, STAGE_PREFILL_KV, STAGE_DECODE, STAGE_TREE = 0, 1, 2, 3
 W4_KV_BF16, W4_KV_INT4 = 0, 1
 _CAPTURE_RELAXED = 2                     # hipStreamCaptureModeRelaxed: memory may be allocated while a stream is captured
+W4_TREE_MAX = 256
 KV_FORMAT_CODE = {"bf16": W4_KV_BF16, "int4": W4_KV_INT4}
 LINEAR_INDEX = {"q": 0, "k": 1, "v": 2, "o": 3, "gate": 4, "up": 5, "down": 6}
 
@@ -113,6 +114,18 @@ _SIG = {
     "kv4_attn_decode": (ctypes.c_int, [ctypes.POINTER(kv4_desc), _P, _P, _I, _P, _I, _I, _P, _P, _P, _P,
                                        ctypes.c_size_t, _P]),
     "kv4_attn_prefill": (ctypes.c_int, [ctypes.POINTER(kv4_desc), _P, _I, _I, _I, _P, _P, _P, _P, ctypes.c_size_t, _P]),
+    "kv_attn_workspace_size": (ctypes.c_size_t, [ctypes.POINTER(kv_desc), _I, _I, _I, _I, _I]),
+    "kv_attn_decode": (ctypes.c_int, [ctypes.POINTER(kv_desc), _P, _P, _I, _I, _I, _P, _I, _I, _P, _P, _P, _P,
+                                      ctypes.c_size_t, _P]),
+    "kv_attn_prefill": (ctypes.c_int, [ctypes.POINTER(kv_desc), _P, _I, _I, _I, _I, _I, _P, _P, _P, _P, ctypes.c_size_t,
+                                       _P]),
+    "kv_attn_tree": (ctypes.c_int, [ctypes.POINTER(kv_desc), _P, _P, _I, _P, _P, _I, _I, _I, _I, _I, _P, _P, _P, _P,
+                                    ctypes.c_size_t, _P]),
+    "kv_attn_load": (ctypes.c_int, []),
+    "kv_append_step": (ctypes.c_int, [ctypes.POINTER(kv_desc), _P, _P, _P, _P, _I, _I, _P, _P]),
+    "tree_plan": (ctypes.c_int, [_P, _P, _I, _I, _I, _I, _P, _P, _P]),
+    "tree_accept": (ctypes.c_int, [_P, _P, _P, _I, _I, _P, _P, _P, _P]),
+    "kv_tree_keep": (ctypes.c_int, [ctypes.POINTER(kv_desc), _P, _P, _I, _P, _P, _P, _I, _I, _P]),
     "layer_debug_dequant": (ctypes.c_int, [_P, _I, _P, _P]),
     "layer_set_decode_path": (ctypes.c_int, [_P, _I]),
     "layer_set_kv_format": (ctypes.c_int, [_P, _I]),
@@ -354,6 +367,51 @@ def kv4_attn_decode(desc: kv4_desc, q, ctx_lens, max_ctx, attn_mask, B, n_heads,
 def kv4_attn_prefill(desc: kv4_desc, q, T, hist_len, n_heads, k_cache, v_cache, out, ws, ws_bytes, stream=None) -> int:
     return _lib.kv4_attn_prefill(ctypes.byref(desc), _ptr(q), T, hist_len, n_heads, _ptr(k_cache), _ptr(v_cache),
                                  _ptr(out), _ptr(ws), ws_bytes, _stream(stream))
+
+
+def kv_attn_load() -> int:
+    return _lib.kv_attn_load()
+
+
+def kv_attn_workspace_size(desc: kv_desc, n_heads, stage, B, T, max_ctx) -> int:
+    return _lib.kv_attn_workspace_size(ctypes.byref(desc), n_heads, stage, B, T, max_ctx)
+
+
+def kv_attn_decode(desc: kv_desc, q, ctx_lens, max_ctx, window, sinks, attn_mask, B, n_heads, k_cache, v_cache, out, ws,
+                   ws_bytes, stream=None) -> int:
+    return _lib.kv_attn_decode(ctypes.byref(desc), _ptr(q), _ptr(ctx_lens), max_ctx, window, sinks, _ptr(attn_mask), B,
+                               n_heads, _ptr(k_cache), _ptr(v_cache), _ptr(out), _ptr(ws), ws_bytes, _stream(stream))
+
+
+def kv_attn_prefill(desc: kv_desc, q, T, hist_len, window, sinks, n_heads, k_cache, v_cache, out, ws, ws_bytes,
+                    stream=None) -> int:
+    return _lib.kv_attn_prefill(ctypes.byref(desc), _ptr(q), T, hist_len, window, sinks, n_heads, _ptr(k_cache),
+                                _ptr(v_cache), _ptr(out), _ptr(ws), ws_bytes, _stream(stream))
+
+
+def kv_attn_tree(desc: kv_desc, q, ctx_lens, max_ctx, tree_mask, pos, window, sinks, B, N, n_heads, k_cache, v_cache, out,
+                 ws, ws_bytes, stream=None) -> int:
+    return _lib.kv_attn_tree(ctypes.byref(desc), _ptr(q), _ptr(ctx_lens), max_ctx, _ptr(tree_mask), _ptr(pos), window, sinks,
+                             B, N, n_heads, _ptr(k_cache), _ptr(v_cache), _ptr(out), _ptr(ws), ws_bytes, _stream(stream))
+
+
+def kv_append_step(desc: kv_desc, k_cache, v_cache, k_new, v_new, B, T, ctx_lens, stream=None) -> int:
+    return _lib.kv_append_step(ctypes.byref(desc), _ptr(k_cache), _ptr(v_cache), _ptr(k_new), _ptr(v_new), B, T,
+                               _ptr(ctx_lens), _stream(stream))
+
+
+def tree_plan(parents, ctx_lens, B, N, window, sinks, tree_mask, pos, stream=None) -> int:
+    return _lib.tree_plan(_ptr(parents), _ptr(ctx_lens), B, N, window, sinks, _ptr(tree_mask), _ptr(pos), _stream(stream))
+
+
+def tree_accept(parents, tokens, picks, B, N, path, n_path, next_tokens, stream=None) -> int:
+    return _lib.tree_accept(_ptr(parents), _ptr(tokens), _ptr(picks), B, N, _ptr(path), _ptr(n_path), _ptr(next_tokens),
+                            _stream(stream))
+
+
+def kv_tree_keep(desc: kv_desc, k_caches, v_caches, n_caches, ctx_lens, path, n_path, B, N, stream=None) -> int:
+    return _lib.kv_tree_keep(ctypes.byref(desc), _ptr_array(k_caches), _ptr_array(v_caches), n_caches, _ptr(ctx_lens),
+                             _ptr(path), _ptr(n_path), B, N, _stream(stream))
 
 
 def layer_debug_dequant(handle, which, out, stream=None) -> int:
@@ -676,50 +734,20 @@ class Stack:
                            stream))
 
 
-class KV4Cache:
-    """A K and a V cache in 4 bits (kv4_layout(cfg, batch)) with the operators
-    over them; methods raise W4Error for what the library refuses and
-    ValueError for tensors that do not fit.
+class _OnDevice:
+    """What the classes of operators on tensors share: checks of the tensors, streams, and a workspace for each stream."""
 
-    Keys, values, queries and outputs are contiguous bf16 tensors (or 16-bit
-    integers holding the bits) on the cache's device, which must be the current
-    one.  Calls run on ``stream`` (default: torch's current stream).  A call's
-    workspace is allocated on that stream and kept per stream; where that stream is
-    being captured (torch.cuda.graph), it is allocated in the capture, so that
-    every graph, and every branch of one, has its own.  The caches k and v stay the same tensors."""
-
-    def __init__(self, cfg, batch: int):
+    def _setup(self, device, what: str):
         import torch
-        rc, self.desc = kv4_layout(cfg, batch)
-        check(rc)
-        check(kv4_load())
-        self.n_heads = cfg.n_heads
-        self._k = torch.empty(self.desc.bytes, dtype=torch.uint8, device="cuda")
-        self._v = torch.empty(self.desc.bytes, dtype=torch.uint8, device="cuda")
-        self._ws = {}                    # stream: address, bytes and tensor
-        # what every call needs, in the form that costs a call least
-        self._desc_ref = ctypes.byref(self.desc)
-        self._dev = self._k.device.index
-        self._kp, self._vp = self._k.data_ptr(), self._v.data_ptr()
-        self._no_ws = (self._kp, 0)
-        self._slot_arrays = {}
-        self._head = (self.desc.n_kv_heads, self.desc.head_dim)
-        self._q_head = (cfg.n_heads, self.desc.head_dim)
-        self._torch = torch
+        self._torch, self._device, self._dev, self._what = torch, device, device.index, what
         self._bits16 = (torch.bfloat16, torch.int16, torch.uint16)
         self._capturing = torch.cuda.is_current_stream_capturing
         # (torch.cuda.current_stream() builds a Stream object, 2.7 us; its handle alone takes 0.1)
         self._raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream",
                                    lambda dev: torch.cuda.current_stream(dev).cuda_stream)
         self._current_device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
-
-    @property
-    def k(self):
-        return self._k
-
-    @property
-    def v(self):
-        return self._v
+        self._ws = {}                    # stream: address, bytes and tensor
+        self._slot_arrays = {}
 
     def _refuse(self, t, shape, what, dtypes):
         """The reason why a tensor does not fit."""
@@ -728,7 +756,7 @@ class KV4Cache:
         if t.dtype not in dtypes:
             raise ValueError(f"{what}: dtype {t.dtype}")
         if t.get_device() != self._dev:
-            raise ValueError(f"{what} is on {t.device}, the cache on {self.k.device}")
+            raise ValueError(f"{what} is on {t.device}, {self._what} on {self._device}")
         raise ValueError(f"{what} must be contiguous")
 
     def _tensor(self, t, shape, what):
@@ -737,15 +765,20 @@ class KV4Cache:
             self._refuse(t, shape, what, self._bits16)
         return t.data_ptr()
 
-    def _ints(self, t, B, what):
-        if t.dtype != self._torch.int32 or t.shape != (B,) or t.get_device() != self._dev or not t.is_contiguous():
-            self._refuse(t, (B,), what, (self._torch.int32,))
+    def _ints(self, t, shape, what):
+        if t.dtype != self._torch.int32 or t.shape != shape or t.get_device() != self._dev or not t.is_contiguous():
+            self._refuse(t, shape, what, (self._torch.int32,))
+        return t.data_ptr()
+
+    def _floats(self, t, shape, what):
+        if t.dtype != self._torch.float32 or t.shape != shape or t.get_device() != self._dev or not t.is_contiguous():
+            self._refuse(t, shape, what, (self._torch.float32,))
         return t.data_ptr()
 
     def _on(self, stream):
         """The stream's handle; the cache's device has to be the current one."""
         if self._current_device() != self._dev:
-            raise ValueError(f"the cache is on {self.k.device}, the current device is {self._current_device()}")
+            raise ValueError(f"{self._what} is on {self._device}, the current device is {self._current_device()}")
         if stream is None:
             return self._raw_stream(self._dev)
         return stream if isinstance(stream, int) else stream.cuda_stream
@@ -788,19 +821,57 @@ class KV4Cache:
         ws = self._no_ws if capturing else self._ws.get(stream, self._no_ws)
         rc = fn(*args, ws[0], ws[1], stream)                 # (without a workspace: refuses the arguments, or asks for one)
         if rc == W4_EWORKSPACE:
-            n = max(kv4_attn_workspace_size(self.desc, self.n_heads, stage, B, T, ctx), 0 if capturing else 2 * ws[1])
+            n = max(self._workspace_size(self._desc_ref, self.n_heads, stage, B, T, ctx), 0 if capturing else 2 * ws[1])
             if capturing:
-                new = self._torch.empty(n, dtype=self._torch.uint8, device=self._k.device)
+                new = self._torch.empty(n, dtype=self._torch.uint8, device=self._device)
             else:
                 mode = _lib.w4_capture_mode(_CAPTURE_RELAXED)      # (some other stream may be in a capture)
                 try:
-                    new = self._torch.empty(n, dtype=self._torch.uint8, device=self._k.device)
+                    new = self._torch.empty(n, dtype=self._torch.uint8, device=self._device)
                 finally:
                     if mode >= 0:
                         _lib.w4_capture_mode(mode)
                 self._ws[stream] = (new.data_ptr(), n, new)
             rc = fn(*args, new.data_ptr(), n, stream)
         check(rc)
+
+
+class KV4Cache(_OnDevice):
+    """A K and a V cache in 4 bits (kv4_layout(cfg, batch)) with the operators
+    over them; methods raise W4Error for what the library refuses and
+    ValueError for tensors that do not fit.
+
+    Keys, values, queries and outputs are contiguous bf16 tensors (or 16-bit
+    integers holding the bits) on the cache's device, which must be the current
+    one.  Calls run on ``stream`` (default: torch's current stream).  A call's
+    workspace is allocated on that stream and kept per stream; where that stream is
+    being captured (torch.cuda.graph), it is allocated in the capture, so that
+    every graph, and every branch of one, has its own.  The caches k and v stay the same tensors."""
+
+    def __init__(self, cfg, batch: int):
+        import torch
+        rc, self.desc = kv4_layout(cfg, batch)
+        check(rc)
+        check(kv4_load())
+        self.n_heads = cfg.n_heads
+        self._k = torch.empty(self.desc.bytes, dtype=torch.uint8, device="cuda")
+        self._v = torch.empty(self.desc.bytes, dtype=torch.uint8, device="cuda")
+        self._setup(self._k.device, "the cache")
+        # what every call needs, in the form that costs a call least
+        self._workspace_size = _lib.kv4_attn_workspace_size
+        self._desc_ref = ctypes.byref(self.desc)
+        self._kp, self._vp = self._k.data_ptr(), self._v.data_ptr()
+        self._no_ws = (self._kp, 0)
+        self._head = (self.desc.n_kv_heads, self.desc.head_dim)
+        self._q_head = (cfg.n_heads, self.desc.head_dim)
+
+    @property
+    def k(self):
+        return self._k
+
+    @property
+    def v(self):
+        return self._v
 
     def append(self, k_new, v_new, slot_start, stream=None):
         """k_new, v_new [B][T][n_kv_heads][head_dim] into slots slot_start[b] .. + T - 1 (host integers)."""
@@ -816,7 +887,7 @@ class KV4Cache:
         B = k_new.shape[0]
         shape = (B, 1) + self._head if k_new.dim() == 4 else (B,) + self._head
         kp, vp = self._tensor(k_new, shape, "k_new"), self._tensor(v_new, shape, "v_new")
-        check(_lib.kv4_append_step(self._desc_ref, self._kp, self._vp, kp, vp, B, self._ints(ctx_lens, B, "ctx_lens"),
+        check(_lib.kv4_append_step(self._desc_ref, self._kp, self._vp, kp, vp, B, self._ints(ctx_lens, (B,), "ctx_lens"),
                                    self._on(stream)))
 
     def read(self, slot_start, T, k_out, v_out, stream=None):
@@ -830,13 +901,9 @@ class KV4Cache:
         """One query per sequence: q, out [B][n_heads][head_dim], slots 0 .. ctx_lens[b] (int32 [B] on the device)."""
         B = q.shape[0]
         shape = (B,) + self._q_head
-        qp, op, cp, mp = self._tensor(q, shape, "q"), self._tensor(out, shape, "out"), self._ints(ctx_lens, B, "ctx_lens"), None
+        qp, op, cp, mp = self._tensor(q, shape, "q"), self._tensor(out, shape, "out"), self._ints(ctx_lens, (B,), "ctx_lens"), None
         if attn_mask is not None:
-            mshape, f32 = (B, self.desc.max_seq), self._torch.float32
-            if attn_mask.shape != mshape or attn_mask.dtype != f32 or attn_mask.get_device() != self._dev or \
-                    not attn_mask.is_contiguous():
-                self._refuse(attn_mask, mshape, "attn_mask", (f32,))
-            mp = attn_mask.data_ptr()
+            mp = self._floats(attn_mask, (B, self.desc.max_seq), "attn_mask")
         max_ctx, st = self._i32(max_ctx, "max_ctx"), self._on(stream)
         self._attend(_lib.kv4_attn_decode, (self._desc_ref, qp, cp, max_ctx, mp, B, self.n_heads, self._kp, self._vp, op),
                      STAGE_DECODE, B, 1, max_ctx, st)
@@ -851,3 +918,139 @@ class KV4Cache:
         hist_len, off, st = self._i32(hist_len, "hist_len"), row * self.desc.stride_b, self._on(stream)
         self._attend(_lib.kv4_attn_prefill, (self._desc_ref, qp, T, hist_len, self.n_heads, self._kp + off, self._vp + off, op),
                      STAGE_PREFILL_KV, 1, T, hist_len, st)
+
+
+class KVCache(_OnDevice):
+    """A K and a V cache in bf16 (kv_layout(cfg, batch)) with the operators over them: appending, and attention with a
+    window and sinks, of single queries, of a prompt's and of drafted tokens (DraftTree).  Methods raise W4Error for what
+    the library refuses and ValueError for tensors that do not fit.
+
+    k, v: existing caches [batch][n_kv_heads][max_seq][head_dim] to work on (bf16, or 16-bit integers holding the bits,
+    such as Layer.new_cache gives; views with other strides as long as a slot's dims are contiguous); without
+    them new ones are made.  window 0: every slot up to the query's own.  Tensors, streams and workspaces as for KV4Cache."""
+
+    def __init__(self, cfg, batch: int, k=None, v=None):
+        import torch
+        rc, self.desc = kv_layout(cfg, batch)
+        check(rc)
+        shape = (batch, cfg.n_kv_heads, cfg.max_seq, cfg.head_dim)
+        if (k is None) != (v is None):
+            raise ValueError("either both caches or none")
+        if k is None:
+            k, v = (torch.empty(shape, dtype=torch.bfloat16, device="cuda") for _ in range(2))
+        self.n_heads, self.k, self.v = cfg.n_heads, k, v
+        self._setup(k.device, "the cache")
+        for t, what in ((k, "k"), (v, "v")):
+            if tuple(t.shape) != shape or t.dtype not in self._bits16 or t.device != k.device or t.device.type != "cuda":
+                self._refuse(t, shape, what, self._bits16)
+            if t.stride(3) != 1 or t.stride() != k.stride():
+                raise ValueError(f"{what}: strides {t.stride()}")
+        check(kv_attn_load())
+        if not k.is_contiguous():
+            self.desc.stride_b, self.desc.stride_h, self.desc.stride_s = k.stride()[:3]
+            self.desc.bytes = 2 * (1 + sum((n - 1) * m for n, m in zip(k.shape, k.stride())))
+        self._workspace_size = _lib.kv_attn_workspace_size
+        self._desc_ref = ctypes.byref(self.desc)
+        self._kp, self._vp = k.data_ptr(), v.data_ptr()
+        self._no_ws = (self._kp, 0)
+        self._head = (cfg.n_kv_heads, cfg.head_dim)
+        self._q_head = (cfg.n_heads, cfg.head_dim)
+
+    def append(self, k_new, v_new, slot_start, stream=None):
+        """k_new, v_new [B][T][n_kv_heads][head_dim] into slots slot_start[b] .. + T - 1 (host integers)."""
+        B, T = k_new.shape[:2]
+        shape = (B, T) + self._head
+        kp, vp = self._tensor(k_new, shape, "k_new"), self._tensor(v_new, shape, "v_new")
+        check(_lib.kv_append(self._desc_ref, self._kp, self._vp, kp, vp, B, T, self._slots(slot_start, B), self._on(stream)))
+
+    def append_step(self, k_new, v_new, ctx_lens, stream=None):
+        """k_new, v_new [B][T][n_kv_heads][head_dim] into slots ctx_lens[b] .. + T - 1 (int32 [B] on the device)."""
+        B, T = k_new.shape[:2]
+        shape = (B, T) + self._head
+        kp, vp = self._tensor(k_new, shape, "k_new"), self._tensor(v_new, shape, "v_new")
+        check(_lib.kv_append_step(self._desc_ref, self._kp, self._vp, kp, vp, B, T, self._ints(ctx_lens, (B,), "ctx_lens"),
+                                  self._on(stream)))
+
+    def attn_decode(self, q, ctx_lens, max_ctx, out, window: int = 0, sinks: int = 0, attn_mask=None, stream=None):
+        """One query per sequence: q, out [B][n_heads][head_dim], at positions ctx_lens[b] (int32 [B] on the device)."""
+        B = q.shape[0]
+        shape = (B,) + self._q_head
+        qp, op, cp = self._tensor(q, shape, "q"), self._tensor(out, shape, "out"), self._ints(ctx_lens, (B,), "ctx_lens")
+        mp = None if attn_mask is None else self._floats(attn_mask, (B, self.desc.max_seq), "attn_mask")
+        max_ctx, st = self._i32(max_ctx, "max_ctx"), self._on(stream)
+        self._attend(_lib.kv_attn_decode, (self._desc_ref, qp, cp, max_ctx, self._i32(window, "window"), self._i32(sinks, "sinks"),
+                                           mp, B, self.n_heads, self._kp, self._vp, op), STAGE_DECODE, B, 1, max_ctx, st)
+
+    def attn_prefill(self, q, hist_len, out, window: int = 0, sinks: int = 0, row: int = 0, stream=None):
+        """T queries of sequence `row` behind hist_len tokens: q, out [T][n_heads][head_dim]."""
+        T = q.shape[0]
+        shape = (T,) + self._q_head
+        qp, op = self._tensor(q, shape, "q"), self._tensor(out, shape, "out")
+        if not 0 <= row < self.desc.batch:
+            raise ValueError(f"row {row} of a cache of {self.desc.batch} sequences")
+        off = 2 * row * self.desc.stride_b
+        hist_len, st = self._i32(hist_len, "hist_len"), self._on(stream)
+        self._attend(_lib.kv_attn_prefill, (self._desc_ref, qp, T, hist_len, self._i32(window, "window"), self._i32(sinks, "sinks"),
+                                            self.n_heads, self._kp + off, self._vp + off, op),
+                     STAGE_PREFILL_KV, 1, T, hist_len, st)
+
+    def attn_tree(self, q, tree, ctx_lens, max_ctx, out, stream=None):
+        """The drafted tokens of a DraftTree, after its plan and with that plan's window: q, out
+        [B][N][n_heads][head_dim], their keys and values in slots ctx_lens[b] .. + N - 1."""
+        B, N = tree.batch, tree.nodes
+        shape = (B, N) + self._q_head
+        qp, op, cp = self._tensor(q, shape, "q"), self._tensor(out, shape, "out"), self._ints(ctx_lens, (B,), "ctx_lens")
+        if tree._dev != self._dev:
+            raise ValueError(f"the tree is on {tree._device}, the cache on {self._device}")
+        if tree.window is None:
+            raise ValueError("the tree has no plan yet")
+        max_ctx, st = self._i32(max_ctx, "max_ctx"), self._on(stream)
+        self._attend(_lib.kv_attn_tree, (self._desc_ref, qp, cp, max_ctx, tree.mask.data_ptr(), tree.pos.data_ptr(), tree.window,
+                                         tree.sinks, B, N, self.n_heads, self._kp, self._vp, op), STAGE_TREE, B, N, max_ctx, st)
+
+
+class DraftTree(_OnDevice):
+    """N drafted tokens for each of B sequences as trees: one step is plan (masks and positions), the model's layers with
+    KVCache.attn_tree, accept (the path that the model's picks follow), keep (its rows moved together in every layer's
+    caches).  The results are tensors of this object, which every step writes again: mask int64 [B][N][ceil(N / 64)] (bits),
+    pos, path int32 [B][N], n_path, next_tokens int32 [B].  parents, tokens and picks are int32 [B][N] on the device, ctx_lens int32 [B].
+    Calls run on ``stream`` (default: torch's current stream)."""
+
+    def __init__(self, batch: int, nodes: int):
+        import torch
+        if batch < 1 or not 1 <= nodes <= W4_TREE_MAX:
+            raise ValueError(f"trees of {nodes} nodes for {batch} sequences")
+        self.batch, self.nodes, self.window, self.sinks = batch, nodes, None, 0
+        self.mask = torch.zeros((batch, nodes, (nodes + 63) // 64), dtype=torch.int64, device="cuda")
+        self.pos, self.path = (torch.zeros((batch, nodes), dtype=torch.int32, device="cuda") for _ in range(2))
+        self.n_path, self.next_tokens = (torch.zeros(batch, dtype=torch.int32, device="cuda") for _ in range(2))
+        self._setup(self.mask.device, "the tree")
+        check(kv_attn_load())
+
+    def plan(self, parents, ctx_lens, window: int = 0, sinks: int = 0, stream=None):
+        B, N = self.batch, self.nodes
+        pp, cp = self._ints(parents, (B, N), "parents"), self._ints(ctx_lens, (B,), "ctx_lens")
+        window, sinks = self._i32(window, "window"), self._i32(sinks, "sinks")
+        check(_lib.tree_plan(pp, cp, B, N, window, sinks, self.mask.data_ptr(), self.pos.data_ptr(), self._on(stream)))
+        self.window, self.sinks = window, sinks
+
+    def accept(self, parents, tokens, picks, stream=None):
+        B, N = self.batch, self.nodes
+        pp, tp, kp = (self._ints(t, (B, N), what) for t, what in ((parents, "parents"), (tokens, "tokens"), (picks, "picks")))
+        check(_lib.tree_accept(pp, tp, kp, B, N, self.path.data_ptr(), self.n_path.data_ptr(), self.next_tokens.data_ptr(),
+                               self._on(stream)))
+
+    def keep(self, caches, ctx_lens, stream=None):
+        """Moves the path's rows together in the KVCaches of the model's layers (one layout, none twice)."""
+        caches = list(caches)
+        if not caches:
+            raise ValueError("no caches")
+        d = caches[0].desc
+        for c in caches:
+            if c._dev != self._dev:
+                raise ValueError(f"a cache is on {c._device}, the tree on {self._device}")
+            if bytes(c.desc) != bytes(d):
+                raise ValueError("the caches have different layouts")
+        kind, cp = ctypes.c_void_p * len(caches), self._ints(ctx_lens, (self.batch,), "ctx_lens")
+        check(_lib.kv_tree_keep(ctypes.byref(d), kind(*[c._kp for c in caches]), kind(*[c._vp for c in caches]), len(caches), cp,
+                                self.path.data_ptr(), self.n_path.data_ptr(), self.batch, self.nodes, self._on(stream)))

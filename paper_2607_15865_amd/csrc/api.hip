@@ -21,6 +21,7 @@
 #include "common.h"
 #include "decode_fused.h"
 #include "kv4.h"
+#include "kv_attn.h"
 #include "launch.h"
 #include "lm.h"
 
@@ -385,7 +386,8 @@ int check_device() {
 
 int load_kernels() {
     if (load_gemm_w4_qkv() || load_gemm_w4_resid() || load_gemm_w4_swiglu() || load_gemv_w4() || load_attention() ||
-        load_misc() || load_decode_fused() || load_lm() || load_kv4() || load_kv4_attn())
+        load_misc() || load_decode_fused() || load_lm() || load_kv4() || load_kv4_attn() ||
+        load_kv_attn() || load_tree())
         return fail(W4_EHIP, "kernels not loaded: %s", hipGetErrorString(hipGetLastError()));
     return W4_OK;
 }
@@ -1587,6 +1589,209 @@ int kv4_attn_prefill(const kv4_desc* d, const void* q, int32_t T, int32_t hist_l
     a.part = (float*)ws;
     if (launch_kv4_prefill(a, (hipStream_t)stream))
         return fail(W4_EHIP, "kernel launch failed: %s", hipGetErrorString(hipGetLastError()));
+    return W4_OK;
+}
+
+// ---------------------------------------------------------------- attention over the bf16 cache, draft trees
+
+// B is the batch of a call on the cache; of a launch, at most 65535.
+static int check_kv_desc(const kv_desc* d, int32_t B) {
+    if (d->batch < 1 || d->n_kv_heads < 1 || d->max_seq < 1) return fail(W4_EINVAL, "bad kv_desc");
+    if (d->max_seq > kKv4MaxSeq) return fail(W4_EUNSUPPORTED, "max_seq must be at most 2^27");
+    if (d->head_dim != 64 && d->head_dim != 128) return fail(W4_EUNSUPPORTED, "head_dim must be 64 or 128");
+    const int64_t D = d->head_dim;
+    if (d->stride_s < D || d->stride_h < D || d->stride_b < D || (d->stride_s | d->stride_h | d->stride_b) % 8)
+        return fail(W4_EINVAL, "bad kv_desc strides");
+    const __int128 last = (__int128)(d->batch - 1) * d->stride_b + (__int128)(d->n_kv_heads - 1) * d->stride_h +
+                          (__int128)(d->max_seq - 1) * d->stride_s + D;
+    if (last * 2 > (__int128)d->bytes || d->bytes > (size_t)1 << 62) return fail(W4_EINVAL, "kv_desc reaches beyond its bytes");
+    if (B < 1) return fail(W4_EINVAL, "B must be >= 1");
+    if (B > d->batch || B > 65535 || d->n_kv_heads > 65535) return fail(W4_ECAPACITY, "B = %d exceeds the cache batch", B);
+    return W4_OK;
+}
+
+static int check_kv_heads(const kv_desc* d, int32_t n_heads) {
+    if (n_heads < 1) return fail(W4_EINVAL, "n_heads must be >= 1");
+    if (n_heads % d->n_kv_heads) return fail(W4_EUNSUPPORTED, "n_heads must be a multiple of n_kv_heads");
+    if (n_heads / d->n_kv_heads > 64) return fail(W4_EUNSUPPORTED, "at most 64 query heads per kv head");
+    return W4_OK;
+}
+
+static int check_tree_size(int32_t B, int32_t N) {
+    if (B < 1 || N < 1) return fail(W4_EINVAL, "B and N must be >= 1");
+    if (N > W4_TREE_MAX) return fail(W4_EUNSUPPORTED, "N = %d, at most %d", N, W4_TREE_MAX);
+    return W4_OK;
+}
+
+static int check_window(int32_t window, int32_t sinks) {
+    if (window < 0 || sinks < 0) return fail(W4_EINVAL, "window and sinks must be >= 0");
+    return W4_OK;
+}
+
+size_t kv_attn_workspace_size(const kv_desc* d, int32_t n_heads, int32_t stage, int32_t B, int32_t T, int32_t max_ctx) {
+    if (!d || stage < 0 || stage > 3 || max_ctx < 0 || check_kv_desc(d, stage >= 2 ? B : 1) || check_kv_heads(d, n_heads))
+        return 0;
+    if (stage != 2 && T < 1) return 0;
+    if (stage == 3 && check_tree_size(B, T)) return 0;
+    return 256;
+}
+
+// Checks that the three attention calls share, and their launch.
+static int kv_attn_run(const kv_desc* d, KvAttnArgs a, int32_t stage, int32_t window, int32_t sinks, int32_t n_heads, const void* q,
+                       const void* kc, const void* vc, void* out, void* ws, size_t ws_bytes, void* stream) {
+    int rc;
+    if ((rc = check_kv_desc(d, a.B)) || (rc = check_kv_heads(d, n_heads)) || (rc = check_window(window, sinks))) return rc;
+    const long long slots = (long long)a.max_ctx + a.N;
+    if (slots > d->max_seq) return fail(W4_ECAPACITY, "%lld slots, max_seq %d", slots, d->max_seq);
+    if (!aligned16({q, kc, vc, out, ws})) return fail(W4_EINVAL, "pointers must be 16-byte aligned");
+    if (q == out) return fail(W4_EINVAL, "q and out must not alias");
+    const size_t need = kv_attn_workspace_size(d, n_heads, stage, a.B, a.N, a.max_ctx);
+    if (ws_bytes < need) return fail(W4_EWORKSPACE, "workspace %zu bytes, need %zu", ws_bytes, need);
+    a.q = (const uint16_t*)q;
+    a.k = (const uint16_t*)kc;
+    a.v = (const uint16_t*)vc;
+    a.out = (uint16_t*)out;
+    a.stride_b = d->stride_b;
+    a.stride_h = d->stride_h;
+    a.stride_s = d->stride_s;
+    a.max_seq = d->max_seq;
+    a.window = window ? window : INT_MAX;
+    a.sinks = window ? sinks : 0;
+    a.nq = n_heads;
+    a.nkv = d->n_kv_heads;
+    a.d = d->head_dim;
+    a.scale = (float)(1.0 / std::sqrt((double)d->head_dim));
+    if (launch_kv_attn(a, (hipStream_t)stream))
+        return fail(W4_EHIP, "kernel launch failed: %s", hipGetErrorString(hipGetLastError()));
+    return W4_OK;
+}
+
+int kv_attn_load(void) {
+    if (int rc = check_device()) return rc;
+    if (load_kv_attn() || load_tree()) return fail(W4_EHIP, "kernels not loaded: %s", hipGetErrorString(hipGetLastError()));
+    return W4_OK;
+}
+
+int kv_attn_decode(const kv_desc* d, const void* q, const int32_t* ctx_lens, int32_t max_ctx, int32_t window, int32_t sinks,
+                   const float* attn_mask, int32_t B, int32_t n_heads, const void* kc, const void* vc, void* out, void* ws,
+                   size_t ws_bytes, void* stream) {
+    if (!d || !q || !ctx_lens || !kc || !vc || !out || !ws) return fail(W4_EINVAL, "null pointer argument");
+    if (max_ctx < 0) return fail(W4_EINVAL, "max_ctx must be >= 0");
+    KvAttnArgs a{};
+    a.ctx_lens = ctx_lens;
+    a.max_ctx = max_ctx;
+    a.mask = attn_mask;
+    a.B = B;
+    a.N = 1;
+    return kv_attn_run(d, a, 2, window, sinks, n_heads, q, kc, vc, out, ws, ws_bytes, stream);
+}
+
+int kv_attn_prefill(const kv_desc* d, const void* q, int32_t T, int32_t hist_len, int32_t window, int32_t sinks, int32_t n_heads,
+                    const void* kc, const void* vc, void* out, void* ws, size_t ws_bytes, void* stream) {
+    if (!d || !q || !kc || !vc || !out || !ws) return fail(W4_EINVAL, "null pointer argument");
+    if (T < 1 || hist_len < 0) return fail(W4_EINVAL, "T must be >= 1 and hist_len >= 0");
+    KvAttnArgs a{};
+    a.ctx_base = a.max_ctx = hist_len;
+    a.B = 1;
+    a.N = T;
+    return kv_attn_run(d, a, 1, window, sinks, n_heads, q, kc, vc, out, ws, ws_bytes, stream);
+}
+
+int kv_attn_tree(const kv_desc* d, const void* q, const int32_t* ctx_lens, int32_t max_ctx, const uint64_t* tree_mask,
+                 const int32_t* pos, int32_t window, int32_t sinks, int32_t B, int32_t N, int32_t n_heads, const void* kc,
+                 const void* vc, void* out, void* ws, size_t ws_bytes, void* stream) {
+    if (!d || !q || !ctx_lens || !tree_mask || !kc || !vc || !out || !ws) return fail(W4_EINVAL, "null pointer argument");
+    if (window > 0 && !pos) return fail(W4_EINVAL, "a window needs the nodes' positions");
+    if (max_ctx < 0) return fail(W4_EINVAL, "max_ctx must be >= 0");
+    if (int rc = check_tree_size(B, N)) return rc;
+    KvAttnArgs a{};
+    a.ctx_lens = ctx_lens;
+    a.max_ctx = max_ctx;
+    a.tree = (const unsigned long long*)tree_mask;
+    a.pos = window > 0 ? pos : nullptr;
+    a.words = (N + 63) / 64;
+    a.B = B;
+    a.N = N;
+    return kv_attn_run(d, a, 3, window, sinks, n_heads, q, kc, vc, out, ws, ws_bytes, stream);
+}
+
+static KvSlotArgs kv_slot_args(const kv_desc* d, const int32_t* ctx_lens, int32_t B, int32_t T) {
+    KvSlotArgs a{};
+    a.stride_b = d->stride_b;
+    a.stride_h = d->stride_h;
+    a.stride_s = d->stride_s;
+    a.ctx_lens = ctx_lens;
+    a.max_seq = d->max_seq;
+    a.B = B;
+    a.T = T;
+    a.nkv = d->n_kv_heads;
+    a.d = d->head_dim;
+    return a;
+}
+
+int kv_append_step(const kv_desc* d, void* kc, void* vc, const void* k_new, const void* v_new, int32_t B, int32_t T,
+                   const int32_t* ctx_lens, void* stream) {
+    if (!d || !kc || !vc || !k_new || !v_new || !ctx_lens) return fail(W4_EINVAL, "null pointer argument");
+    if (int rc = check_kv_desc(d, B)) return rc;
+    if (T < 1) return fail(W4_EINVAL, "T must be >= 1");
+    if (!aligned16({kc, vc, k_new, v_new})) return fail(W4_EINVAL, "pointers must be 16-byte aligned");
+    if (kc == vc) return fail(W4_EINVAL, "K and V must not alias");
+    if (launch_kv_append_step(kv_slot_args(d, ctx_lens, B, T), (uint16_t*)kc, (uint16_t*)vc, (const uint16_t*)k_new,
+                              (const uint16_t*)v_new, (hipStream_t)stream))
+        return fail(W4_EHIP, "kernel launch failed: %s", hipGetErrorString(hipGetLastError()));
+    return W4_OK;
+}
+
+int tree_plan(const int32_t* parents, const int32_t* ctx_lens, int32_t B, int32_t N, int32_t window, int32_t sinks,
+              uint64_t* tree_mask, int32_t* pos, void* stream) {
+    if (!parents || !ctx_lens || !tree_mask || !pos) return fail(W4_EINVAL, "null pointer argument");
+    int rc;
+    if ((rc = check_tree_size(B, N)) || (rc = check_window(window, sinks))) return rc;
+    const TreePlanArgs a{parents, ctx_lens, B, N, window ? window : INT_MAX, sinks, (unsigned long long*)tree_mask, pos};
+    if (launch_tree_plan(a, (hipStream_t)stream))
+        return fail(W4_EHIP, "kernel launch failed: %s", hipGetErrorString(hipGetLastError()));
+    return W4_OK;
+}
+
+int tree_accept(const int32_t* parents, const int32_t* tokens, const int32_t* picks, int32_t B, int32_t N, int32_t* path,
+                int32_t* n_path, int32_t* next_tokens, void* stream) {
+    if (!parents || !tokens || !picks || !path || !n_path || !next_tokens) return fail(W4_EINVAL, "null pointer argument");
+    if (int rc = check_tree_size(B, N)) return rc;
+    const TreeAcceptArgs a{parents, tokens, picks, B, N, path, n_path, next_tokens};
+    if (launch_tree_accept(a, (hipStream_t)stream))
+        return fail(W4_EHIP, "kernel launch failed: %s", hipGetErrorString(hipGetLastError()));
+    return W4_OK;
+}
+
+constexpr int kMaxKeep = 1024;           // pairs of caches of a call
+
+int kv_tree_keep(const kv_desc* d, void* const* k_caches, void* const* v_caches, int32_t n_caches, const int32_t* ctx_lens,
+                 const int32_t* path, const int32_t* n_path, int32_t B, int32_t N, void* stream) {
+    if (!d || !k_caches || !v_caches || !ctx_lens || !path || !n_path) return fail(W4_EINVAL, "null pointer argument");
+    int rc;
+    if ((rc = check_kv_desc(d, B)) || (rc = check_tree_size(B, N))) return rc;
+    if (n_caches < 1) return fail(W4_EINVAL, "n_caches must be >= 1");
+    if (n_caches > kMaxKeep) return fail(W4_ECAPACITY, "n_caches = %d, at most %d", n_caches, kMaxKeep);
+    const void* all[2 * kMaxKeep];
+    for (int i = 0; i < n_caches; i++) {
+        if (!k_caches[i] || !v_caches[i]) return fail(W4_EINVAL, "null cache");
+        if (!aligned16({k_caches[i], v_caches[i]})) return fail(W4_EINVAL, "pointers must be 16-byte aligned");
+        all[2 * i] = k_caches[i];
+        all[2 * i + 1] = v_caches[i];
+    }
+    std::sort(all, all + 2 * n_caches);
+    if (std::adjacent_find(all, all + 2 * n_caches) != all + 2 * n_caches) return fail(W4_EINVAL, "a cache is given twice");
+    const KvSlotArgs a = kv_slot_args(d, ctx_lens, B, N);
+    for (int i = 0; i < n_caches; i += KEEP_CACHES) {
+        KeepCaches c{};
+        const int n = std::min(KEEP_CACHES, n_caches - i);
+        for (int j = 0; j < n; j++) {
+            c.p[2 * j] = (uint16_t*)k_caches[i + j];
+            c.p[2 * j + 1] = (uint16_t*)v_caches[i + j];
+        }
+        if (launch_kv_keep(a, c, n, path, n_path, (hipStream_t)stream))
+            return fail(W4_EHIP, "kernel launch failed: %s", hipGetErrorString(hipGetLastError()));
+    }
     return W4_OK;
 }
 
