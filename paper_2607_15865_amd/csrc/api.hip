@@ -6,6 +6,7 @@
 #include <algorithm>
 #include <atomic>
 #include <chrono>
+#include <climits>
 #include <cmath>
 #include <cstdio>
 #include <cstdarg>
@@ -1594,12 +1595,16 @@ int kv4_attn_prefill(const kv4_desc* d, const void* q, int32_t T, int32_t hist_l
 
 // ---------------------------------------------------------------- attention over the bf16 cache, draft trees
 
+constexpr int kKvMaxRows = INT_MAX - 256;        // of a kv head: queries times heads, in whole tiles
+constexpr int64_t kKvMaxStride = 1 << 25;        // (64 slots' offsets fit 32 bits)
+
 // B is the batch of a call on the cache; of a launch, at most 65535.
 static int check_kv_desc(const kv_desc* d, int32_t B) {
     if (d->batch < 1 || d->n_kv_heads < 1 || d->max_seq < 1) return fail(W4_EINVAL, "bad kv_desc");
     if (d->max_seq > kKv4MaxSeq) return fail(W4_EUNSUPPORTED, "max_seq must be at most 2^27");
     if (d->head_dim != 64 && d->head_dim != 128) return fail(W4_EUNSUPPORTED, "head_dim must be 64 or 128");
     const int64_t D = d->head_dim;
+    if (d->stride_s > kKvMaxStride) return fail(W4_EUNSUPPORTED, "stride_s must be at most 2^25");
     if (d->stride_s < D || d->stride_h < D || d->stride_b < D || (d->stride_s | d->stride_h | d->stride_b) % 8)
         return fail(W4_EINVAL, "bad kv_desc strides");
     const __int128 last = (__int128)(d->batch - 1) * d->stride_b + (__int128)(d->n_kv_heads - 1) * d->stride_h +
@@ -1633,7 +1638,9 @@ size_t kv_attn_workspace_size(const kv_desc* d, int32_t n_heads, int32_t stage, 
         return 0;
     if (stage != 2 && T < 1) return 0;
     if (stage == 3 && check_tree_size(B, T)) return 0;
-    return 256;
+    const int32_t N = stage == 2 ? 1 : std::min(T, d->max_seq);
+    return kv_attn_part_bound(KvAttnShape{stage >= 2 ? B : 1, N, d->n_kv_heads, n_heads / d->n_kv_heads, d->head_dim,
+                                          std::min(max_ctx, d->max_seq), INT_MAX, 0});
 }
 
 // Checks that the three attention calls share, and their launch.
@@ -1641,7 +1648,8 @@ static int kv_attn_run(const kv_desc* d, KvAttnArgs a, int32_t stage, int32_t wi
                        const void* kc, const void* vc, void* out, void* ws, size_t ws_bytes, void* stream) {
     int rc;
     if ((rc = check_kv_desc(d, a.B)) || (rc = check_kv_heads(d, n_heads)) || (rc = check_window(window, sinks))) return rc;
-    const long long slots = (long long)a.max_ctx + a.N;
+    const long long slots = (long long)a.max_ctx + a.N, rows = (long long)a.N * (n_heads / d->n_kv_heads);
+    if (rows > kKvMaxRows) return fail(W4_ECAPACITY, "%lld rows per kv head, at most %d", rows, kKvMaxRows);
     if (slots > d->max_seq) return fail(W4_ECAPACITY, "%lld slots, max_seq %d", slots, d->max_seq);
     if (!aligned16({q, kc, vc, out, ws})) return fail(W4_EINVAL, "pointers must be 16-byte aligned");
     if (q == out) return fail(W4_EINVAL, "q and out must not alias");
@@ -1661,7 +1669,8 @@ static int kv_attn_run(const kv_desc* d, KvAttnArgs a, int32_t stage, int32_t wi
     a.nkv = d->n_kv_heads;
     a.d = d->head_dim;
     a.scale = (float)(1.0 / std::sqrt((double)d->head_dim));
-    if (launch_kv_attn(a, (hipStream_t)stream))
+    a.part = (float*)ws;
+    if (launch_kv_attn(a, ws_bytes, (hipStream_t)stream))
         return fail(W4_EHIP, "kernel launch failed: %s", hipGetErrorString(hipGetLastError()));
     return W4_OK;
 }

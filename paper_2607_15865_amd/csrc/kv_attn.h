@@ -24,8 +24,21 @@ struct KvAttnArgs {
     uint16_t* out;           // bf16 [B][N][nq][d]
     int B, N, nq, nkv, d;
     float scale;             // of the scores
+    int nsplit;              // set by the launcher: shares of a row tile's keys
+    float* part;             // their states
 };
-int launch_kv_attn(const KvAttnArgs& a, hipStream_t stream);
+// What a plan depends on (r: query heads per kv head).
+struct KvAttnShape {
+    int B, N, nkv, r, d, max_ctx, window, sinks;
+};
+struct KvAttnPlan {
+    bool few = false;        // the kernel of few rows
+    int ct = 1, nsplit = 1;  // its column tiles; shares of a row tile's keys
+};
+KvAttnPlan kv_attn_plan(const KvAttnShape& s);
+size_t kv_attn_part_bytes(const KvAttnShape& s, const KvAttnPlan& p);
+size_t kv_attn_part_bound(const KvAttnShape& s);     // of any plan, window and sinks; grows with B, N and max_ctx
+int launch_kv_attn(const KvAttnArgs& a, size_t part_bytes, hipStream_t stream);
 
 struct KvSlotArgs {
     long long stride_b, stride_h, stride_s;
