@@ -555,7 +555,7 @@ int layer_set_kv_format(layer_t layer, int32_t format);
  * softmax statistics and sums are fp32; the weights are multiplied as bf16
  * pairs (2^-16), or, where many rows share the keys, rounded to bf16 (2^-8).
  * Deterministic.  *desc: head_dim 64 or 128, max_seq at most 2^27, strides that are multiples
- * of 8 elements (any order: stride_s need not be head_dim, and is at most 2^25), and that stay within `bytes`; cache, q and out pointers
+ * of 8 elements (any order: stride_s need not be head_dim, and is at most 2^24), and that stay within `bytes`; cache, q and out pointers
  * 16-byte aligned.  The calls check their arguments on the host before anything is
  * launched, are asynchronous on the stream, allocate nothing and may be captured
  * into a graph.

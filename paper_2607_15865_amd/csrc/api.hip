@@ -1596,7 +1596,7 @@ int kv4_attn_prefill(const kv4_desc* d, const void* q, int32_t T, int32_t hist_l
 // ---------------------------------------------------------------- attention over the bf16 cache, draft trees
 
 constexpr int kKvMaxRows = INT_MAX - 256;        // of a kv head: queries times heads, in whole tiles
-constexpr int64_t kKvMaxStride = 1 << 25;        // (64 slots' offsets fit 32 bits)
+constexpr int64_t kKvMaxStride = 1 << 24;        // (64 slots' offsets fit 32 bits)
 
 // B is the batch of a call on the cache; of a launch, at most 65535.
 static int check_kv_desc(const kv_desc* d, int32_t B) {
@@ -1604,7 +1604,7 @@ static int check_kv_desc(const kv_desc* d, int32_t B) {
     if (d->max_seq > kKv4MaxSeq) return fail(W4_EUNSUPPORTED, "max_seq must be at most 2^27");
     if (d->head_dim != 64 && d->head_dim != 128) return fail(W4_EUNSUPPORTED, "head_dim must be 64 or 128");
     const int64_t D = d->head_dim;
-    if (d->stride_s > kKvMaxStride) return fail(W4_EUNSUPPORTED, "stride_s must be at most 2^25");
+    if (d->stride_s > kKvMaxStride) return fail(W4_EUNSUPPORTED, "stride_s must be at most 2^24");
     if (d->stride_s < D || d->stride_h < D || d->stride_b < D || (d->stride_s | d->stride_h | d->stride_b) % 8)
         return fail(W4_EINVAL, "bad kv_desc strides");
     const __int128 last = (__int128)(d->batch - 1) * d->stride_b + (__int128)(d->n_kv_heads - 1) * d->stride_h +
@@ -1640,7 +1640,7 @@ size_t kv_attn_workspace_size(const kv_desc* d, int32_t n_heads, int32_t stage, 
     if (stage == 3 && check_tree_size(B, T)) return 0;
     const int32_t N = stage == 2 ? 1 : std::min(T, d->max_seq);
     return kv_attn_part_bound(KvAttnShape{stage >= 2 ? B : 1, N, d->n_kv_heads, n_heads / d->n_kv_heads, d->head_dim,
-                                          std::min(max_ctx, d->max_seq), INT_MAX, 0});
+                                          std::min(max_ctx, d->max_seq), INT_MAX, 0, stage == 3, false});
 }
 
 // Checks that the three attention calls share, and their launch.

@@ -24,16 +24,19 @@ struct KvAttnArgs {
     uint16_t* out;           // bf16 [B][N][nq][d]
     int B, N, nq, nkv, d;
     float scale;             // of the scores
-    int nsplit;              // set by the launcher: shares of a row tile's keys
+    int nsplit;              // set by the launcher: shares of a row tile's keys,
+    int whole, rest;         // many rows: of the tiles behind the first `whole`, `rest` in number
     float* part;             // their states
 };
 // What a plan depends on (r: query heads per kv head).
 struct KvAttnShape {
     int B, N, nkv, r, d, max_ctx, window, sinks;
+    bool tree, mask;
 };
 struct KvAttnPlan {
     bool few = false;        // the kernel of few rows
-    int ct = 1, nsplit = 1;  // its column tiles; shares of a row tile's keys
+    int ct = 1, nsplit = 1;  // its column tiles; shares of a row tile's keys,
+    int whole = 0;           // many rows: except for so many tiles
 };
 KvAttnPlan kv_attn_plan(const KvAttnShape& s);
 size_t kv_attn_part_bytes(const KvAttnShape& s, const KvAttnPlan& p);

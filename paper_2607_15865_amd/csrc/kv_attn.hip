@@ -12,7 +12,7 @@
 //
 // A value that is not finite must not reach rows that do not see its slot, as 0
 // times it would: where rows differ in what they see, such values are 0 in the
-// products, and the rows that do see them are set to NaN.
+// products, and the rows that do see them get a sum of weights that is NaN.
 #include <algorithm>
 #include <climits>
 
@@ -111,11 +111,11 @@ __device__ __forceinline__ u64 seen_bits(const KvAttnArgs& a, const RowView& v, 
 
 // ---------------------------------------------------------------- few rows
 
-constexpr int FW = 8;            // waves per block
 constexpr int FKT = 32;          // keys per tile
+constexpr int FW = 8;            // waves per block
 
 // One block: up to 16 CT rows of a (sequence, kv head) and a share of its key
-// tiles; wave w takes tiles w, w + 8, .. of the share on its own, so there is no
+// tiles; the waves take the tiles of the share in turn, each on its own, so there is no
 // barrier in the loop.  K goes from memory straight into the A operand of the
 // 16x16x32 MFMA, V through a swizzled LDS tile of the wave, out of which the
 // transposing read takes V^T; both are requested a tile ahead.  Scores are
@@ -126,8 +126,10 @@ constexpr int FKT = 32;          // keys per tile
 template <int D, int CT>
 __global__ void __launch_bounds__(64 * FW) kv_attn_few_kernel(KvAttnArgs a) {
     constexpr int NCK = D / 8, KROWS = 64 / NCK, NV = FKT / KROWS, NS = D / 32, NDB = D / 16, RT = 16 * CT;
+    constexpr bool QLDS = CT >= 2;                           // queries in LDS, not in registers
     extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
     __shared__ float gst[FW][RT][2];
+    u32x4* const Qs = reinterpret_cast<u32x4*>(smem + FW * 16 * D * 4);      // [CT][NS][64 lanes]
     const int tid = threadIdx.x, lane = tid & 63;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int hk = blockIdx.x % a.nkv, row0 = blockIdx.x / a.nkv * RT, part = blockIdx.y, b = blockIdx.z;
@@ -136,13 +138,18 @@ __global__ void __launch_bounds__(64 * FW) kv_attn_few_kernel(KvAttnArgs a) {
     int ctx = a.ctx_lens ? a.ctx_lens[b] : a.ctx_base;
 
     // ---- queries: column n16 of column tile ct is row row0 + 16 ct + n16, dims 32 s + 8 q4 .. + 7
-    u32x4 qw[CT][NS];
-#pragma unroll
-    for (int ct = 0; ct < CT; ct++) {
+    u32x4 qw[QLDS ? 1 : NS];
+    auto query = [&](int ct, int s) __attribute__((always_inline)) {
         const int row = min(row0 + 16 * ct + n16, R - 1);
-        const uint16_t* qp = a.q + (((size_t)b * a.N + row / r) * a.nq + hk * r + row % r) * D + 8 * q4;
+        return reinterpret_cast<const u32x4*>(a.q + (((size_t)b * a.N + row / r) * a.nq + hk * r + row % r) * D + 32 * s + 8 * q4);
+    };
+    if constexpr (QLDS) {
 #pragma unroll
-        for (int s = 0; s < NS; s++) qw[ct][s] = *reinterpret_cast<const u32x4*>(qp + 32 * s);
+        for (int i = 0; i < CT * NS; i += FW)
+            if (i + wave < CT * NS) Qs[(i + wave) * 64 + lane] = *query((i + wave) / NS, (i + wave) % NS);
+    } else {
+#pragma unroll
+        for (int s = 0; s < NS; s++) qw[s] = *query(0, s);
     }
     ctx = min(ctx, a.max_ctx);
 
@@ -190,11 +197,10 @@ __global__ void __launch_bounds__(64 * FW) kv_attn_few_kernel(KvAttnArgs a) {
         load_k(tile_at(kt, t) * FKT);
         load_v(tile_at(kt, t) * FKT);
     }
-    bf16x8 qf[CT][NS];
-#pragma unroll
-    for (int ct = 0; ct < CT; ct++)
-#pragma unroll
-        for (int s = 0; s < NS; s++) qf[ct][s] = __builtin_bit_cast(bf16x8, qw[ct][s]);
+    if constexpr (QLDS) __syncthreads();
+    auto qf = [&](int ct, int s) __attribute__((always_inline)) {
+        return __builtin_bit_cast(bf16x8, QLDS ? Qs[(ct * NS + s) * 64 + lane] : qw[QLDS ? 0 : s]);
+    };
 
     f32x4 o[CT][NDB];
     float m[CT], l[CT];
@@ -213,10 +219,12 @@ __global__ void __launch_bounds__(64 * FW) kv_attn_few_kernel(KvAttnArgs a) {
 #pragma unroll
         for (int s = 0; s < NS; s++)
 #pragma unroll
-            for (int h = 0; h < 2; h++)
+            for (int ct = 0; ct < CT; ct++) {
+                const bf16x8 q = qf(ct, s);
 #pragma unroll
-                for (int ct = 0; ct < CT; ct++)
-                    acc[ct][h] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, kr[h][s]), qf[ct][s], acc[ct][h], 0, 0, 0);
+                for (int h = 0; h < 2; h++)
+                    acc[ct][h] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, kr[h][s]), q, acc[ct][h], 0, 0, 0);
+            }
         float p[CT][8];
 #pragma unroll
         for (int ct = 0; ct < CT; ct++)
@@ -319,60 +327,54 @@ __global__ void __launch_bounds__(64 * FW) kv_attn_few_kernel(KvAttnArgs a) {
         if (bad) {
 #pragma unroll
             for (int ct = 0; ct < CT; ct++)
-                if (seen[ct] & bad)
-#pragma unroll
-                    for (int i = 0; i < NDB; i++)
-#pragma unroll
-                        for (int e = 0; e < 4; e++) o[ct][i][e] = __builtin_nanf("");
+                if (seen[ct] & bad) l[ct] = __builtin_nanf("");
         }
         __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
     }
 
-    // ---- the waves' states meet in LDS, over the V tiles
-    __syncthreads();
-    float* const ored = reinterpret_cast<float*>(smem);      // [FW][nr][D]
-#pragma unroll
-    for (int ct = 0; ct < CT; ct++) {
-        const int lr = 16 * ct + n16;
-        l[ct] = sum_quarters(l[ct]);
-        if (lr >= nr) continue;
-#pragma unroll
-        for (int db = 0; db < NDB; db++) *reinterpret_cast<f32x4*>(ored + (wave * nr + lr) * D + 16 * db + 4 * q4) = o[ct][db];
-        if (q4 == 0) {
-            gst[wave][lr][0] = m[ct];
-            gst[wave][lr][1] = l[ct];
-        }
-    }
-    __syncthreads();
+    // ---- the waves' states meet in LDS, over the V tiles, a column tile at a time
+    float* const ored = reinterpret_cast<float*>(smem);      // [FW][16][D]
     // one share: the output; more: its state, [(sequence, kv head)][share][R rows][D] outputs, then [..][R] (max, sum)
     const size_t slot = (((size_t)b * a.nkv + hk) * a.nsplit + part) * R + row0;
     float* const po = a.part + slot * D;
     float2* const pst = reinterpret_cast<float2*>(a.part + (size_t)a.B * a.nkv * a.nsplit * R * D) + slot;
-    for (int idx = tid; idx < nr * (D / 2); idx += 64 * FW) {
-        const int lr = idx / (D / 2), d = 2 * (idx % (D / 2));
-        float M = -INFINITY;
 #pragma unroll
-        for (int w = 0; w < FW; w++) M = fmaxf(M, gst[w][lr][0]);
-        const float Mb = M == -INFINITY ? 0.f : M;
-        float x = 0.f, y = 0.f, lt = 0.f;
+    for (int ct = 0; ct < CT; ct++) {
+        __syncthreads();
+        l[ct] = sum_quarters(l[ct]);
+        if (16 * ct + n16 < nr) {
 #pragma unroll
-        for (int w = 0; w < FW; w++) {
-            const float sc = exp2_hw((gst[w][lr][0] - Mb) * LOG2E), lw = gst[w][lr][1];
-            const float2 v = *reinterpret_cast<const float2*>(ored + (w * nr + lr) * D + d);
-            // (a wave whose scores were NaN alone has the maximum -inf and a NaN sum)
-            const bool on = sc != 0.f || lw != lw;
-            x += on ? (lw != lw ? lw : sc * v.x) : 0.f;
-            y += on ? (lw != lw ? lw : sc * v.y) : 0.f;
-            lt += on ? (lw != lw ? lw : sc * lw) : 0.f;
+            for (int db = 0; db < NDB; db++) *reinterpret_cast<f32x4*>(ored + (wave * 16 + n16) * D + 16 * db + 4 * q4) = o[ct][db];
+            if (q4 == 0) {
+                gst[wave][16 * ct + n16][0] = m[ct];
+                gst[wave][16 * ct + n16][1] = l[ct];
+            }
         }
-        if (a.nsplit == 1) {
-            const int row = row0 + lr;
-            const float u = lt == 0.f ? 0.f : x / lt, v = lt == 0.f ? 0.f : y / lt;
-            *reinterpret_cast<uint32_t*>(a.out + (((size_t)b * a.N + row / r) * a.nq + hk * r + row % r) * D + d) =
-                (uint32_t)bf16_bits_rne(u) | (uint32_t)bf16_bits_rne(v) << 16;
-        } else {
-            *reinterpret_cast<float2*>(po + 2 * idx) = float2{x, y};
-            if (d == 0) pst[lr] = float2{M, lt};
+        __syncthreads();
+        for (int idx = tid; idx < min(16, nr - 16 * ct) * (D / 2); idx += 64 * FW) {
+            const int lr = 16 * ct + idx / (D / 2), d = 2 * (idx % (D / 2));
+            float M = -INFINITY;
+#pragma unroll
+            for (int w = 0; w < FW; w++) M = fmaxf(M, gst[w][lr][0]);
+            const float Mb = M == -INFINITY ? 0.f : M;
+            float x = 0.f, y = 0.f, lt = 0.f;
+#pragma unroll
+            for (int w = 0; w < FW; w++) {
+                const float lw = gst[w][lr][1], sc = lw != lw ? lw : exp2_hw((gst[w][lr][0] - Mb) * LOG2E);   // (NaN stays)
+                const float2 v = *reinterpret_cast<const float2*>(ored + (w * 16 + lr % 16) * D + d);
+                x += sc == 0.f ? 0.f : sc * v.x;
+                y += sc == 0.f ? 0.f : sc * v.y;
+                lt += sc * lw;
+            }
+            if (a.nsplit == 1) {
+                const int row = row0 + lr;
+                const float u = lt == 0.f ? 0.f : x / lt, v = lt == 0.f ? 0.f : y / lt;
+                *reinterpret_cast<uint32_t*>(a.out + (((size_t)b * a.N + row / r) * a.nq + hk * r + row % r) * D + d) =
+                    (uint32_t)bf16_bits_rne(u) | (uint32_t)bf16_bits_rne(v) << 16;
+            } else {
+                *reinterpret_cast<float2*>(po + lr * D + d) = float2{x, y};
+                if (d == 0) pst[lr] = float2{M, lt};
+            }
         }
     }
 }
@@ -450,45 +452,61 @@ constexpr int MKT = 64;          // keys per stage
 template <int D>
 constexpr int M_NREG = 2 + 16 * (D / 32);    // floats of a lane's state: maximum, sum, output
 
+// 16 bytes a lane from src + off to LDS, 1 KB from dst on.  Written out, because before any LDS read the compiler
+// waits for every such load of its own builtin that is in flight; nothing but lds_load_wait waits for these, of which at most N
+// stay in flight then.  (No registers are written.  The compiler's own waits count these too, and so only wait longer.)
+__device__ __forceinline__ void lds_load16(const void* src, uint32_t off, uint32_t dst) {
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2"
+                 :: "s"(__builtin_amdgcn_readfirstlane(dst)), "v"(off), "s"(src) : "memory", "m0");
+}
+template <int N>
+__device__ __forceinline__ void lds_load_wait() {
+    asm volatile("s_waitcnt vmcnt(%0)" :: "i"(N) : "memory");
+}
+
 __device__ __forceinline__ int key_perm(int x) { return (x & ~12) | (x & 4) << 1 | (x & 8) >> 1; }   // swap bits 2 and 3
 
-// What is common to the rows of a block (and a merge).
+// What is common to the rows of a block (and a merge).  Row tiles are dealt out in this order: the last one (of a chain
+// the longest) of every (sequence, kv head), the one before, ..; the first a.whole of them in one part, the others in up to
+// a.nsplit.
 struct ManyTile {
     int b, hk, q, ctx;       // sequence, kv head, row tile, context
     KeyTiles kt;
     int end, high_min, low_max, n;   // n: parts of the tile
 };
-__device__ __forceinline__ ManyTile many_tile(const KvAttnArgs& a, int unit, int q) {
+__device__ __forceinline__ ManyTile many_tile(const KvAttnArgs& a, int order) {
     ManyTile t;
+    const int units = a.B * a.nkv, unit = order % units;
+    const int r = a.nq / a.nkv, R = a.N * r;
     t.b = unit / a.nkv;
     t.hk = unit % a.nkv;
-    t.q = q;
+    t.q = (R + MROWS - 1) / MROWS - 1 - order / units;
     t.ctx = min(a.ctx_lens ? a.ctx_lens[t.b] : a.ctx_base, a.max_ctx);
-    const int r = a.nq / a.nkv, R = a.N * r;
+    const int q = t.q;
     const int i0 = q * MROWS / r, i1 = (min((q + 1) * MROWS, R) - 1) / r;
     t.end = t.ctx < 0 ? -1 : a.tree ? t.ctx + a.N - 1 : t.ctx + i1;
     t.high_min = a.tree ? t.ctx - 1 : t.ctx + i0;
     t.low_max = window_low(a.tree ? t.ctx + a.N - 1 : t.ctx + i1, a.window);
     t.kt = key_tiles<MKT>(window_low(a.tree ? t.ctx : t.ctx + i0, a.window), t.end, a.sinks);
-    t.n = max(1, min(a.nsplit, t.kt.n));
+    t.n = order < a.whole ? 1 : max(1, min(a.nsplit, t.kt.n));
     return t;
 }
 
 template <int D>
 __global__ void __launch_bounds__(64 * MW) kv_attn_many_kernel(KvAttnArgs a) {
-    constexpr int NS = D / 32, NF = D / 16, NCH = D / 8, NL = MKT * NCH / (64 * MW);     // pieces per thread of K (of V)
+    constexpr int NS = D / 32, NF = D / 16, NCH = D / 8, NL = MKT * NCH / (64 * MW);     // loads per wave of K (of V)
     constexpr int STB = MKT * D * 2;
     extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
-    unsigned char* const Ks = smem;                          // [2 stages][64 keys][D]
-    unsigned char* const Vs = smem + 2 * STB;
-    u64* const vbad = reinterpret_cast<u64*>(smem + 4 * STB);   // [4] keys of V that are not finite, by stage % 4
+    unsigned char* const Ks = smem;                          // [4 stages][64 keys][D]
+    unsigned char* const Vs = smem + 4 * STB;
+    u64* const vbad = reinterpret_cast<u64*>(smem + 8 * STB);   // [4] keys of V that are not finite, by stage % 4
     const int tid = threadIdx.x, lane = tid & 63;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int h = lane >> 5, c = lane & 31;
-    const int units = a.B * a.nkv, unit = blockIdx.x % units, rest = blockIdx.x / units;
-    const int r = a.nq / a.nkv, R = a.N * r, nqt = (R + MROWS - 1) / MROWS;
-    const int part = rest % a.nsplit;
-    const ManyTile mt = many_tile(a, unit, nqt - 1 - rest / a.nsplit);       // (the last, longest ones first)
+    const int r = a.nq / a.nkv, R = a.N * r;
+    const int in = (int)blockIdx.x - a.whole;                // place among the parts
+    const int part = in < 0 ? 0 : in / a.rest;
+    const ManyTile mt = many_tile(a, in < 0 ? blockIdx.x : a.whole + in % a.rest);
     if (part >= mt.n) return;
     const int st0 = (int)((long long)mt.kt.n * part / mt.n), st1 = (int)((long long)mt.kt.n * (part + 1) / mt.n);
     const long long base = mt.b * a.stride_b + mt.hk * a.stride_h;
@@ -496,65 +514,40 @@ __global__ void __launch_bounds__(64 * MW) kv_attn_many_kernel(KvAttnArgs a) {
     const uint16_t* const vc = a.v + base;
     const uint32_t ss = (uint32_t)a.stride_s;
 
-    // piece j of this thread: row j 64 MW / NCH + tid / NCH, chunk tid % NCH
+    // load j of a wave: rows j LROWS + lrow, a lane the 16-byte chunk that belongs into the place lane % NCH
     constexpr int LROWS = 64 * MW / NCH;
-    const int lrow = tid / NCH, lch = tid % NCH;
+    const int lrow = tid / NCH, lch = lane % NCH;
     auto kswz = [](int row) { return D == 128 ? row & 15 : row >> 1 & 7; };
     auto vswz = [](int row) { return D == 128 ? 4 * (row & 3) : 4 * (row >> 1 & 1); };
-    u32x4 kr[NL], vr[NL];
-    auto load = [&](u32x4 (&x)[NL], const uint16_t* src, int st) __attribute__((always_inline)) {
-        const int kb = tile_at(mt.kt, st) * MKT, lim = mt.end - kb;      // (keys past the last one read that one)
-        const uint16_t* p = src + kb * a.stride_s;
+    const uint32_t smem0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) unsigned char*)smem;
+    const uint32_t klane = (lch ^ kswz(lrow)) * 16, vlane = (lch ^ vswz(lrow)) * 16, lrow_off = (uint32_t)lrow * ss * 2;
+    auto load = [&](const uint16_t* src, uint32_t lane_off, uint32_t dst, int st) __attribute__((always_inline)) {
+        const int kb = tile_at(mt.kt, st) * MKT, lim = mt.end - kb;
 #pragma unroll
-        for (int j = 0; j < NL; j++) x[j] = *reinterpret_cast<const u32x4*>(p + (uint32_t)min(j * LROWS + lrow, lim) * ss + lch * 8);
+        for (int j = 0; j < NL; j++) {
+            uint32_t off = lrow_off + (uint32_t)(j * LROWS) * ss * 2;
+            if (lim < MKT - 1) off = (uint32_t)min(j * LROWS + lrow, lim) * ss * 2;      // (keys past the last one read that one)
+            lds_load16(src + kb * a.stride_s, off + lane_off, smem0 + dst + (j * MW + wave) * 1024);
+        }
     };
     // some row of the block does not see some key of the stage
     auto mixed = [&](int st) {
         const int kb = tile_at(mt.kt, st) * MKT;
         return kb + MKT - 1 > mt.high_min || (kb < mt.low_max && kb + MKT > a.sinks);
     };
-    auto store_k = [&](int s) __attribute__((always_inline)) {
-#pragma unroll
-        for (int j = 0; j < NL; j++) {
-            const int row = j * LROWS + lrow;
-            *reinterpret_cast<u32x4*>(Ks + (s & 1) * STB + row * 2 * D + ((lch ^ kswz(row)) << 4)) = kr[j];
-        }
-    };
-    auto store_v = [&](int s) __attribute__((always_inline)) {
-        if (mixed(st0 + s)) {
-#pragma unroll
-            for (int j = 0; j < NL; j++)
-                if (not_finite(vr[j])) {
-                    atomicOr(vbad + (s & 3), 1ull << (j * LROWS + lrow));
-                    vr[j] = u32x4{0u, 0u, 0u, 0u};
-                }
-        }
-#pragma unroll
-        for (int j = 0; j < NL; j++) {
-            const int row = j * LROWS + lrow;
-            *reinterpret_cast<u32x4*>(Vs + (s & 1) * STB + row * 2 * D + ((lch ^ vswz(row)) << 4)) = vr[j];
-        }
-    };
 
     const int n = st1 - st0;
-    if (n > 0) load(kr, kc, st0);
     // ---- queries: this lane's row, dims 16 f + 8 h .. + 7 of every fragment f
     const int row = mt.q * MROWS + wave * 32 + c, rowc = min(row, R - 1);
     const uint16_t* qp = a.q + (((size_t)mt.b * a.N + rowc / r) * a.nq + mt.hk * r + rowc % r) * D + 8 * h;
     bf16x8 qf[NF];
 #pragma unroll
     for (int f = 0; f < NF; f++) qf[f] = *reinterpret_cast<const bf16x8*>(qp + 16 * f);
-    const RowView view = row_view(a, mt.b, rowc / r, mt.ctx);
     const bool active = mt.q * MROWS + wave * 32 < R;
     const float sl = a.scale * LOG2E;
-    // stages that none of the wave's rows sees (of a chain: their first and last positions)
+    // (of the wave's rows: what all see)
     const int wi0 = min(mt.q * MROWS + wave * 32, R - 1) / r, wi1 = min(mt.q * MROWS + wave * 32 + 31, R - 1) / r;
-    const int w_low = window_low(a.tree ? mt.ctx : mt.ctx + wi0, a.window), w_high = a.tree ? mt.end : mt.ctx + wi1;
     const int w_low_max = window_low(a.tree ? mt.ctx + a.N - 1 : mt.ctx + wi1, a.window), w_high_min = a.tree ? mt.ctx - 1 : mt.ctx + wi0;
-    auto on = [&](int st) {
-        const int kb = tile_at(mt.kt, st) * MKT;
-        return active && kb <= w_high && (kb + MKT > w_low || kb < a.sinks);
-    };
 
     f32x16 o[NS];
 #pragma unroll
@@ -562,110 +555,153 @@ __global__ void __launch_bounds__(64 * MW) kv_attn_many_kernel(KvAttnArgs a) {
     float m = -INFINITY, l = 0.f;
 
     if (n > 0) {
-        if (tid < 4) vbad[tid] = 0;
-        store_k(0);
-        if (n > 1) load(kr, kc, st0 + 1);
-        load(vr, vc, st0);
-        __syncthreads();
-        int next = 0;                                        // K of stage next + 1 and V of stage next go to LDS
-        auto store_next = [&]() __attribute__((always_inline)) {
-            if (next + 1 < n) store_k(next + 1);
-            if (next < n) store_v(next);
-            if (next + 2 < n) load(kr, kc, st0 + next + 2);
-            if (next + 1 < n) load(vr, vc, st0 + next + 1);
-            next++;
+        // K of stage s + 3 and V of stage s + 2, of the block's part
+        auto load_ahead = [&](int s) __attribute__((always_inline)) {
+            if (s + 3 < n) load(kc, klane, (s + 3 & 3) * STB, st0 + s + 3);
+            if (s + 2 < n) load(vc, vlane, (4 + (s + 2 & 3)) * STB, st0 + s + 2);
         };
-        if (wave >= MW / 2) {                                // half a stage behind: vector work where the others multiply
-            store_next();
-            __syncthreads();
-        }
+        // waits until K of stage s + 1 and V of stage s are there, after load_ahead(s)
+        auto wait_for = [&](int s) __attribute__((always_inline)) {
+            if (s + 3 < n) lds_load_wait<4 * NL>();
+            else if (s + 3 == n) lds_load_wait<3 * NL>();
+            else if (s + 2 == n) lds_load_wait<NL>();
+            else lds_load_wait<0>();
+        };
+        load(kc, klane, 0, st0);
+        load_ahead(-2);
+        load_ahead(-1);
+        if (tid < 4) vbad[tid] = 0;
+#pragma unroll
+        for (int j = 0; j < NL; j++) *reinterpret_cast<u32x4*>(Vs + 3 * STB + (j * 64 * MW + tid) * 16) = u32x4{0u, 0u, 0u, 0u};
         const int krow = key_perm(c);
+        f32x16 sc[2];
         bf16x8 pf[4];
-#pragma clang loop unroll(disable)
-        for (int s = 0; s <= n; s++) {
-            // ---- matrix half: scores of stage s, output of stage s - 1
-            f32x16 sc[2];
-            const bool now = s < n && on(st0 + s);
-            if (now) {
-                const unsigned char* K = Ks + (s & 1) * STB;
-                sc[0] = f32x16{};
-                sc[1] = f32x16{};
+        auto scores = [&](int s) __attribute__((always_inline)) {
+            const unsigned char* K = Ks + (s & 3) * STB;
+            sc[0] = f32x16{};
+            sc[1] = f32x16{};
 #pragma unroll
-                for (int f = 0; f < NF; f++)
+            for (int f = 0; f < NF; f++)
 #pragma unroll
-                    for (int t = 0; t < 2; t++) {
-                        const bf16x8 kf = *reinterpret_cast<const bf16x8*>(K + (32 * t + krow) * 2 * D + (((2 * f + h) ^ kswz(krow)) << 4));
-                        sc[t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf, qf[f], sc[t], 0, 0, 0);
-                    }
-            }
-            if (s > 0 && on(st0 + s - 1)) {
-                const __bf16* V = reinterpret_cast<const __bf16*>(Vs + (s - 1 & 1) * STB);
-                // this lane's 8 keys 16 ks + 8 h .. + 7, dim 32 i + c, by two transposing reads: lane x of a 16-lane group
-                // points at key 16 ks + 8 h + x / 4 (+ 4), dims 32 i + 16 (c / 16) + 4 (x % 4) .. + 3
-                const int vrow = 8 * h + ((lane & 15) >> 2), vch = 2 * (c >> 4) + ((lane & 3) >> 1);
+                for (int t = 0; t < 2; t++) {
+                    const bf16x8 kf = *reinterpret_cast<const bf16x8*>(K + (32 * t + krow) * 2 * D + (((2 * f + h) ^ kswz(krow)) << 4));
+                    sc[t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf, qf[f], sc[t], 0, 0, 0);
+                }
+        };
+        // this lane's 8 keys 16 ks + 8 h .. + 7, dim 32 i + c, by two transposing reads: lane x of a 16-lane group points at
+        // key 16 ks + 8 h + x / 4 (+ 4), dims 32 i + 16 (c / 16) + 4 (x % 4) .. + 3
+        const int vrow = 8 * h + ((lane & 15) >> 2), vch = 2 * (c >> 4) + ((lane & 3) >> 1);
+        auto output = [&](int s) __attribute__((always_inline)) {
+            const __bf16* V = reinterpret_cast<const __bf16*>(Vs + (s & 3) * STB);
 #pragma unroll
-                for (int ks = 0; ks < 4; ks++)
+            for (int ks = 0; ks < 4; ks++)
 #pragma unroll
-                    for (int i = 0; i < NS; i++) {
-                        const __bf16* p0 = V + (16 * ks + vrow) * D + (((4 * i + vch) ^ vswz(vrow)) << 3) + 4 * (lane & 1);
-                        const __bf16* p1 = V + (16 * ks + vrow + 4) * D + (((4 * i + vch) ^ vswz(vrow + 4)) << 3) + 4 * (lane & 1);
-                        const i16x4 v0 = lds_read_tr16(p0), v1 = lds_read_tr16(p1);
-                        const bf16x8 vf = __builtin_bit_cast(bf16x8, __builtin_shufflevector(v0, v1, 0, 1, 2, 3, 4, 5, 6, 7));
-                        o[i] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf, pf[ks], o[i], 0, 0, 0);
-                    }
-                const u64 bad = vbad[s - 1 & 3];
-                if (bad != 0 && (seen_bits(a, view, mt.ctx, tile_at(mt.kt, st0 + s - 1) * MKT) & bad) != 0) {
+                for (int i = 0; i < NS; i++) {
+                    const __bf16* p0 = V + (16 * ks + vrow) * D + (((4 * i + vch) ^ vswz(vrow)) << 3) + 4 * (lane & 1);
+                    const __bf16* p1 = V + (16 * ks + vrow + 4) * D + (((4 * i + vch) ^ vswz(vrow + 4)) << 3) + 4 * (lane & 1);
+                    const i16x4 v0 = lds_read_tr16(p0), v1 = lds_read_tr16(p1);
+                    const bf16x8 vf = __builtin_bit_cast(bf16x8, __builtin_shufflevector(v0, v1, 0, 1, 2, 3, 4, 5, 6, 7));
+                    o[i] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf, pf[ks], o[i], 0, 0, 0);
+                }
+        };
+        // NaN for the rows that see a value of stage s that is not finite (they may not be 0 times it to the others)
+        auto poison = [&](int s) __attribute__((always_inline)) {
+            if (!mixed(st0 + s)) return;
+            const u64 bad = vbad[s & 3];
+            if (bad != 0 && (seen_bits(a, row_view(a, mt.b, rowc / r, mt.ctx), mt.ctx, tile_at(mt.kt, st0 + s) * MKT) & bad) != 0)
+                l = __builtin_nanf("");
+        };
+        // V of stage s, the pieces that this wave has loaded: keys that are not finite are noted, and 0 in the products
+        auto check_v = [&](int s) __attribute__((always_inline)) {
+            if (s >= n || !mixed(st0 + s)) return;
 #pragma unroll
-                    for (int i = 0; i < NS; i++)
-#pragma unroll
-                        for (int e = 0; e < 16; e++) o[i][e] = __builtin_nanf("");
+            for (int j = 0; j < NL; j++) {
+                u32x4* const x = reinterpret_cast<u32x4*>(Vs + (s & 3) * STB + (j * MW + wave) * 1024 + lane * 16);
+                if (not_finite(*x)) {
+                    atomicOr(vbad + (s & 3), 1ull << (j * LROWS + lrow));
+                    *x = u32x4{0u, 0u, 0u, 0u};
                 }
             }
-            if (s == n) break;
-            __syncthreads();
-            // ---- vector half: weights of stage s, the next tiles
-            if (tid == 0) vbad[s + 1 & 3] = 0;               // (the list of stage s - 3)
-            if (now) {
-                const int kb = tile_at(mt.kt, st0 + s) * MKT;
-                float p[32];
+        };
 #pragma unroll
-                for (int e = 0; e < 32; e++) p[e] = sc[e / 16][e % 16];
-                if (kb + MKT - 1 > w_high_min || (kb < w_low_max && kb + MKT > a.sinks)) {
-                    const u64 seen = seen_bits(a, view, mt.ctx, kb) >> (8 * h);
-                    const uint32_t lo = (uint32_t)seen, hi = (uint32_t)(seen >> 32);
+        for (int i = 0; i < 4; i++) pf[i] = bf16x8{};
 #pragma unroll
-                    for (int e = 0; e < 32; e++)
-                        p[e] = (e < 16 ? lo : hi) >> (16 * (e % 16 / 8) + e % 8) & 1 ? p[e] : -INFINITY;
-                }
-                float mt2 = fmaxf(p[0], p[1]);
-#pragma unroll
-                for (int e = 2; e < 32; e++) mt2 = fmaxf(mt2, p[e]);
-                if (__builtin_amdgcn_ballot_w64(mt2 * sl > m + 8.f) != 0) {
-                    const float mn = fmaxf(m, max_halves(mt2) * sl);
-                    const float alpha = exp2_hw(m - (mn == -INFINITY ? 0.f : mn));
-                    l *= alpha;
-#pragma unroll
-                    for (int i = 0; i < NS; i++)
-#pragma unroll
-                        for (int e = 0; e < 16; e++) o[i][e] *= alpha;
-                    m = mn;
-                }
-                const float mb = m == -INFINITY ? 0.f : m;
-                float ls[4] = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-                for (int e = 0; e < 32; e += 2) {
-                    const float x = exp2_hw(__builtin_fmaf(p[e], sl, -mb)), y = exp2_hw(__builtin_fmaf(p[e + 1], sl, -mb));
-                    ls[e / 2 % 2] += x;
-                    ls[2 + e / 2 % 2] += y;
-                    const bf16x2 w = __builtin_convertvector(f32x2{x, y}, bf16x2);
-                    pf[e / 8][e % 8] = w[0];
-                    pf[e / 8][e % 8 + 1] = w[1];
-                }
-                l += (ls[0] + ls[1]) + (ls[2] + ls[3]);
-            }
-            store_next();
+        for (int f = 0; f < NF; f++) asm volatile("" : "+v"(qf[f]));         // (waited for here, not in the loop)
+        wait_for(-1);                                        // (K of stage 0)
+        __syncthreads();
+        // The second half of the waves runs half a stage behind: vector work where the others multiply.  What it loads has
+        // to be there for the others too, so it takes that part a stage earlier.
+        const int early = wave >= MW / 2;
+        if (early) {
+            load_ahead(0);
+            wait_for(0);
+            check_v(0);
             __syncthreads();
         }
+#pragma clang loop unroll(disable)
+        for (int s = 0; s < n; s++) {
+            // ---- matrix half: scores of stage s, output of stage s - 1 (of the first: weights and values 0).  Operands are read
+            // some products ahead: left to itself the compiler waits for every pair of them.
+            scores(s);
+            output(s - 1);
+            constexpr int DS = 0x100, MFMA = 0x008;          // (classes of the scheduler's groups)
+            __builtin_amdgcn_sched_group_barrier(DS, 6, 0);
+#pragma unroll
+            for (int j = 0; j < 2 * NF - 6; j++) {
+                __builtin_amdgcn_sched_group_barrier(MFMA, 1, 0);
+                __builtin_amdgcn_sched_group_barrier(DS, 1, 0);
+            }
+#pragma unroll
+            for (int j = 0; j < 4 * NS; j++) {
+                __builtin_amdgcn_sched_group_barrier(MFMA, 1, 0);
+                __builtin_amdgcn_sched_group_barrier(DS, 2, 0);
+            }
+            __builtin_amdgcn_sched_group_barrier(MFMA, 6, 0);
+            if (s > 0) poison(s - 1);
+            __syncthreads();
+            // ---- vector half: weights of stage s, the tiles to come
+            load_ahead(s + early);
+            if (tid == 0) vbad[s + 1 & 3] = 0;               // (the list of stage s - 3)
+            const int kb = tile_at(mt.kt, st0 + s) * MKT;
+            if (kb + MKT - 1 > w_high_min || (kb < w_low_max && kb + MKT > a.sinks)) {
+                const u64 seen = seen_bits(a, row_view(a, mt.b, rowc / r, mt.ctx), mt.ctx, kb) >> (8 * h);
+                const uint32_t lo = (uint32_t)seen, hi = (uint32_t)(seen >> 32);
+#pragma unroll
+                for (int e = 0; e < 32; e++)
+                    sc[e / 16][e % 16] = (e < 16 ? lo : hi) >> (16 * (e % 16 / 8) + e % 8) & 1 ? sc[e / 16][e % 16] : -INFINITY;
+            }
+            float top = fmaxf(sc[0][0], sc[0][1]);
+#pragma unroll
+            for (int e = 2; e < 32; e++) top = fmaxf(top, sc[e / 16][e % 16]);
+            if (__builtin_amdgcn_ballot_w64(top * sl > m + 8.f) != 0) {
+                const float mn = fmaxf(m, max_halves(top) * sl);
+                const float alpha = exp2_hw(m - (mn == -INFINITY ? 0.f : mn));
+                l *= alpha;
+#pragma unroll
+                for (int i = 0; i < NS; i++)
+#pragma unroll
+                    for (int e = 0; e < 16; e++) o[i][e] *= alpha;
+                m = mn;
+            }
+            const float mb = m == -INFINITY ? 0.f : m;
+            float ls[2] = {0.f, 0.f};
+#pragma unroll
+            for (int e = 0; e < 32; e += 2) {
+                const float x = exp2_hw(__builtin_fmaf(sc[e / 16][e % 16], sl, -mb));
+                const float y = exp2_hw(__builtin_fmaf(sc[e / 16][e % 16 + 1], sl, -mb));
+                ls[0] += x;
+                ls[1] += y;
+                const bf16x2 w = __builtin_convertvector(f32x2{x, y}, bf16x2);
+                pf[e / 8][e % 8] = w[0];
+                pf[e / 8][e % 8 + 1] = w[1];
+            }
+            l += ls[0] + ls[1];
+            wait_for(s + early);
+            check_v(s + early);
+            __syncthreads();
+        }
+        output(n - 1);
+        poison(n - 1);
         if (wave < MW / 2) __syncthreads();
     }
     const float lt = l + __shfl_xor(l, 32, 64);
@@ -683,7 +719,7 @@ __global__ void __launch_bounds__(64 * MW) kv_attn_many_kernel(KvAttnArgs a) {
         return;
     }
     if (!active) return;
-    float* pp = a.part + ((size_t)blockIdx.x * MW + wave) * M_NREG<D> * 64 + lane;       // state of this part
+    float* pp = a.part + ((size_t)in * MW + wave) * M_NREG<D> * 64 + lane;       // state of this part
     pp[0] = m;
     pp[64] = l;
 #pragma unroll
@@ -692,15 +728,14 @@ __global__ void __launch_bounds__(64 * MW) kv_attn_many_kernel(KvAttnArgs a) {
         for (int e = 0; e < 16; e++) pp[(2 + i * 16 + e) * 64] = o[i][e];
 }
 
-// Merges the parts of the row tiles that have more than one: block (row tile and unit, 32-dim slice), thread
-// (wave, lane) the lane's registers of the slice, part after part in key order.
+// Merges the parts of the row tiles that have more than one: block (row tile, wave of it, 32-dim slice), a lane its
+// registers of the slice, part after part in key order.
 template <int D>
-__global__ void __launch_bounds__(64 * MW) kv_attn_many_merge_kernel(KvAttnArgs a) {
-    constexpr int CB = 4;                                    // parts requested together
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, h = lane >> 5, c = lane & 31, i = blockIdx.y;
-    const int units = a.B * a.nkv, unit = blockIdx.x % units, back = blockIdx.x / units;
-    const int r = a.nq / a.nkv, R = a.N * r, nqt = (R + MROWS - 1) / MROWS;
-    const ManyTile mt = many_tile(a, unit, nqt - 1 - back);
+__global__ void __launch_bounds__(64) kv_attn_many_merge_kernel(KvAttnArgs a) {
+    constexpr int CB = 8;                                    // parts requested together
+    const int lane = threadIdx.x, wave = blockIdx.y, h = lane >> 5, c = lane & 31, i = blockIdx.z;
+    const int r = a.nq / a.nkv, R = a.N * r;
+    const ManyTile mt = many_tile(a, a.whole + blockIdx.x);
     const int row = mt.q * MROWS + wave * 32 + c;
     if (mt.n == 1 || mt.q * MROWS + wave * 32 >= R) return;
     float M = -INFINITY, L = 0.f, acc[16] = {};
@@ -708,8 +743,7 @@ __global__ void __launch_bounds__(64 * MW) kv_attn_many_merge_kernel(KvAttnArgs 
         float mc[CB], lc[CB], v[CB][16];
 #pragma unroll
         for (int j = 0; j < CB; j++) {
-            const size_t block = (size_t)(back * a.nsplit + min(p0 + j, mt.n - 1)) * units + unit;
-            const float* pp = a.part + (block * MW + wave) * M_NREG<D> * 64 + lane;
+            const float* pp = a.part + (((size_t)min(p0 + j, mt.n - 1) * a.rest + blockIdx.x) * MW + wave) * M_NREG<D> * 64 + lane;
             mc[j] = pp[0];
             lc[j] = pp[64];
 #pragma unroll
@@ -746,37 +780,100 @@ __global__ void __launch_bounds__(64 * MW) kv_attn_many_merge_kernel(KvAttnArgs 
 
 }  // namespace
 
-constexpr int kFewRows = 64;             // at most, for the kernel of few rows
-constexpr int kFewBlocks = 512, kManyParts = 512;   // of a call that has more than one share (part) per tile
+constexpr int kFewBlocks = 512, kManyParts = 512;    // of a call whose row tiles have more than one share (part)
 
-// Slots from the lowest that a row may see to the last, of the longest sequence.
-static KeyTiles longest(const KvAttnShape& s, int kt) {
-    const int end = s.max_ctx + s.N - 1, low = window_low(s.max_ctx, s.window);
-    return kt == FKT ? key_tiles<FKT>(low, end, s.sinks) : key_tiles<MKT>(low, end, s.sinks);
+// Tiles (of KT keys) that the longest sequence's queries i0 .. i1 see.
+template <int KT>
+static int tiles_of(const KvAttnShape& s, long long i0, long long i1) {
+    return key_tiles<KT>(window_low((int)(s.max_ctx + i0), s.window), (int)(s.max_ctx + i1), s.sinks).n;
 }
 
+// The way of the least estimated time, in us; both kernels split a tile's keys where the grid would leave CUs idle.
+//
+// Few rows: a wave takes w a tile, most of it the latency of its memory, and more with the chip full; a block takes 4 (6.5) to begin
+// and end, a second share the merge launch; a CU draws 35 GB/s, the chip 5.3 TB/s from memory and 8.2 through its L2. Many rows: 1.45 a stage of one block, 1.75 with the chip full, 5 to begin and end (9 where the last stages are a tree's), and
+// the parts' states, written and read back; the row tiles that are left after the last full round of the chip
+// may be cut alone.  Measured (few rows with one, two column tiles; many): 32 heads of 8 of 128, 1 sequence of 8190 tokens, 8 drafts
+// 17.7, 22.2 and 31.9; 16 22.1, 22.7 and 32.4; 64 55, 38.9 and 36.4; 16 sequences of 4000, 13 drafts 99, 64 and 72; 28 heads of 4, 8 of
+// 2000, 32 drafts -, 35 and 27.7, 8001 queries, 876 row tiles in one part 477, the last 108 in two 454.
+// Four column tiles (64 rows, four waves of 512 registers) were slower than two tiles of two everywhere: 16 drafts behind 8190 30.6,
+// 13 behind 4000 66 to 89.
 KvAttnPlan kv_attn_plan(const KvAttnShape& s) {
-    KvAttnPlan p;
+    KvAttnPlan best;
+    double least = -1;
     const long long R = (long long)s.N * s.r, pairs = (long long)s.B * s.nkv;
-    p.few = R <= kFewRows;
-    if (p.few) {
-        p.ct = R <= 16 ? 1 : 2;
-        const long long tiles = longest(s, FKT).n, blocks = pairs * ((R + 16 * p.ct - 1) / (16 * p.ct));
-        const long long n = tiles < 32 ? 1 : std::min((p.ct == 1 ? 2 : 1) * kCus / blocks, (tiles + FW - 1) / FW);
-        p.nsplit = (int)std::max(1ll, n);
-        return p;
+    const bool wide = s.d == 128;
+    auto consider = [&](double us, bool few, int ct, long long n, long long whole) {
+        if (least >= 0 && us >= least) return;
+        least = us;
+        best.few = few;
+        best.ct = ct;
+        best.nsplit = (int)n;
+        best.whole = (int)whole;
+    };
+    auto step = [](long long n) { return n < 8 ? n + 1 : n + n / 4; };
+    const int most32 = tiles_of<FKT>(s, 0, s.N - 1);
+    for (int ct = 1; ct <= (R > 16 ? 2 : 1); ct++) {
+        const long long tiles = (R + 16 * ct - 1) / (16 * ct), blocks = pairs * tiles;
+        const long long slots = (!wide && ct == 1 ? 2 : 1) * kCus;
+        const double bytes = (double)blocks * most32 * FKT * s.d * 4;        // through the L2; from memory:
+        const double floor = std::max(bytes / 8.2e6, bytes / tiles / 5.3e6);
+        for (long long n = 1; n <= most32 && (n == 1 || blocks * n <= kFewBlocks); n = step(n)) {
+            const double w = (ct == 1 ? 2.1 : 2.5) * (blocks * n > kCus / 2 ? 1.25 : 1.0) * (wide ? 1.0 : 0.55);
+            const long long per = ((most32 + n - 1) / n + FW - 1) / FW;
+            const double us = std::max((double)((blocks * n + slots - 1) / slots) * (per * w + (ct == 1 ? 4.0 : 6.5) * (wide ? 1.0 : 0.75)),
+                                       std::max(floor, bytes / (std::min(blocks * n, slots) * 35e3)));
+            consider(us + (n > 1 ? 2.8 + 0.05 * n : 0.0), true, ct, n, 0);
+        }
     }
-    const long long stages = longest(s, MKT).n, blocks = pairs * ((R + MROWS - 1) / MROWS);
-    const long long n = std::min(2 * kCus / blocks, stages / 4);
-    p.nsplit = (int)std::max(1ll, n);
-    return p;
+    if (R <= 32 || s.mask) return best;                      // (masks are the kernel of few rows' alone)
+    const long long nqt = (R + MROWS - 1) / MROWS, blocks = pairs * nqt;
+    double sum = 0;                                          // stages of a row tile: mean of some, and the longest
+    int longest = 0;
+    const int samples = (int)std::min<long long>(nqt, 8);
+    for (int j = 0; j < samples; j++) {
+        const long long q = nqt - 1 - j * (nqt - 1) / std::max(samples - 1, 1);
+        const long long i0 = s.tree ? 0 : q * MROWS / s.r, i1 = s.tree ? s.N - 1 : (std::min((q + 1) * MROWS, R) - 1) / s.r;
+        const int t = tiles_of<MKT>(s, i0, i1);
+        sum += t;
+        longest = std::max(longest, t);
+    }
+    const double mean = sum / samples, t1 = wide ? 1.45 : 1.2, tf = 1.2 * t1, start = s.tree ? 9.0 : 5.0;
+    const double state = std::min<double>(R, MROWS) * (s.d + 4) * 4 * 2 / 5e6;
+    auto rounds = [&](long long n, long long parts) {        // us of so many blocks, a row tile in n parts
+        const double t = parts <= kCus / 2 ? t1 : tf, part = (double)longest / n * t + start;
+        if (parts <= kCus) return part;
+        if (mean > 0.9 * longest) return (double)((parts + kCus - 1) / kCus) * part;
+        return std::max(part, parts * (mean / n * t + start) / kCus + 0.5 * mean / n * t);      // (the longest go first)
+    };
+    const long long full = blocks / kCus * kCus;
+    for (long long n = 1; n <= longest && (n == 1 || (blocks - full) * n <= kManyParts); n = step(n)) {
+        if (n == 1) consider(rounds(1, blocks), false, 0, 1, blocks);
+        if (n > 1 && blocks * n <= kManyParts) consider(rounds(n, blocks * n) + 3.0 + blocks * n * state, false, 0, n, 0);
+        if (n > 1 && full > 0 && full < blocks)
+            consider(rounds(1, full) + rounds(n, (blocks - full) * n) + 3.0 + (blocks - full) * n * state, false, 0, n, full);
+    }
+    return best;
+}
+
+// (for the host tests)
+extern "C" void w4_kv_attn_plan(int B, int N, int nkv, int r, int d, int max_ctx, int window, int sinks, int tree, int* few, int* ct,
+                                int* nsplit, int* whole, size_t* part, size_t* bound) {
+    const KvAttnShape s{B, N, nkv, r, d, max_ctx, window ? window : INT_MAX, window ? sinks : 0, tree != 0, false};
+    const KvAttnPlan p = kv_attn_plan(s);
+    *few = p.few;
+    *ct = p.ct;
+    *nsplit = p.nsplit;
+    *whole = p.whole;
+    *part = kv_attn_part_bytes(s, p);
+    *bound = kv_attn_part_bound(s);
 }
 
 size_t kv_attn_part_bytes(const KvAttnShape& s, const KvAttnPlan& p) {
     const size_t R = (size_t)s.N * s.r, pairs = (size_t)s.B * s.nkv;
     if (p.nsplit == 1) return 0;
     if (p.few) return pairs * p.nsplit * R * (s.d + 2) * 4;
-    return pairs * p.nsplit * ((R + MROWS - 1) / MROWS) * MROWS * (s.d + 4) * 4;
+    return (pairs * ((R + MROWS - 1) / MROWS) - p.whole) * p.nsplit * MROWS * (s.d + 4) * 4;
 }
 
 // (either kernel's; a product of what grows, and a constant)
@@ -790,7 +887,7 @@ size_t kv_attn_part_bound(const KvAttnShape& s) {
 template <int D, int CT>
 static int launch_few(const KvAttnArgs& a, hipStream_t stream) {
     const int R = a.N * (a.nq / a.nkv), tiles = (R + 16 * CT - 1) / (16 * CT);
-    const size_t lds = (size_t)FW * std::max(FKT * D * 2, std::min(R, 16 * CT) * D * 4);
+    const size_t lds = (size_t)FW * 16 * D * 4 + (CT >= 2 ? CT * 16 * D * 2 : 0);     // V tiles, outputs over them; queries
     static LdsLimit lim;
     if (ensure_lds_limit(lim, (const void*)kv_attn_few_kernel<D, CT>, lds)) return -1;
     hipLaunchKernelGGL((kv_attn_few_kernel<D, CT>), dim3(a.nkv * tiles, a.nsplit, a.B), dim3(64 * FW), lds, stream, a);
@@ -802,21 +899,25 @@ template <int D>
 static int launch_many(const KvAttnArgs& a, hipStream_t stream) {
     const int R = a.N * (a.nq / a.nkv);
     const long long tiles = (long long)a.B * a.nkv * ((R + MROWS - 1) / MROWS);
-    if (tiles * a.nsplit > INT_MAX) return -1;
-    const size_t lds = (size_t)4 * MKT * D * 2 + 4 * 8;
+    KvAttnArgs x = a;
+    x.rest = (int)(tiles - a.whole);
+    const long long blocks = a.whole + (long long)x.rest * a.nsplit;
+    if (tiles > INT_MAX || x.rest < 0 || blocks > INT_MAX) return -1;
+    const size_t lds = (size_t)8 * MKT * D * 2 + 4 * 8;
     static LdsLimit lim;
     if (ensure_lds_limit(lim, (const void*)kv_attn_many_kernel<D>, lds)) return -1;
-    hipLaunchKernelGGL(kv_attn_many_kernel<D>, dim3((unsigned)(tiles * a.nsplit)), dim3(64 * MW), lds, stream, a);
-    if (a.nsplit > 1) hipLaunchKernelGGL(kv_attn_many_merge_kernel<D>, dim3((unsigned)tiles, D / 32), dim3(64 * MW), 0, stream, a);
+    hipLaunchKernelGGL(kv_attn_many_kernel<D>, dim3((unsigned)blocks), dim3(64 * MW), lds, stream, x);
+    if (x.rest) hipLaunchKernelGGL(kv_attn_many_merge_kernel<D>, dim3(x.rest, MW, D / 32), dim3(64), 0, stream, x);
     return hipGetLastError() == hipSuccess ? 0 : -1;
 }
 
 int launch_kv_attn(const KvAttnArgs& args, size_t part_bytes, hipStream_t stream) {
     KvAttnArgs a = args;
-    const KvAttnShape s{a.B, a.N, a.nkv, a.nq / a.nkv, a.d, a.max_ctx, a.window, a.sinks};
+    const KvAttnShape s{a.B, a.N, a.nkv, a.nq / a.nkv, a.d, a.max_ctx, a.window, a.sinks, a.tree != nullptr, a.mask != nullptr};
     const KvAttnPlan p = kv_attn_plan(s);
     if (kv_attn_part_bytes(s, p) > part_bytes || (a.mask && a.N != 1)) return -1;
     a.nsplit = p.nsplit;
+    a.whole = p.whole;
     if (p.few) {
         if (p.ct == 1) return a.d == 128 ? launch_few<128, 1>(a, stream) : launch_few<64, 1>(a, stream);
         return a.d == 128 ? launch_few<128, 2>(a, stream) : launch_few<64, 2>(a, stream);

@@ -111,7 +111,7 @@ def test_decode_flat_and_sharp_scores(scale):
 
 
 @pytest.mark.parametrize("window,sinks", [(0, 0), (200, 4), (200, 300)])
-@pytest.mark.parametrize("nq,nkv,d", [(14, 2, 64), (32, 8, 128), (40, 2, 128)])
+@pytest.mark.parametrize("nq,nkv,d", [(14, 2, 64), (32, 8, 128), (40, 2, 128), (64, 1, 128), (45, 1, 64)])
 def test_decode_mask(nq, nkv, d, window, sinks):
     """Additive masks: padded on the left, scattered, nothing left, finite values; what is hidden holds NaN."""
     log(f"mask heads {nq} {nkv} {d} window {window} sinks {sinks}")
