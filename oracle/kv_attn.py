@@ -33,11 +33,12 @@ def attend(q, k, v, seen, add=None, w_eps: float = 2.0 ** -16):
       a score is off by at most e = (d + 16) 2^-23 max_j (|q| . |k_j|) / sqrt(d) + 2^-21 max_j |z_j| (an addition is off by
       at most 2^-23 whatever its order; scaling, mask and the exponential's argument take a few operations);
       with every score off by at most e, a weight is off by a factor within exp(2 e), and so
-      |error| <= sum_j w_j |v_j| (expm1(2 e) + w_eps + (n / 16 + 96) 2^-24 + 2^-14) + 2^-24 max|v|,
+      |error| <= sum_j w_j |v_j| (expm1(2 e) + w_eps + (n / 16 + 96) 2^-24 + 2^-14) + |out| w_eps + 2^-24 max|v|,
+      the |out| w_eps where the sum that divides is of the rounded weights (sum_j w_j d_j (v_j - out), |d_j| <= w_eps),
       the last terms for the sums over n keys, of which a matrix instruction does 16 and more at a time, the
       exponential, the joining of parts and weights below fp32's range.
     spread is the standard deviation of the error that the weights' rounding alone makes, if the roundings are independent and
-    spread evenly over +-w_eps: w_eps / sqrt(3) sqrt(sum_j w_j^2 v_j^2)."""
+    spread evenly over +-w_eps: w_eps / sqrt(3) sqrt(sum_j w_j^2 v_j^2 + out^2 sum_j w_j^2) at most."""
     d, n = q.shape[-1], k.shape[0]
     kk = torch.where(seen.any(0)[:, None], k, 0.0)           # (keys that no row sees may be NaN)
     vv = torch.where(seen.any(0)[:, None], v, 0.0)
@@ -52,7 +53,8 @@ def attend(q, k, v, seen, add=None, w_eps: float = 2.0 ** -16):
     reach = (q.abs() @ kk.abs().T.contiguous() / math.sqrt(d)).masked_fill(~(z > -math.inf), 0.0).amax(-1)
     e = (d + 16) * 2.0 ** -23 * reach + 2.0 ** -21 * z.masked_fill(z == -math.inf, 0.0).abs().amax(-1)
     tol = (w @ vv.abs()) * (torch.expm1(2 * e) + w_eps + (n / 16 + 96) * 2.0 ** -24 + 2.0 ** -14)[:, None] + 2.0 ** -24 * vv.abs().amax()
-    return w @ vv, tol, w_eps / math.sqrt(3) * torch.sqrt(w ** 2 @ vv ** 2)
+    out = w @ vv
+    return out, tol + out.abs() * w_eps, w_eps / math.sqrt(3) * torch.sqrt(w ** 2 @ vv ** 2 + out ** 2 * (w ** 2).sum(-1, keepdim=True))
 
 
 # ------------------------------------------------------------- draft trees

@@ -82,28 +82,18 @@ __device__ __forceinline__ u64 up_to(int x, int kb) {
     return n < 0 ? 0 : n >= 63 ? ~0ull : (2ull << n) - 1;
 }
 
-// What a row sees of a sequence.
-struct RowView {
-    int low, high;           // context: slots low .. high
-    const u64* tree;         // its mask, or null
-};
-__device__ __forceinline__ RowView row_view(const KvAttnArgs& a, int b, int i, int ctx) {
-    const size_t at = (size_t)b * a.N + i;
-    RowView v;
-    const int p = a.tree ? (a.pos ? a.pos[at] : ctx) : ctx + i;
-    v.low = window_low(p, a.window);
-    v.high = a.tree ? ctx - 1 : p;
-    v.tree = a.tree ? a.tree + at * a.words : nullptr;
-    return v;
+// First slot of the window of query i of a sequence, and, as bits, what it sees of keys kb .. kb + 63; tree: its mask
+// (of a tree).
+__device__ __forceinline__ int row_low(const KvAttnArgs& a, int b, int i, int ctx) {
+    return window_low(a.tree ? (a.pos ? a.pos[(size_t)b * a.N + i] : ctx) : ctx + i, a.window);
 }
-// Of keys kb .. kb + 63, as bits.
-__device__ __forceinline__ u64 seen_bits(const KvAttnArgs& a, const RowView& v, int ctx, int kb) {
-    u64 x = up_to(v.high, kb) & (~up_to(v.low - 1, kb) | up_to(a.sinks - 1, kb));
+__device__ __forceinline__ u64 seen_bits(const KvAttnArgs& a, int low, int i, const u64* tree, int ctx, int kb) {
+    u64 x = up_to(a.tree ? ctx - 1 : ctx + i, kb) & (~up_to(low - 1, kb) | up_to(a.sinks - 1, kb));
     const int n = kb - ctx;                                  // (node of the first key)
-    if (v.tree && n > -64 && n < a.N) {
+    if (a.tree && n > -64 && n < a.N) {
         const int w = n >> 6, sh = n & 63;
-        u64 t = w >= 0 ? v.tree[w] >> sh : 0;
-        if (sh && w + 1 < a.words) t |= v.tree[w + 1] << (64 - sh);
+        u64 t = w >= 0 ? tree[w] >> sh : 0;
+        if (sh && w + 1 < a.words) t |= tree[w + 1] << (64 - sh);
         x |= t & up_to(a.N - 1, n);
     }
     return x;
@@ -235,8 +225,10 @@ __global__ void __launch_bounds__(64 * FW) kv_attn_few_kernel(KvAttnArgs a) {
             int col = n16;
             asm volatile("" : "+v"(col));                    // (worked out here: not kept in registers all along)
 #pragma unroll
-            for (int ct = 0; ct < CT; ct++)
-                seen[ct] = (uint32_t)seen_bits(a, row_view(a, b, min(row0 + 16 * ct + col, R - 1) / r, ctx), ctx, kb);
+            for (int ct = 0; ct < CT; ct++) {
+                const int i = min(row0 + 16 * ct + col, R - 1) / r;
+                seen[ct] = (uint32_t)seen_bits(a, row_low(a, b, i, ctx), i, a.tree + ((size_t)b * a.N + i) * a.words, ctx, kb);
+            }
             if (a.N == 1) {                                  // all rows see the same: what they do not see is 0
                 uint32_t mine = seen[0] >> (8 * q4) & 0xFF;
                 if (mrow) {
@@ -500,6 +492,7 @@ __global__ void __launch_bounds__(64 * MW) kv_attn_many_kernel(KvAttnArgs a) {
     unsigned char* const Ks = smem;                          // [4 stages][64 keys][D]
     unsigned char* const Vs = smem + 4 * STB;
     u64* const vbad = reinterpret_cast<u64*>(smem + 8 * STB);   // [4] keys of V that are not finite, by stage % 4
+    u64* const masks = vbad + 4;                             // [256 rows][words] of a tree
     const int tid = threadIdx.x, lane = tid & 63;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int h = lane >> 5, c = lane & 31;
@@ -543,6 +536,11 @@ __global__ void __launch_bounds__(64 * MW) kv_attn_many_kernel(KvAttnArgs a) {
     bf16x8 qf[NF];
 #pragma unroll
     for (int f = 0; f < NF; f++) qf[f] = *reinterpret_cast<const bf16x8*>(qp + 16 * f);
+    // What the row sees.  (Masks in LDS: a load in the loop would wait for all the stages that are on their way.)
+    const int node = rowc / r, low = row_low(a, mt.b, node, mt.ctx);
+    u64* const mask = masks + (wave * 32 + c) * a.words;
+    if (a.tree && h == 0)
+        for (int w = 0; w < a.words; w++) mask[w] = a.tree[((size_t)mt.b * a.N + node) * a.words + w];
     const bool active = mt.q * MROWS + wave * 32 < R;
     const float sl = a.scale * LOG2E;
     // (of the wave's rows: what all see)
@@ -608,7 +606,7 @@ __global__ void __launch_bounds__(64 * MW) kv_attn_many_kernel(KvAttnArgs a) {
         auto poison = [&](int s) __attribute__((always_inline)) {
             if (!mixed(st0 + s)) return;
             const u64 bad = vbad[s & 3];
-            if (bad != 0 && (seen_bits(a, row_view(a, mt.b, rowc / r, mt.ctx), mt.ctx, tile_at(mt.kt, st0 + s) * MKT) & bad) != 0)
+            if (bad != 0 && (seen_bits(a, low, node, mask, mt.ctx, tile_at(mt.kt, st0 + s) * MKT) & bad) != 0)
                 l = __builtin_nanf("");
         };
         // V of stage s, the pieces that this wave has loaded: keys that are not finite are noted, and 0 in the products
@@ -664,7 +662,7 @@ __global__ void __launch_bounds__(64 * MW) kv_attn_many_kernel(KvAttnArgs a) {
             if (tid == 0) vbad[s + 1 & 3] = 0;               // (the list of stage s - 3)
             const int kb = tile_at(mt.kt, st0 + s) * MKT;
             if (kb + MKT - 1 > w_high_min || (kb < w_low_max && kb + MKT > a.sinks)) {
-                const u64 seen = seen_bits(a, row_view(a, mt.b, rowc / r, mt.ctx), mt.ctx, kb) >> (8 * h);
+                const u64 seen = seen_bits(a, low, node, mask, mt.ctx, kb) >> (8 * h);
                 const uint32_t lo = (uint32_t)seen, hi = (uint32_t)(seen >> 32);
 #pragma unroll
                 for (int e = 0; e < 32; e++)
@@ -684,14 +682,15 @@ __global__ void __launch_bounds__(64 * MW) kv_attn_many_kernel(KvAttnArgs a) {
                 m = mn;
             }
             const float mb = m == -INFINITY ? 0.f : m;
+            // (the sum is that of the rounded weights, so that they add up to 1)
+            const bf16x2 one{(__bf16)1.f, (__bf16)1.f};
             float ls[2] = {0.f, 0.f};
 #pragma unroll
             for (int e = 0; e < 32; e += 2) {
                 const float x = exp2_hw(__builtin_fmaf(sc[e / 16][e % 16], sl, -mb));
                 const float y = exp2_hw(__builtin_fmaf(sc[e / 16][e % 16 + 1], sl, -mb));
-                ls[0] += x;
-                ls[1] += y;
                 const bf16x2 w = __builtin_convertvector(f32x2{x, y}, bf16x2);
+                ls[e / 2 % 2] = __builtin_amdgcn_fdot2_f32_bf16(w, one, ls[e / 2 % 2], false);
                 pf[e / 8][e % 8] = w[0];
                 pf[e / 8][e % 8 + 1] = w[1];
             }
@@ -728,12 +727,12 @@ __global__ void __launch_bounds__(64 * MW) kv_attn_many_kernel(KvAttnArgs a) {
         for (int e = 0; e < 16; e++) pp[(2 + i * 16 + e) * 64] = o[i][e];
 }
 
-// Merges the parts of the row tiles that have more than one: block (row tile, wave of it, 32-dim slice), a lane its
-// registers of the slice, part after part in key order.
+// Merges the parts of the row tiles that have more than one: block (row tile, wave of it, 32 dims), a lane its
+// registers of them, part after part in key order.
 template <int D>
 __global__ void __launch_bounds__(64) kv_attn_many_merge_kernel(KvAttnArgs a) {
     constexpr int CB = 8;                                    // parts requested together
-    const int lane = threadIdx.x, wave = blockIdx.y, h = lane >> 5, c = lane & 31, i = blockIdx.z;
+    const int lane = threadIdx.x, wave = blockIdx.y, h = lane >> 5, c = lane & 31, e0 = 16 * blockIdx.z;
     const int r = a.nq / a.nkv, R = a.N * r;
     const ManyTile mt = many_tile(a, a.whole + blockIdx.x);
     const int row = mt.q * MROWS + wave * 32 + c;
@@ -743,11 +742,12 @@ __global__ void __launch_bounds__(64) kv_attn_many_merge_kernel(KvAttnArgs a) {
         float mc[CB], lc[CB], v[CB][16];
 #pragma unroll
         for (int j = 0; j < CB; j++) {
-            const float* pp = a.part + (((size_t)min(p0 + j, mt.n - 1) * a.rest + blockIdx.x) * MW + wave) * M_NREG<D> * 64 + lane;
+            if (p0 + j >= mt.n) break;
+            const float* pp = a.part + (((size_t)(p0 + j) * a.rest + blockIdx.x) * MW + wave) * M_NREG<D> * 64 + lane;
             mc[j] = pp[0];
             lc[j] = pp[64];
 #pragma unroll
-            for (int e = 0; e < 16; e++) v[j][e] = pp[(2 + i * 16 + e) * 64];
+            for (int e = 0; e < 16; e++) v[j][e] = pp[(2 + e0 + e) * 64];
         }
         float Mn = M;
 #pragma unroll
@@ -770,7 +770,8 @@ __global__ void __launch_bounds__(64) kv_attn_many_merge_kernel(KvAttnArgs a) {
     const float lt = L + __shfl_xor(L, 32, 64);
     if (row >= R) return;
     const float inv = lt == 0.f ? 0.f : 1.f / lt;
-    uint16_t* const out = a.out + (((size_t)mt.b * a.N + row / r) * a.nq + mt.hk * r + row % r) * D + i * 32 + 4 * h;
+    // (register e of block i is dim 32 i + 8 (e / 4) + 4 h + e % 4)
+    uint16_t* const out = a.out + (((size_t)mt.b * a.N + row / r) * a.nq + mt.hk * r + row % r) * D + 2 * e0 + 4 * h;
 #pragma unroll
     for (int e = 0; e < 16; e += 4)
         *reinterpret_cast<uint2*>(out + 2 * e) =
@@ -791,7 +792,7 @@ static int tiles_of(const KvAttnShape& s, long long i0, long long i1) {
 // The way of the least estimated time, in us; both kernels split a tile's keys where the grid would leave CUs idle.
 //
 // Few rows: a wave takes w a tile, most of it the latency of its memory, and more with the chip full; a block takes 4 (6.5) to begin
-// and end, a second share the merge launch; a CU draws 35 GB/s, the chip 5.3 TB/s from memory and 8.2 through its L2. Many rows: 1.45 a stage of one block, 1.75 with the chip full, 5 to begin and end (9 where the last stages are a tree's), and
+// and end, a second share the merge launch; a CU draws 35 GB/s, the chip 5.3 TB/s from memory and 8.2 through its L2. Many rows: 1.45 a stage of one block, 1.75 with the chip full, 5 to begin and end (6 where the last stages are a tree's), and
 // the parts' states, written and read back; the row tiles that are left after the last full round of the chip
 // may be cut alone.  Measured (few rows with one, two column tiles; many): 32 heads of 8 of 128, 1 sequence of 8190 tokens, 8 drafts
 // 17.7, 22.2 and 31.9; 16 22.1, 22.7 and 32.4; 64 55, 38.9 and 36.4; 16 sequences of 4000, 13 drafts 99, 64 and 72; 28 heads of 4, 8 of
@@ -819,11 +820,13 @@ KvAttnPlan kv_attn_plan(const KvAttnShape& s) {
         const double bytes = (double)blocks * most32 * FKT * s.d * 4;        // through the L2; from memory:
         const double floor = std::max(bytes / 8.2e6, bytes / tiles / 5.3e6);
         for (long long n = 1; n <= most32 && (n == 1 || blocks * n <= kFewBlocks); n = step(n)) {
-            const double w = (ct == 1 ? 2.1 : 2.5) * (blocks * n > kCus / 2 ? 1.25 : 1.0) * (wide ? 1.0 : 0.55);
+            const double shared = blocks * n <= kCus / 2 ? 1.0 : blocks * n <= kCus || slots == kCus ? 1.25 : 2.0;
+            const double w = (ct == 1 ? 2.1 : 2.5) * shared * (wide ? 1.0 : 0.55);
             const long long per = ((most32 + n - 1) / n + FW - 1) / FW;
             const double us = std::max((double)((blocks * n + slots - 1) / slots) * (per * w + (ct == 1 ? 4.0 : 6.5) * (wide ? 1.0 : 0.75)),
                                        std::max(floor, bytes / (std::min(blocks * n, slots) * 35e3)));
-            consider(us + (n > 1 ? 2.8 + 0.05 * n : 0.0), true, ct, n, 0);
+            const double merge = 2.8 + 0.05 * n + (double)pairs * R * (0.001 + n * (s.d + 2) * 8 / 5e6);
+            consider(us + (n > 1 ? merge : 0.0), true, ct, n, 0);
         }
     }
     if (R <= 32 || s.mask) return best;                      // (masks are the kernel of few rows' alone)
@@ -838,7 +841,7 @@ KvAttnPlan kv_attn_plan(const KvAttnShape& s) {
         sum += t;
         longest = std::max(longest, t);
     }
-    const double mean = sum / samples, t1 = wide ? 1.45 : 1.2, tf = 1.2 * t1, start = s.tree ? 9.0 : 5.0;
+    const double mean = sum / samples, t1 = wide ? 1.45 : 1.2, tf = 1.2 * t1, start = s.tree ? 6.0 : 5.0;
     const double state = std::min<double>(R, MROWS) * (s.d + 4) * 4 * 2 / 5e6;
     auto rounds = [&](long long n, long long parts) {        // us of so many blocks, a row tile in n parts
         const double t = parts <= kCus / 2 ? t1 : tf, part = (double)longest / n * t + start;
@@ -903,7 +906,7 @@ static int launch_many(const KvAttnArgs& a, hipStream_t stream) {
     x.rest = (int)(tiles - a.whole);
     const long long blocks = a.whole + (long long)x.rest * a.nsplit;
     if (tiles > INT_MAX || x.rest < 0 || blocks > INT_MAX) return -1;
-    const size_t lds = (size_t)8 * MKT * D * 2 + 4 * 8;
+    const size_t lds = (size_t)8 * MKT * D * 2 + 4 * 8 + (size_t)MROWS * a.words * 8;
     static LdsLimit lim;
     if (ensure_lds_limit(lim, (const void*)kv_attn_many_kernel<D>, lds)) return -1;
     hipLaunchKernelGGL(kv_attn_many_kernel<D>, dim3((unsigned)blocks), dim3(64 * MW), lds, stream, x);

@@ -12,7 +12,7 @@ def test_equal_scores_average_the_visible_values():
     seen = torch.tensor([[1, 0, 0, 1, 1, 0], [0, 0, 0, 0, 0, 0]], dtype=torch.bool)
     out, tol, spread = O.attend(torch.zeros((2, 2), dtype=torch.float64), torch.ones((6, 2), dtype=torch.float64), v, seen)
     assert torch.allclose(out[0], (v[0] + v[3] + v[4]) / 3) and torch.all(out[1] == 0)
-    assert torch.all(tol > 0) and torch.allclose(spread[0], 2.0 ** -16 / math.sqrt(3) / 3 * (v[[0, 3, 4]] ** 2).sum(0).sqrt())
+    assert torch.all(tol > 0) and torch.allclose(spread[0], 2.0 ** -16 / math.sqrt(3) / 3 * ((v[[0, 3, 4]] ** 2).sum(0) + 3 * out[0] ** 2).sqrt())
 
 
 def test_two_keys_by_hand_and_a_mask():
