@@ -35,7 +35,7 @@ struct KvAttnShape {
 };
 struct KvAttnPlan {
     bool few = false;        // the kernel of few rows
-    int ct = 1, nsplit = 1;  // its column tiles; shares of a row tile's keys,
+    int nsplit = 1;          // shares of a row tile's keys,
     int whole = 0;           // many rows: except for so many tiles
 };
 KvAttnPlan kv_attn_plan(const KvAttnShape& s);

@@ -104,7 +104,7 @@ __device__ __forceinline__ u64 seen_bits(const KvAttnArgs& a, int low, int i, co
 constexpr int FKT = 32;          // keys per tile
 constexpr int FW = 8;            // waves per block
 
-// One block: up to 16 CT rows of a (sequence, kv head) and a share of its key
+// One block: up to 16 rows of a (sequence, kv head) and a share of its key
 // tiles; the waves take the tiles of the share in turn, each on its own, so there is no
 // barrier in the loop.  K goes from memory straight into the A operand of the
 // 16x16x32 MFMA, V through a swizzled LDS tile of the wave, out of which the
@@ -113,13 +113,11 @@ constexpr int FW = 8;            // waves per block
 // in the operand layout of P^T.  A maximum moves only when a score passes it by more
 // than 5 (weights below e^5); the weights are multiplied as bf16 pairs hi + lo: the matrix units
 // have the time, and the weights of short contexts keep 16 bits.
-template <int D, int CT>
+template <int D>
 __global__ void __launch_bounds__(64 * FW) kv_attn_few_kernel(KvAttnArgs a) {
-    constexpr int NCK = D / 8, KROWS = 64 / NCK, NV = FKT / KROWS, NS = D / 32, NDB = D / 16, RT = 16 * CT;
-    constexpr bool QLDS = CT >= 2;                           // queries in LDS, not in registers
+    constexpr int NCK = D / 8, KROWS = 64 / NCK, NV = FKT / KROWS, NS = D / 32, NDB = D / 16, RT = 16;
     extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
     __shared__ float gst[FW][RT][2];
-    u32x4* const Qs = reinterpret_cast<u32x4*>(smem + FW * 16 * D * 4);      // [CT][NS][64 lanes]
     const int tid = threadIdx.x, lane = tid & 63;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int hk = blockIdx.x % a.nkv, row0 = blockIdx.x / a.nkv * RT, part = blockIdx.y, b = blockIdx.z;
@@ -127,20 +125,12 @@ __global__ void __launch_bounds__(64 * FW) kv_attn_few_kernel(KvAttnArgs a) {
     const int n16 = lane & 15, q4 = lane >> 4;
     int ctx = a.ctx_lens ? a.ctx_lens[b] : a.ctx_base;
 
-    // ---- queries: column n16 of column tile ct is row row0 + 16 ct + n16, dims 32 s + 8 q4 .. + 7
-    u32x4 qw[QLDS ? 1 : NS];
-    auto query = [&](int ct, int s) __attribute__((always_inline)) {
-        const int row = min(row0 + 16 * ct + n16, R - 1);
-        return reinterpret_cast<const u32x4*>(a.q + (((size_t)b * a.N + row / r) * a.nq + hk * r + row % r) * D + 32 * s + 8 * q4);
-    };
-    if constexpr (QLDS) {
+    // ---- queries: column n16 is row row0 + n16, dims 32 s + 8 q4 .. + 7
+    bf16x8 qf[NS];
+    const int row = min(row0 + n16, R - 1);
+    const uint16_t* const qp = a.q + (((size_t)b * a.N + row / r) * a.nq + hk * r + row % r) * D + 8 * q4;
 #pragma unroll
-        for (int i = 0; i < CT * NS; i += FW)
-            if (i + wave < CT * NS) Qs[(i + wave) * 64 + lane] = *query((i + wave) / NS, (i + wave) % NS);
-    } else {
-#pragma unroll
-        for (int s = 0; s < NS; s++) qw[s] = *query(0, s);
-    }
+    for (int s = 0; s < NS; s++) qf[s] = *reinterpret_cast<const bf16x8*>(qp + 32 * s);
     ctx = min(ctx, a.max_ctx);
 
     // ---- this block's tiles
@@ -187,62 +177,38 @@ __global__ void __launch_bounds__(64 * FW) kv_attn_few_kernel(KvAttnArgs a) {
         load_k(tile_at(kt, t) * FKT);
         load_v(tile_at(kt, t) * FKT);
     }
-    if constexpr (QLDS) __syncthreads();
-    auto qf = [&](int ct, int s) __attribute__((always_inline)) {
-        return __builtin_bit_cast(bf16x8, QLDS ? Qs[(ct * NS + s) * 64 + lane] : qw[QLDS ? 0 : s]);
-    };
-
-    f32x4 o[CT][NDB];
-    float m[CT], l[CT];
+    f32x4 o[NDB];
 #pragma unroll
-    for (int ct = 0; ct < CT; ct++) {
-#pragma unroll
-        for (int i = 0; i < NDB; i++) o[ct][i] = f32x4{0.f, 0.f, 0.f, 0.f};
-        m[ct] = -INFINITY;
-        l[ct] = 0.f;
-    }
+    for (int i = 0; i < NDB; i++) o[i] = f32x4{0.f, 0.f, 0.f, 0.f};
+    float m = -INFINITY, l = 0.f;
     for (; t < t1; t += FW) {
         const int kb = tile_at(kt, t) * FKT, next = t + FW < t1 ? tile_at(kt, t + FW) * FKT : -1;
-        f32x4 acc[CT][2];
-#pragma unroll
-        for (int ct = 0; ct < CT; ct++) acc[ct][0] = acc[ct][1] = f32x4{0.f, 0.f, 0.f, 0.f};
+        f32x4 acc[2] = {f32x4{0.f, 0.f, 0.f, 0.f}, f32x4{0.f, 0.f, 0.f, 0.f}};
 #pragma unroll
         for (int s = 0; s < NS; s++)
 #pragma unroll
-            for (int ct = 0; ct < CT; ct++) {
-                const bf16x8 q = qf(ct, s);
+            for (int h = 0; h < 2; h++)
+                acc[h] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, kr[h][s]), qf[s], acc[h], 0, 0, 0);
+        float p[8];
 #pragma unroll
-                for (int h = 0; h < 2; h++)
-                    acc[ct][h] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, kr[h][s]), q, acc[ct][h], 0, 0, 0);
-            }
-        float p[CT][8];
-#pragma unroll
-        for (int ct = 0; ct < CT; ct++)
-#pragma unroll
-            for (int e = 0; e < 8; e++) p[ct][e] = acc[ct][e / 4][e % 4] * a.scale;
-        uint32_t bad = 0, seen[CT];                          // keys whose values are not finite, keys that the rows see
+        for (int e = 0; e < 8; e++) p[e] = acc[e / 4][e % 4] * a.scale;
+        uint32_t bad = 0, seen = 0;                          // keys whose values are not finite, keys that the row sees
         if (mrow || kb + FKT - 1 > high_min || (kb < low_max && kb + FKT > a.sinks)) {
             int col = n16;
             asm volatile("" : "+v"(col));                    // (worked out here: not kept in registers all along)
-#pragma unroll
-            for (int ct = 0; ct < CT; ct++) {
-                const int i = min(row0 + 16 * ct + col, R - 1) / r;
-                seen[ct] = (uint32_t)seen_bits(a, row_low(a, b, i, ctx), i, a.tree + ((size_t)b * a.N + i) * a.words, ctx, kb);
-            }
+            const int i = min(row0 + col, R - 1) / r;
+            seen = (uint32_t)seen_bits(a, row_low(a, b, i, ctx), i, a.tree + ((size_t)b * a.N + i) * a.words, ctx, kb);
             if (a.N == 1) {                                  // all rows see the same: what they do not see is 0
-                uint32_t mine = seen[0] >> (8 * q4) & 0xFF;
+                uint32_t mine = seen >> (8 * q4) & 0xFF;
                 if (mrow) {
 #pragma unroll
                     for (int e = 0; e < 8; e++) {
                         mine &= ~((uint32_t)(mk[e] == -INFINITY) << e);
-#pragma unroll
-                        for (int ct = 0; ct < CT; ct++) p[ct][e] += mk[e];
+                        p[e] += mk[e];
                     }
                 }
 #pragma unroll
-                for (int ct = 0; ct < CT; ct++)
-#pragma unroll
-                    for (int e = 0; e < 8; e++) p[ct][e] = mine >> e & 1 ? p[ct][e] : -INFINITY;
+                for (int e = 0; e < 8; e++) p[e] = mine >> e & 1 ? p[e] : -INFINITY;
 #pragma unroll
                 for (int i = 0; i < NV; i++) {
                     const int k = i * KROWS + lane / NCK;    // (lane 16 (k / 8) has its bit)
@@ -250,9 +216,7 @@ __global__ void __launch_bounds__(64 * FW) kv_attn_few_kernel(KvAttnArgs a) {
                 }
             } else {
 #pragma unroll
-                for (int ct = 0; ct < CT; ct++)
-#pragma unroll
-                    for (int e = 0; e < 8; e++) p[ct][e] = seen[ct] >> (8 * q4 + e) & 1 ? p[ct][e] : -INFINITY;
+                for (int e = 0; e < 8; e++) p[e] = seen >> (8 * q4 + e) & 1 ? p[e] : -INFINITY;
 #pragma unroll
                 for (int i = 0; i < NV; i++) {
                     const u64 x = __builtin_amdgcn_ballot_w64(not_finite(vr[i]));
@@ -275,32 +239,29 @@ __global__ void __launch_bounds__(64 * FW) kv_attn_few_kernel(KvAttnArgs a) {
             load_k(next);
             load_v(next);
         }
-        bf16x8 phi[CT], plo[CT];
+        float mx = p[0];
 #pragma unroll
-        for (int ct = 0; ct < CT; ct++) {
-            float mx = p[ct][0];
+        for (int e = 1; e < 8; e++) mx = fmaxf(mx, p[e]);
+        if (__builtin_amdgcn_ballot_w64(mx > m + 5.f) != 0) {
+            const float mn = fmaxf(m, max_quarters(mx));
+            const float alpha = exp2_hw((m - (mn == -INFINITY ? 0.f : mn)) * LOG2E);
+            l *= alpha;
+            m = mn;
 #pragma unroll
-            for (int e = 1; e < 8; e++) mx = fmaxf(mx, p[ct][e]);
-            if (__builtin_amdgcn_ballot_w64(mx > m[ct] + 5.f) != 0) {
-                const float mn = fmaxf(m[ct], max_quarters(mx));
-                const float alpha = exp2_hw((m[ct] - (mn == -INFINITY ? 0.f : mn)) * LOG2E);
-                l[ct] *= alpha;
-                m[ct] = mn;
+            for (int i = 0; i < NDB; i++)
 #pragma unroll
-                for (int i = 0; i < NDB; i++)
+                for (int e = 0; e < 4; e++) o[i][e] *= alpha;
+        }
+        const float mb = m == -INFINITY ? 0.f : m;
+        bf16x8 phi, plo;
 #pragma unroll
-                    for (int e = 0; e < 4; e++) o[ct][i][e] *= alpha;
-            }
-            const float mb = m[ct] == -INFINITY ? 0.f : m[ct];
-#pragma unroll
-            for (int e = 0; e < 8; e += 2) {                 // (the difference first: a mask may be the lowest float)
-                const float x = exp2_hw((p[ct][e] - mb) * LOG2E), y = exp2_hw((p[ct][e + 1] - mb) * LOG2E);
-                l[ct] += x + y;
-                const bf16x2 hi = __builtin_convertvector(f32x2{x, y}, bf16x2);
-                const bf16x2 lo = __builtin_convertvector(f32x2{x - (float)hi[0], y - (float)hi[1]}, bf16x2);
-                phi[ct][e] = hi[0]; phi[ct][e + 1] = hi[1];
-                plo[ct][e] = lo[0]; plo[ct][e + 1] = lo[1];
-            }
+        for (int e = 0; e < 8; e += 2) {                     // (the difference first: a mask may be the lowest float)
+            const float x = exp2_hw((p[e] - mb) * LOG2E), y = exp2_hw((p[e + 1] - mb) * LOG2E);
+            l += x + y;
+            const bf16x2 hi = __builtin_convertvector(f32x2{x, y}, bf16x2);
+            const bf16x2 lo = __builtin_convertvector(f32x2{x - (float)hi[0], y - (float)hi[1]}, bf16x2);
+            phi[e] = hi[0]; phi[e + 1] = hi[1];
+            plo[e] = lo[0]; plo[e + 1] = lo[1];
         }
         // O^T += V^T P^T per 16-dim block db: lane (n16, q4) takes V of keys 8 q4 .. + 7, dim 16 db + n16 (two transposing
         // reads: lane n16 of its group points at key 8 q4 + n16 / 4 (+ 4), dims 16 db + 4 (n16 % 4) .. + 3)
@@ -310,63 +271,53 @@ __global__ void __launch_bounds__(64 * FW) kv_attn_few_kernel(KvAttnArgs a) {
             const int off = (((2 * db + ((n16 & 3) >> 1)) ^ (2 * q4)) << 3) | (4 * (n16 & 1));
             const i16x4 v0 = lds_read_tr16(Vw + off), v1 = lds_read_tr16(Vw + 4 * D + off);
             const bf16x8 vf = __builtin_bit_cast(bf16x8, __builtin_shufflevector(v0, v1, 0, 1, 2, 3, 4, 5, 6, 7));
-#pragma unroll
-            for (int ct = 0; ct < CT; ct++) {
-                o[ct][db] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, phi[ct], o[ct][db], 0, 0, 0);
-                o[ct][db] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, plo[ct], o[ct][db], 0, 0, 0);
-            }
+            o[db] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, phi, o[db], 0, 0, 0);
+            o[db] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, plo, o[db], 0, 0, 0);
         }
-        if (bad) {
-#pragma unroll
-            for (int ct = 0; ct < CT; ct++)
-                if (seen[ct] & bad) l[ct] = __builtin_nanf("");
-        }
+        if (seen & bad) l = __builtin_nanf("");
         __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
     }
 
-    // ---- the waves' states meet in LDS, over the V tiles, a column tile at a time
+    // ---- the waves' states meet in LDS, over the V tiles
+    __syncthreads();
     float* const ored = reinterpret_cast<float*>(smem);      // [FW][16][D]
+    l = sum_quarters(l);
+    if (n16 < nr) {
+#pragma unroll
+        for (int db = 0; db < NDB; db++) *reinterpret_cast<f32x4*>(ored + (wave * RT + n16) * D + 16 * db + 4 * q4) = o[db];
+        if (q4 == 0) {
+            gst[wave][n16][0] = m;
+            gst[wave][n16][1] = l;
+        }
+    }
+    __syncthreads();
     // one share: the output; more: its state, [(sequence, kv head)][share][R rows][D] outputs, then [..][R] (max, sum)
     const size_t slot = (((size_t)b * a.nkv + hk) * a.nsplit + part) * R + row0;
     float* const po = a.part + slot * D;
     float2* const pst = reinterpret_cast<float2*>(a.part + (size_t)a.B * a.nkv * a.nsplit * R * D) + slot;
+    for (int idx = tid; idx < nr * (D / 2); idx += 64 * FW) {
+        const int lr = idx / (D / 2), d = 2 * (idx % (D / 2));
+        float M = -INFINITY;
 #pragma unroll
-    for (int ct = 0; ct < CT; ct++) {
-        __syncthreads();
-        l[ct] = sum_quarters(l[ct]);
-        if (16 * ct + n16 < nr) {
+        for (int w = 0; w < FW; w++) M = fmaxf(M, gst[w][lr][0]);
+        const float Mb = M == -INFINITY ? 0.f : M;
+        float x = 0.f, y = 0.f, lt = 0.f;
 #pragma unroll
-            for (int db = 0; db < NDB; db++) *reinterpret_cast<f32x4*>(ored + (wave * 16 + n16) * D + 16 * db + 4 * q4) = o[ct][db];
-            if (q4 == 0) {
-                gst[wave][16 * ct + n16][0] = m[ct];
-                gst[wave][16 * ct + n16][1] = l[ct];
-            }
+        for (int w = 0; w < FW; w++) {
+            const float lw = gst[w][lr][1], sc = lw != lw ? lw : exp2_hw((gst[w][lr][0] - Mb) * LOG2E);   // (NaN stays)
+            const float2 v = *reinterpret_cast<const float2*>(ored + (w * RT + lr) * D + d);
+            x += sc == 0.f ? 0.f : sc * v.x;
+            y += sc == 0.f ? 0.f : sc * v.y;
+            lt += sc * lw;
         }
-        __syncthreads();
-        for (int idx = tid; idx < min(16, nr - 16 * ct) * (D / 2); idx += 64 * FW) {
-            const int lr = 16 * ct + idx / (D / 2), d = 2 * (idx % (D / 2));
-            float M = -INFINITY;
-#pragma unroll
-            for (int w = 0; w < FW; w++) M = fmaxf(M, gst[w][lr][0]);
-            const float Mb = M == -INFINITY ? 0.f : M;
-            float x = 0.f, y = 0.f, lt = 0.f;
-#pragma unroll
-            for (int w = 0; w < FW; w++) {
-                const float lw = gst[w][lr][1], sc = lw != lw ? lw : exp2_hw((gst[w][lr][0] - Mb) * LOG2E);   // (NaN stays)
-                const float2 v = *reinterpret_cast<const float2*>(ored + (w * 16 + lr % 16) * D + d);
-                x += sc == 0.f ? 0.f : sc * v.x;
-                y += sc == 0.f ? 0.f : sc * v.y;
-                lt += sc * lw;
-            }
-            if (a.nsplit == 1) {
-                const int row = row0 + lr;
-                const float u = lt == 0.f ? 0.f : x / lt, v = lt == 0.f ? 0.f : y / lt;
-                *reinterpret_cast<uint32_t*>(a.out + (((size_t)b * a.N + row / r) * a.nq + hk * r + row % r) * D + d) =
-                    (uint32_t)bf16_bits_rne(u) | (uint32_t)bf16_bits_rne(v) << 16;
-            } else {
-                *reinterpret_cast<float2*>(po + lr * D + d) = float2{x, y};
-                if (d == 0) pst[lr] = float2{M, lt};
-            }
+        if (a.nsplit == 1) {
+            const int orow = row0 + lr;
+            const float u = lt == 0.f ? 0.f : x / lt, v = lt == 0.f ? 0.f : y / lt;
+            *reinterpret_cast<uint32_t*>(a.out + (((size_t)b * a.N + orow / r) * a.nq + hk * r + orow % r) * D + d) =
+                (uint32_t)bf16_bits_rne(u) | (uint32_t)bf16_bits_rne(v) << 16;
+        } else {
+            *reinterpret_cast<float2*>(po + lr * D + d) = float2{x, y};
+            if (d == 0) pst[lr] = float2{M, lt};
         }
     }
 }
@@ -531,20 +482,21 @@ __global__ void __launch_bounds__(64 * MW) kv_attn_many_kernel(KvAttnArgs a) {
 
     const int n = st1 - st0;
     // ---- queries: this lane's row, dims 16 f + 8 h .. + 7 of every fragment f
-    const int row = mt.q * MROWS + wave * 32 + c, rowc = min(row, R - 1);
+    // (the two waves of a SIMD, one of either half of the block, take neighbouring rows)
+    const int grp = 2 * (wave % (MW / 2)) + wave / (MW / 2), row = mt.q * MROWS + grp * 32 + c, rowc = min(row, R - 1);
     const uint16_t* qp = a.q + (((size_t)mt.b * a.N + rowc / r) * a.nq + mt.hk * r + rowc % r) * D + 8 * h;
     bf16x8 qf[NF];
 #pragma unroll
     for (int f = 0; f < NF; f++) qf[f] = *reinterpret_cast<const bf16x8*>(qp + 16 * f);
     // What the row sees.  (Masks in LDS: a load in the loop would wait for all the stages that are on their way.)
     const int node = rowc / r, low = row_low(a, mt.b, node, mt.ctx);
-    u64* const mask = masks + (wave * 32 + c) * a.words;
+    u64* const mask = masks + (grp * 32 + c) * a.words;
     if (a.tree && h == 0)
         for (int w = 0; w < a.words; w++) mask[w] = a.tree[((size_t)mt.b * a.N + node) * a.words + w];
-    const bool active = mt.q * MROWS + wave * 32 < R;
+    const bool active = mt.q * MROWS + grp * 32 < R;
     const float sl = a.scale * LOG2E;
     // (of the wave's rows: what all see)
-    const int wi0 = min(mt.q * MROWS + wave * 32, R - 1) / r, wi1 = min(mt.q * MROWS + wave * 32 + 31, R - 1) / r;
+    const int wi0 = min(mt.q * MROWS + grp * 32, R - 1) / r, wi1 = min(mt.q * MROWS + grp * 32 + 31, R - 1) / r;
     const int w_low_max = window_low(a.tree ? mt.ctx + a.N - 1 : mt.ctx + wi1, a.window), w_high_min = a.tree ? mt.ctx - 1 : mt.ctx + wi0;
 
     f32x16 o[NS];
@@ -636,8 +588,16 @@ __global__ void __launch_bounds__(64 * MW) kv_attn_many_kernel(KvAttnArgs a) {
             check_v(0);
             __syncthreads();
         }
+        if (!active)                                         // (loads for the others)
+            for (int s = 0; s < n; s++) {
+                __syncthreads();
+                load_ahead(s + early);
+                wait_for(s + early);
+                check_v(s + early);
+                __syncthreads();
+            }
 #pragma clang loop unroll(disable)
-        for (int s = 0; s < n; s++) {
+        for (int s = active ? 0 : n; s < n; s++) {
             // ---- matrix half: scores of stage s, output of stage s - 1 (of the first: weights and values 0).  Operands are read
             // some products ahead: left to itself the compiler waits for every pair of them.
             scores(s);
@@ -699,8 +659,10 @@ __global__ void __launch_bounds__(64 * MW) kv_attn_many_kernel(KvAttnArgs a) {
             check_v(s + early);
             __syncthreads();
         }
-        output(n - 1);
-        poison(n - 1);
+        if (active) {
+            output(n - 1);
+            poison(n - 1);
+        }
         if (wave < MW / 2) __syncthreads();
     }
     const float lt = l + __shfl_xor(l, 32, 64);
@@ -718,7 +680,7 @@ __global__ void __launch_bounds__(64 * MW) kv_attn_many_kernel(KvAttnArgs a) {
         return;
     }
     if (!active) return;
-    float* pp = a.part + ((size_t)in * MW + wave) * M_NREG<D> * 64 + lane;       // state of this part
+    float* pp = a.part + ((size_t)in * MW + grp) * M_NREG<D> * 64 + lane;       // state of this part
     pp[0] = m;
     pp[64] = l;
 #pragma unroll
@@ -791,45 +753,43 @@ static int tiles_of(const KvAttnShape& s, long long i0, long long i1) {
 
 // The way of the least estimated time, in us; both kernels split a tile's keys where the grid would leave CUs idle.
 //
-// Few rows: a wave takes w a tile, most of it the latency of its memory, and more with the chip full; a block takes 4 (6.5) to begin
-// and end, a second share the merge launch; a CU draws 35 GB/s, the chip 5.3 TB/s from memory and 8.2 through its L2. Many rows: 1.45 a stage of one block, 1.75 with the chip full, 5 to begin and end (6 where the last stages are a tree's), and
-// the parts' states, written and read back; the row tiles that are left after the last full round of the chip
-// may be cut alone.  Measured (few rows with one, two column tiles; many): 32 heads of 8 of 128, 1 sequence of 8190 tokens, 8 drafts
-// 17.7, 22.2 and 31.9; 16 22.1, 22.7 and 32.4; 64 55, 38.9 and 36.4; 16 sequences of 4000, 13 drafts 99, 64 and 72; 28 heads of 4, 8 of
-// 2000, 32 drafts -, 35 and 27.7, 8001 queries, 876 row tiles in one part 477, the last 108 in two 454.
-// Four column tiles (64 rows, four waves of 512 registers) were slower than two tiles of two everywhere: 16 drafts behind 8190 30.6,
-// 13 behind 4000 66 to 89.
+// Few rows: a wave takes w a tile, most of it the latency of its memory, and more with the chip full; a block takes 4 to begin
+// and end, a second share the merge launch; a CU draws 35 GB/s, the chip 5.3 TB/s from memory and 8.2 through its L2.
+// Many rows: 1.2 to 1.45 a stage of one block, more with the chip full, 5 to begin and end (6 where the last stages are a
+// tree's), and the parts' states, written and read back; the row tiles that are left after the last full round of the chip
+// may be cut alone.  Measured (few and many rows, each in its best number of parts): 32 heads of 8 of 128, 1 sequence of 8190 tokens,
+// 4, 8, 16, 32 and 64 drafts 17.3 and 22.3, 17.4 and 22.3, 21.7 and 25.8, 36 and 27.4, 55 and 31.4; 16 sequences of 4000, 4, 8 and 13
+// drafts 53.3 and 55.1, 58.5 and 55.0, 98.7 and 61.4; 28 heads of 4, 8001 queries, 876 row tiles in one part 477, the last 108 in
+// two 454.  Tiles of 32 rows in the kernel of few rows (two column tiles) were within 3% of the better of these at best.
 KvAttnPlan kv_attn_plan(const KvAttnShape& s) {
     KvAttnPlan best;
     double least = -1;
     const long long R = (long long)s.N * s.r, pairs = (long long)s.B * s.nkv;
     const bool wide = s.d == 128;
-    auto consider = [&](double us, bool few, int ct, long long n, long long whole) {
+    auto consider = [&](double us, bool few, long long n, long long whole) {
         if (least >= 0 && us >= least) return;
         least = us;
         best.few = few;
-        best.ct = ct;
         best.nsplit = (int)n;
         best.whole = (int)whole;
     };
     auto step = [](long long n) { return n < 8 ? n + 1 : n + n / 4; };
-    const int most32 = tiles_of<FKT>(s, 0, s.N - 1);
-    for (int ct = 1; ct <= (R > 16 ? 2 : 1); ct++) {
-        const long long tiles = (R + 16 * ct - 1) / (16 * ct), blocks = pairs * tiles;
-        const long long slots = (!wide && ct == 1 ? 2 : 1) * kCus;
-        const double bytes = (double)blocks * most32 * FKT * s.d * 4;        // through the L2; from memory:
+    {
+        const int most = tiles_of<FKT>(s, 0, s.N - 1);
+        const long long tiles = (R + 15) / 16, blocks = pairs * tiles, slots = (wide ? 1 : 2) * kCus;
+        const double bytes = (double)blocks * most * FKT * s.d * 4;          // through the L2; from memory:
         const double floor = std::max(bytes / 8.2e6, bytes / tiles / 5.3e6);
-        for (long long n = 1; n <= most32 && (n == 1 || blocks * n <= kFewBlocks); n = step(n)) {
-            const double shared = blocks * n <= kCus / 2 ? 1.0 : blocks * n <= kCus || slots == kCus ? 1.25 : 2.0;
-            const double w = (ct == 1 ? 2.1 : 2.5) * shared * (wide ? 1.0 : 0.55);
-            const long long per = ((most32 + n - 1) / n + FW - 1) / FW;
-            const double us = std::max((double)((blocks * n + slots - 1) / slots) * (per * w + (ct == 1 ? 4.0 : 6.5) * (wide ? 1.0 : 0.75)),
+        for (long long n = 1; n <= most && (n == 1 || blocks * n <= kFewBlocks); n = step(n)) {
+            const double shared = blocks * n <= kCus / 2 ? 1.0 : blocks * n <= kCus || wide ? 1.25 : 2.0;
+            const double w = 2.1 * shared * (wide ? 1.0 : 0.55);
+            const long long per = ((most + n - 1) / n + FW - 1) / FW;
+            const double us = std::max((double)((blocks * n + slots - 1) / slots) * (per * w + (wide ? 4.0 : 3.0)),
                                        std::max(floor, bytes / (std::min(blocks * n, slots) * 35e3)));
             const double merge = 2.8 + 0.05 * n + (double)pairs * R * (0.001 + n * (s.d + 2) * 8 / 5e6);
-            consider(us + (n > 1 ? merge : 0.0), true, ct, n, 0);
+            consider(us + (n > 1 ? merge : 0.0), true, n, 0);
         }
     }
-    if (R <= 32 || s.mask) return best;                      // (masks are the kernel of few rows' alone)
+    if (R <= 16 || s.mask) return best;                      // (masks are the kernel of few rows' alone)
     const long long nqt = (R + MROWS - 1) / MROWS, blocks = pairs * nqt;
     double sum = 0;                                          // stages of a row tile: mean of some, and the longest
     int longest = 0;
@@ -841,31 +801,31 @@ KvAttnPlan kv_attn_plan(const KvAttnShape& s) {
         sum += t;
         longest = std::max(longest, t);
     }
-    const double mean = sum / samples, t1 = wide ? 1.45 : 1.2, tf = 1.2 * t1, start = s.tree ? 6.0 : 5.0;
-    const double state = std::min<double>(R, MROWS) * (s.d + 4) * 4 * 2 / 5e6;
+    const double mean = sum / samples, start = s.tree ? 6.0 : 5.0;
+    const double t1 = (wide ? 1.0 : 0.85) * (R <= 32 ? 1.2 : R <= 128 ? 1.4 : 1.45), tf = t1 * (R <= 128 ? 1.1 : 1.2);
+    const double state = std::min<double>(R, MROWS) * (s.d + 4) * 8 / 5e6, floor = pairs * mean * MKT * s.d * 4 / 5.3e6;
     auto rounds = [&](long long n, long long parts) {        // us of so many blocks, a row tile in n parts
-        const double t = parts <= kCus / 2 ? t1 : tf, part = (double)longest / n * t + start;
-        if (parts <= kCus) return part;
-        if (mean > 0.9 * longest) return (double)((parts + kCus - 1) / kCus) * part;
+        const double t = parts <= kCus / 2 ? t1 : tf, part = (double)((longest + n - 1) / n) * t + start;
+        if (parts <= kCus) return std::max(floor, part);
+        if (mean > 0.9 * longest) return std::max(floor, (double)((parts + kCus - 1) / kCus) * part);
         return std::max(part, parts * (mean / n * t + start) / kCus + 0.5 * mean / n * t);      // (the longest go first)
     };
     const long long full = blocks / kCus * kCus;
     for (long long n = 1; n <= longest && (n == 1 || (blocks - full) * n <= kManyParts); n = step(n)) {
-        if (n == 1) consider(rounds(1, blocks), false, 0, 1, blocks);
-        if (n > 1 && blocks * n <= kManyParts) consider(rounds(n, blocks * n) + 3.0 + blocks * n * state, false, 0, n, 0);
+        if (n == 1) consider(rounds(1, blocks), false, 1, blocks);
+        if (n > 1 && blocks * n <= kManyParts) consider(rounds(n, blocks * n) + 3.0 + blocks * n * state, false, n, 0);
         if (n > 1 && full > 0 && full < blocks)
-            consider(rounds(1, full) + rounds(n, (blocks - full) * n) + 3.0 + (blocks - full) * n * state, false, 0, n, full);
+            consider(rounds(1, full) + rounds(n, (blocks - full) * n) + 3.0 + (blocks - full) * n * state, false, n, full);
     }
     return best;
 }
 
 // (for the host tests)
-extern "C" void w4_kv_attn_plan(int B, int N, int nkv, int r, int d, int max_ctx, int window, int sinks, int tree, int* few, int* ct,
+extern "C" void w4_kv_attn_plan(int B, int N, int nkv, int r, int d, int max_ctx, int window, int sinks, int tree, int* few,
                                 int* nsplit, int* whole, size_t* part, size_t* bound) {
     const KvAttnShape s{B, N, nkv, r, d, max_ctx, window ? window : INT_MAX, window ? sinks : 0, tree != 0, false};
     const KvAttnPlan p = kv_attn_plan(s);
     *few = p.few;
-    *ct = p.ct;
     *nsplit = p.nsplit;
     *whole = p.whole;
     *part = kv_attn_part_bytes(s, p);
@@ -882,18 +842,16 @@ size_t kv_attn_part_bytes(const KvAttnShape& s, const KvAttnPlan& p) {
 // (either kernel's; a product of what grows, and a constant)
 size_t kv_attn_part_bound(const KvAttnShape& s) {
     const size_t R = (size_t)s.N * s.r, pairs = (size_t)s.B * s.nkv, slots = (size_t)s.max_ctx + s.N;
-    const size_t few = std::min<size_t>(pairs * R * (slots / FKT + 2), (size_t)kFewBlocks * 32);
+    const size_t few = std::min<size_t>(pairs * R * (slots / FKT + 2), (size_t)kFewBlocks * 16);
     const size_t many = std::min<size_t>(pairs * ((R + MROWS - 1) / MROWS) * (slots / MKT + 2), kManyParts) * MROWS;
     return std::max<size_t>(256, std::max(few, many) * (s.d + 4) * 4);
 }
 
-template <int D, int CT>
+template <int D>
 static int launch_few(const KvAttnArgs& a, hipStream_t stream) {
-    const int R = a.N * (a.nq / a.nkv), tiles = (R + 16 * CT - 1) / (16 * CT);
-    const size_t lds = (size_t)FW * 16 * D * 4 + (CT >= 2 ? CT * 16 * D * 2 : 0);     // V tiles, outputs over them; queries
-    static LdsLimit lim;
-    if (ensure_lds_limit(lim, (const void*)kv_attn_few_kernel<D, CT>, lds)) return -1;
-    hipLaunchKernelGGL((kv_attn_few_kernel<D, CT>), dim3(a.nkv * tiles, a.nsplit, a.B), dim3(64 * FW), lds, stream, a);
+    const int R = a.N * (a.nq / a.nkv), tiles = (R + 15) / 16;
+    const size_t lds = (size_t)FW * FKT * D * 2;             // V tiles, and the waves' outputs over them
+    hipLaunchKernelGGL(kv_attn_few_kernel<D>, dim3(a.nkv * tiles, a.nsplit, a.B), dim3(64 * FW), lds, stream, a);
     if (a.nsplit > 1) hipLaunchKernelGGL(kv_attn_few_merge_kernel<D>, dim3(a.nkv, R, a.B), dim3(256), 0, stream, a);
     return hipGetLastError() == hipSuccess ? 0 : -1;
 }
@@ -921,12 +879,9 @@ int launch_kv_attn(const KvAttnArgs& args, size_t part_bytes, hipStream_t stream
     if (kv_attn_part_bytes(s, p) > part_bytes || (a.mask && a.N != 1)) return -1;
     a.nsplit = p.nsplit;
     a.whole = p.whole;
-    if (p.few) {
-        if (p.ct == 1) return a.d == 128 ? launch_few<128, 1>(a, stream) : launch_few<64, 1>(a, stream);
-        return a.d == 128 ? launch_few<128, 2>(a, stream) : launch_few<64, 2>(a, stream);
-    }
+    if (p.few) return a.d == 128 ? launch_few<128>(a, stream) : launch_few<64>(a, stream);
     if (a.mask) return -1;
     return a.d == 128 ? launch_many<128>(a, stream) : launch_many<64>(a, stream);
 }
 
-int load_kv_attn() { return load_code((const void*)kv_attn_few_kernel<128, 1>); }
+int load_kv_attn() { return load_code((const void*)kv_attn_few_kernel<128>); }

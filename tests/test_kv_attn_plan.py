@@ -17,9 +17,9 @@ from paper_2607_15865_amd import binding  # noqa: E402
 
 
 def plan(B, N, nkv, r, d, max_ctx, window, sinks, tree):
-    out = [ctypes.c_int() for _ in range(4)] + [ctypes.c_size_t() for _ in range(2)]
+    out = [ctypes.c_int() for _ in range(3)] + [ctypes.c_size_t() for _ in range(2)]
     binding._lib.w4_kv_attn_plan(B, N, nkv, r, d, max_ctx, window, sinks, tree, *[ctypes.byref(x) for x in out])
-    return dict(zip(("few", "ct", "nsplit", "whole", "part", "bound"), [x.value for x in out]))
+    return dict(zip(("few", "nsplit", "whole", "part", "bound"), [x.value for x in out]))
 
 
 def shapes(seed, count):
@@ -40,8 +40,8 @@ def test_plans_fit_launches_and_workspaces(seed):
         R = N * r
         assert p["nsplit"] >= 1 and p["part"] <= p["bound"], s
         if p["few"]:
-            assert p["ct"] in (1, 2) and p["whole"] == 0
-            tiles = -(-R // (16 * p["ct"]))
+            assert p["whole"] == 0
+            tiles = -(-R // 16)
             assert p["nsplit"] <= 65535 and nkv * tiles < 2 ** 31
             assert p["nsplit"] == 1 or B * nkv * tiles * p["nsplit"] <= 512, s
             assert p["part"] == (B * nkv * R * p["nsplit"] * (d + 2) * 4 if p["nsplit"] > 1 else 0)
