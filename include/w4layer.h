@@ -195,7 +195,8 @@ int kv_layout(const layer_config* cfg, int32_t batch, kv_desc* out);
 
 /* Bytes of device workspace a stage call needs: stage 0 prefill (batch 1,
  * T tokens), 1 prefill_kv (batch 1, T tokens, history up to max_ctx), 2
- * decode (batch sequences, context up to max_ctx).  For stages 0 and 1 it does
+ * decode (batch sequences, context up to max_ctx), 3 layer_verify_tree (batch 1,
+ * T tokens, history up to max_ctx).  For stages 0, 1 and 3 it does
  * not decrease with T: a workspace for a longer prompt serves a shorter one.
  * Returns 0 for invalid arguments. */
 size_t layer_workspace_size(layer_t layer, int32_t stage, int32_t batch, int32_t T, int32_t max_ctx);
@@ -224,6 +225,20 @@ int layer_prefill(layer_t layer, const float* x, const int32_t* pos, int32_t T,
 int layer_prefill_kv(layer_t layer, const float* x, const int32_t* pos, int32_t T, int32_t hist_len,
                      void* k_cache, void* v_cache, float* y,
                      void* ws, size_t ws_bytes, void* stream);
+
+/* Drafted tokens of one sequence, 1 <= T <= W4_TREE_MAX of them, held as a tree
+ * behind hist_len >= 0 cached ones: layer_prefill_kv in which token t, written
+ * to slot hist_len + t, attends to slots 0 .. hist_len-1 and to those of the nodes in
+ * its mask (tree_plan, which also makes pos; kv_attn_tree).  The path that the model's picks
+ * follow (tree_accept) is then moved together in the caches (kv_tree_keep).
+ *   pos        int32 [T] device, as tree_plan gives them;
+ *   tree_mask  uint64 [T][ceil(T / 64)] device, 8-byte aligned;
+ *   k_cache, v_cache  bf16, 16-byte aligned;
+ *   ws         at least layer_workspace_size(layer, 3, 1, T, hist_len).
+ * Errors: as layer_prefill_kv, W4_EUNSUPPORTED (T, a layer on a 4-bit cache). */
+int layer_verify_tree(layer_t layer, const float* x, const int32_t* pos, const uint64_t* tree_mask, int32_t T,
+                      int32_t hist_len, void* k_cache, void* v_cache, float* y,
+                      void* ws, size_t ws_bytes, void* stream);
 
 /* Long prompts in segments (the third scenario of Sec. 4.1): tokens
  * 0..chunk-1 by layer_prefill, then every following run of chunk tokens
@@ -298,6 +313,7 @@ size_t layer_decode_noalloc_max_bytes(void);
  * history up to max_ctx) or 2 (decode: batch sequences, context up to
  * max_ctx); 0 for invalid arguments.
  * stack_prefill: every layer runs layer_prefill_kv with hist_len (0: prefill).
+ * stack_verify_tree: every layer runs layer_verify_tree (workspace: stage 3).
  * stack_decode: every layer runs layer_decode with the same pos, ctx_lens,
  * max_ctx, attn_mask and B.
  * Errors: those of the single-layer calls, and W4_EINVAL for a null or
@@ -308,6 +324,9 @@ size_t stack_workspace_size(const layer_t* layers, int32_t n_layers, int32_t sta
 int stack_prefill(const layer_t* layers, int32_t n_layers, const float* x, const int32_t* pos,
                   int32_t T, int32_t hist_len, void* const* k_caches, void* const* v_caches,
                   float* y, void* ws, size_t ws_bytes, void* stream);
+int stack_verify_tree(const layer_t* layers, int32_t n_layers, const float* x, const int32_t* pos,
+                      const uint64_t* tree_mask, int32_t T, int32_t hist_len, void* const* k_caches,
+                      void* const* v_caches, float* y, void* ws, size_t ws_bytes, void* stream);
 int stack_decode(const layer_t* layers, int32_t n_layers, const float* x, const int32_t* pos,
                  const int32_t* ctx_lens, int32_t max_ctx, const float* attn_mask, int32_t B,
                  void* const* k_caches, void* const* v_caches, float* y,
@@ -535,8 +554,18 @@ int kv4_attn_prefill(const kv4_desc* desc, const void* q, int32_t T, int32_t his
  * raises W4_FLAG_F16_RANGE.  Workspace sizes depend on the format: set it
  * first.  Such a layer decodes as the kernel sequence; with decode path 2 its
  * decode calls are refused (W4_EUNSUPPORTED).  Errors: W4_EINVAL,
- * W4_EUNSUPPORTED (max_seq). */
+ * W4_EUNSUPPORTED (max_seq, a layer with a window). */
 int layer_set_kv_format(layer_t layer, int32_t format);
+
+/* Attention window of a layer's calls from now on: a token at slot p attends
+ * to slots p - window + 1 .. p and to the first `sinks` slots; window 0 (the
+ * default): to all.  It counts for every stage, chunk, stack and model call, whose caches
+ * are then 16-byte aligned; slots before the window (and behind the sinks) are not read any
+ * more and may hold anything.  Workspace sizes depend on it: set it first.
+ * Such a layer decodes as the kernel sequence; with decode path 2 its decode calls
+ * are refused (W4_EUNSUPPORTED).  Errors: W4_EINVAL, W4_EUNSUPPORTED (a layer on a 4-bit cache, max_seq
+ * beyond 2^27). */
+int layer_set_window(layer_t layer, int32_t window, int32_t sinks);
 
 /* ---- attention over the bf16 cache: window, sinks, draft trees ---------------- */
 
@@ -577,7 +606,7 @@ int layer_set_kv_format(layer_t layer, int32_t format);
  * 0 .. ctx_lens[b] - 1, within its window and the sinks, and those nodes whose bit
  * is set in its mask.  Both come from tree_plan, with the same window and sinks.
  * q and out are [B][N][n_heads][head_dim].
- *   tree_mask  uint64 [B][N][ceil(N / 64)] device: bit a % 64 of word a / 64 of
+ *   tree_mask  uint64 [B][N][ceil(N / 64)] device, 8-byte aligned: bit a % 64 of word a / 64 of
  *              node i is set if it sees node a (its own among them);
  *   pos        int32 [B][N] device, every one >= ctx_lens[b]; may be NULL without a window;
  *   ws         at least kv_attn_workspace_size(desc, n_heads, 3, B, N, max_ctx).
@@ -585,8 +614,8 @@ int layer_set_kv_format(layer_t layer, int32_t format);
  * The workspace may hold anything, and belongs to one call at a time.
  * kv_attn_workspace_size: 0 for invalid arguments; it does not decrease with B, T
  * or max_ctx, and serves every window.
- * Errors: W4_EINVAL, W4_ECAPACITY (B > desc->batch, slots beyond max_seq, more rows than a launch
- * takes), W4_EUNSUPPORTED (heads, head_dim, N), W4_EWORKSPACE, W4_EHIP. */
+ * Errors: W4_EINVAL, W4_ECAPACITY (B > desc->batch, slots beyond max_seq, more than 2^26 queries
+ * times heads in a sequence or 2^30 in the batch), W4_EUNSUPPORTED (heads, head_dim, N), W4_EWORKSPACE, W4_EHIP. */
 #define W4_TREE_MAX 256
 size_t kv_attn_workspace_size(const kv_desc* desc, int32_t n_heads, int32_t stage, int32_t B, int32_t T,
                               int32_t max_ctx);
@@ -637,7 +666,7 @@ int kv_append_step(const kv_desc* desc, void* k_cache, void* v_cache, const void
  * (host arrays, at most 1024; one pair per layer, all in the layout of *desc and none twice).  The context is then ctx_lens[b] +
  * n_path[b] tokens.  The other slots keep what they held.  Sequences with ctx_lens[b] < 0 are left alone; so
  * is a move whose slots are not below max_seq or whose node is not in t .. N-1.
- * Errors: W4_EINVAL, W4_EUNSUPPORTED (N, *desc as for the attention calls), W4_ECAPACITY (B, n_caches), W4_EHIP. */
+ * Errors: W4_EINVAL, W4_EUNSUPPORTED (N, *desc as for the attention calls), W4_ECAPACITY (B beyond the cache's batch or 65535, n_caches), W4_EHIP. */
 int tree_plan(const int32_t* parents, const int32_t* ctx_lens, int32_t B, int32_t N, int32_t window, int32_t sinks,
               uint64_t* tree_mask, int32_t* pos, void* stream);
 int tree_accept(const int32_t* parents, const int32_t* tokens, const int32_t* picks, int32_t B, int32_t N,

@@ -99,6 +99,9 @@ _SIG = {
     "layer_workspace_size": (ctypes.c_size_t, [_P, _I, _I, _I, _I]),
     "layer_prefill": (ctypes.c_int, [_P, _P, _P, _I, _P, _P, _P, _P, ctypes.c_size_t, _P]),
     "layer_prefill_kv": (ctypes.c_int, [_P, _P, _P, _I, _I, _P, _P, _P, _P, ctypes.c_size_t, _P]),
+    "layer_verify_tree": (ctypes.c_int, [_P, _P, _P, _P, _I, _I, _P, _P, _P, _P, ctypes.c_size_t, _P]),
+    "layer_set_window": (ctypes.c_int, [_P, _I, _I]),
+    "stack_verify_tree": (ctypes.c_int, [_P, _I, _P, _P, _P, _I, _I, _P, _P, _P, _P, ctypes.c_size_t, _P]),
     "layer_prefill_chunked_workspace_size": (ctypes.c_size_t, [_P, _I, _I]),
     "layer_prefill_chunked": (ctypes.c_int, [_P, _P, _P, _I, _I, _P, _P, _P, _P, ctypes.c_size_t, _P]),
     "layer_decode": (ctypes.c_int, [_P, _P, _P, _P, _I, _P, _I, _P, _P, _P, _P, ctypes.c_size_t, _P]),
@@ -275,6 +278,15 @@ def layer_prefill_kv(handle, x, pos, T, hist_len, k_cache, v_cache, y, ws, ws_by
                                  _ptr(ws), ws_bytes, _stream(stream))
 
 
+def layer_verify_tree(handle, x, pos, tree_mask, T, hist_len, k_cache, v_cache, y, ws, ws_bytes, stream=None) -> int:
+    return _lib.layer_verify_tree(handle, _ptr(x), _ptr(pos), _ptr(tree_mask), T, hist_len, _ptr(k_cache), _ptr(v_cache),
+                                  _ptr(y), _ptr(ws), ws_bytes, _stream(stream))
+
+
+def layer_set_window(handle, window: int, sinks: int) -> int:
+    return _lib.layer_set_window(handle, window, sinks)
+
+
 def layer_prefill_chunked_workspace_size(handle, T, chunk) -> int:
     return _lib.layer_prefill_chunked_workspace_size(handle, T, chunk)
 
@@ -312,6 +324,11 @@ def stack_prefill(handles, x, pos, T, hist_len, k_caches, v_caches, y, ws, ws_by
     return _lib.stack_prefill(_ptr_array(handles), len(handles), _ptr(x), _ptr(pos), T, hist_len,
                               _ptr_array(k_caches), _ptr_array(v_caches), _ptr(y), _ptr(ws), ws_bytes,
                               _stream(stream))
+
+
+def stack_verify_tree(handles, x, pos, tree_mask, T, hist_len, k_caches, v_caches, y, ws, ws_bytes, stream=None) -> int:
+    return _lib.stack_verify_tree(_ptr_array(handles), len(handles), _ptr(x), _ptr(pos), _ptr(tree_mask), T, hist_len,
+                                  _ptr_array(k_caches), _ptr_array(v_caches), _ptr(y), _ptr(ws), ws_bytes, _stream(stream))
 
 
 def stack_decode(handles, x, pos, ctx_lens, max_ctx, attn_mask, B, k_caches, v_caches, y, ws, ws_bytes,
@@ -675,6 +692,15 @@ class Layer:
         ws, n = self.workspace(STAGE_PREFILL_KV, 1, x.shape[0], hist_len)
         check(layer_prefill_kv(self.handle, x, pos, x.shape[0], hist_len, k_cache, v_cache, y, ws, n, stream))
 
+    def set_window(self, window: int, sinks: int = 0):
+        """The attention window (0: none) and the first slots that stay visible, of the layer's calls from now on."""
+        check(layer_set_window(self.handle, window, sinks))
+
+    def verify_tree(self, x, pos, tree_mask, hist_len, k_cache, v_cache, y, stream=None):
+        """Drafted tokens of one sequence: pos [T], tree_mask [T][ceil(T / 64)] of a DraftTree's plan (its row of the batch)."""
+        ws, n = self.workspace(STAGE_TREE, 1, x.shape[0], hist_len)
+        check(layer_verify_tree(self.handle, x, pos, tree_mask, x.shape[0], hist_len, k_cache, v_cache, y, ws, n, stream))
+
     def prefill_chunked(self, x, pos, chunk, k_cache, v_cache, y, stream=None):
         import torch
         T = x.shape[0]
@@ -726,6 +752,10 @@ class Stack:
         stage = STAGE_PREFILL_KV if hist_len > 0 else STAGE_PREFILL
         ws, n = self.workspace(stage, 1, x.shape[0], hist_len)
         check(stack_prefill(self.handles, x, pos, x.shape[0], hist_len, k_caches, v_caches, y, ws, n, stream))
+
+    def verify_tree(self, x, pos, tree_mask, hist_len, k_caches, v_caches, y, stream=None):
+        ws, n = self.workspace(STAGE_TREE, 1, x.shape[0], hist_len)
+        check(stack_verify_tree(self.handles, x, pos, tree_mask, x.shape[0], hist_len, k_caches, v_caches, y, ws, n, stream))
 
     def decode(self, x, pos, ctx_lens, max_ctx, k_caches, v_caches, y, attn_mask=None, stream=None):
         B = x.shape[0]
@@ -957,11 +987,21 @@ class KVCache(_OnDevice):
         self._q_head = (cfg.n_heads, cfg.head_dim)
 
     def append(self, k_new, v_new, slot_start, stream=None):
-        """k_new, v_new [B][T][n_kv_heads][head_dim] into slots slot_start[b] .. + T - 1 (host integers)."""
+        """k_new, v_new [B][T][n_kv_heads][head_dim] into slots slot_start[b] .. + T - 1 (host integers).  For caches whose
+        slots follow each other (append_step takes any)."""
         B, T = k_new.shape[:2]
         shape = (B, T) + self._head
         kp, vp = self._tensor(k_new, shape, "k_new"), self._tensor(v_new, shape, "v_new")
-        check(_lib.kv_append(self._desc_ref, self._kp, self._vp, kp, vp, B, T, self._slots(slot_start, B), self._on(stream)))
+        if B > self.desc.batch:
+            raise ValueError(f"{B} sequences, a cache of {self.desc.batch}")
+        slots, st = list(slot_start), self._on(stream)
+        self._slots(slots, B)
+        if any(s < 0 or s + T > self.desc.max_seq for s in slots):       # (of all of them before the first is written)
+            raise W4Error(W4_ECAPACITY, f"slots {slots} + {T} of {self.desc.max_seq}")
+        for b in range(0, B, 64):            # (as many as kv_append takes)
+            n, cache, new = min(64, B - b), 2 * b * self.desc.stride_b, 2 * b * T * self._head[0] * self._head[1]
+            check(_lib.kv_append(self._desc_ref, self._kp + cache, self._vp + cache, kp + new, vp + new, n, T,
+                                 self._slots(slots[b:b + n], n), st))
 
     def append_step(self, k_new, v_new, ctx_lens, stream=None):
         """k_new, v_new [B][T][n_kv_heads][head_dim] into slots ctx_lens[b] .. + T - 1 (int32 [B] on the device)."""

@@ -288,6 +288,7 @@ struct layer_s {
     unsigned long long* stamps = nullptr;
     int decode_path = 0;   // 0 auto, 1 separate kernels, 2 persistent
     int kv_format = W4_KV_BF16;
+    int window = 0, sinks = 0;   // of the attention (window 0: none)
     bool decode_trace = false;   // persistent decode records its time stamps
     int spin_max = kSpinDefault; // polls per thread per persistent launch before a wait gives up
 };
@@ -445,12 +446,24 @@ GemmPlan prefill_gemm_plan(const layer_s* L, int T, int gemm, const DevLinear& W
 size_t kv_stage_half(const layer_s* L, int rows) { return (size_t)rows * L->cfg.n_kv_heads * L->cfg.head_dim * 2; }
 size_t kv_stage_bytes(const layer_s* L, int rows) { return 2 * kv_stage_half(L, rows); }
 
+// Calls whose attention is that of kv_attn.h: layers with a window, and draft trees.
+size_t kv_attn_bound(const layer_s* L, int B, int N, int max_ctx) {
+    const layer_config& c = L->cfg;
+    return kv_attn_part_bound(KvAttnShape{B, N, c.n_kv_heads, c.n_heads / c.n_kv_heads, c.head_dim, max_ctx, INT_MAX, 0, false, false});
+}
+
+// The nodes' masks and positions of a call on drafted tokens.
+struct DraftMask {
+    const uint64_t* mask;
+    const int32_t* pos;
+};
+
 struct PrefillWs {
-    size_t xn1, q, attn, h, xn2, g, part, cnt, kv, total;   // kv: bf16 keys and values on their way into a 4-bit cache
+    size_t xn1, q, attn, h, xn2, g, part, part_bytes, cnt, kv, total;   // kv: bf16 keys and values on their way into a 4-bit cache
     GemmPlan qkv, o, gu, down;
     AttnPrefillPlan at;
 };
-PrefillWs plan_prefill(const layer_s* L, int T, int hist) {
+PrefillWs plan_prefill(const layer_s* L, int T, int hist, bool tree = false) {
     const layer_config& c = L->cfg;
     const size_t qd = (size_t)c.n_heads * c.head_dim;
     Carve cv;
@@ -460,8 +473,10 @@ PrefillWs plan_prefill(const layer_s* L, int T, int hist) {
     w.gu = prefill_gemm_plan(L, T, 2, L->gu.d);
     w.down = prefill_gemm_plan(L, T, 3, L->down.d);
     const bool kv4 = L->kv_format == W4_KV_INT4;
-    if (!kv4) w.at = attn_prefill_plan(T, hist, c.n_heads, c.n_kv_heads, c.head_dim, L->num_cus);
-    const size_t at_part = kv4 ? kv4_prefill_plan(T, hist, c.n_kv_heads, c.n_heads / c.n_kv_heads, c.head_dim).part_bytes
+    const bool kva = tree || L->window > 0;
+    if (!kv4 && !kva) w.at = attn_prefill_plan(T, hist, c.n_heads, c.n_kv_heads, c.head_dim, L->num_cus);
+    const size_t at_part = kva ? kv_attn_bound(L, 1, T, hist)
+                         : kv4 ? kv4_prefill_plan(T, hist, c.n_kv_heads, c.n_heads / c.n_kv_heads, c.head_dim).part_bytes
                                : w.at.part_bound;
     w.xn1 = cv.take((size_t)T * c.hidden * 2);
     w.q = cv.take((size_t)T * qd * 2);
@@ -471,15 +486,17 @@ PrefillWs plan_prefill(const layer_s* L, int T, int hist) {
     w.g = cv.take((size_t)T * L->F_pad * 2);
     // split-K partials of each GEMM and the attention chunk states, used one kernel at a time
     const size_t split = L->split_bytes[std::min((T - 1) / 32, (int)L->split_bytes.size() - 1)];
-    w.part = cv.take(std::max({split, at_part, w.qkv.part_bytes, w.o.part_bytes, w.gu.part_bytes, w.down.part_bytes}));
+    w.part_bytes = std::max({split, at_part, w.qkv.part_bytes, w.o.part_bytes, w.gu.part_bytes, w.down.part_bytes});
+    w.part = cv.take(w.part_bytes);
     w.cnt = cv.take((size_t)4 * kGemmCounters * 4);   // split-K arrival counters, one set per GEMM
     w.kv = cv.take(kv4 ? kv_stage_bytes(L, T) : 0);
     w.total = cv.off;
     return w;
 }
 
-struct DecodeWs { size_t q, part, attn, h, g, xn, kv, total; int nsplit; };
-DecodeWs plan_decode(const layer_s* L, int B, int max_ctx) {
+struct DecodeWs { size_t q, part, part_bytes, attn, h, g, xn, kv, total; int nsplit; };
+// shared: the rows are tokens of one sequence (max_ctx: the last one's context); tree: drafted ones.
+DecodeWs plan_decode(const layer_s* L, int B, int max_ctx, bool shared = false, bool tree = false) {
     const layer_config& c = L->cfg;
     const size_t qd = (size_t)c.n_heads * c.head_dim;
     DecodeWs w;
@@ -493,8 +510,10 @@ DecodeWs plan_decode(const layer_s* L, int B, int max_ctx) {
     const int nchunks = (max_ctx + 64) / 64;
     Carve cv;
     w.q = cv.take((size_t)B * qd * 2);
-    w.part = cv.take(kv4 ? kv4_decode_part_bound(B, c.n_kv_heads, r, c.head_dim, max_ctx)
-                         : (size_t)B * c.n_heads * nchunks * (c.head_dim + 2) * 4);
+    w.part_bytes = tree || L->window > 0 ? (shared ? kv_attn_bound(L, 1, B, max_ctx) : kv_attn_bound(L, B, 1, max_ctx))
+                   : kv4 ? kv4_decode_part_bound(B, c.n_kv_heads, r, c.head_dim, max_ctx)
+                         : (size_t)B * c.n_heads * nchunks * (c.head_dim + 2) * 4;
+    w.part = cv.take(w.part_bytes);
     w.attn = cv.take((size_t)B * qd * 2);
     w.h = cv.take((size_t)B * c.hidden * 4);
     w.g = cv.take((size_t)B * L->F_pad * 2);
@@ -522,7 +541,7 @@ FusedPlan plan_fused(const layer_s* L, int B, int max_ctx, bool query_device) {
     FusedPlan p;
     const layer_config& c = L->cfg;
     if (B > 4 || L->decode_path == 1) return p;
-    if (L->kv_format != W4_KV_BF16) return p;                                // 4-bit cache: separate kernels
+    if (L->kv_format != W4_KV_BF16 || L->window > 0) return p;               // 4-bit cache, window: separate kernels
     if (L->qkv.d.wf != WF_INT4) return p;                                    // 8- and 16-bit weights: separate kernels
     if (L->qkv.d.sz || L->o.d.sz || L->gu.d.sz || L->down.d.sz) return p;   // zero points: separate kernels
     if (c.group_size < 64) return p;                                         // groups of 32: separate kernels
@@ -773,10 +792,53 @@ Kv4AttnArgs kv4_layer_attn(const layer_s* L, const uint16_t* q, const void* kc, 
     return a;
 }
 
-// A 4-bit cache's kernels take its tiles in 16-byte words.
-int check_cache(const layer_s* L, const void* kc, const void* vc) {
-    if (L->kv_format == W4_KV_INT4 && ((uintptr_t)kc % 16 || (uintptr_t)vc % 16))
-        return fail(W4_EINVAL, "a 4-bit cache must be 16-byte aligned");
+// Attention within the layer's window, or (tree) of drafted tokens.  shared: the rows are tokens of one sequence.
+KvAttnArgs kv_attn_layer(const layer_s* L, const uint16_t* q, const void* kc, const void* vc, f16* out, int rows, bool shared,
+                         const int32_t* ctx_lens, int ctx_base, int max_ctx, const DraftMask* tree, void* part) {
+    const layer_config& c = L->cfg;
+    KvAttnArgs a{};
+    a.q = q;
+    a.k = (const uint16_t*)kc;
+    a.v = (const uint16_t*)vc;
+    a.stride_s = c.head_dim;
+    a.stride_h = (long long)c.max_seq * c.head_dim;
+    a.stride_b = shared ? 0 : a.stride_h * c.n_kv_heads;
+    a.ctx_lens = shared ? nullptr : ctx_lens;
+    a.ctx_base = ctx_base;
+    a.max_ctx = shared ? ctx_base : max_ctx;
+    a.window = L->window > 0 ? L->window : INT_MAX;
+    a.sinks = L->window > 0 ? L->sinks : 0;
+    a.max_seq = c.max_seq;
+    if (tree) {
+        a.tree = (const unsigned long long*)tree->mask;
+        a.pos = L->window > 0 ? tree->pos : nullptr;
+        a.words = (rows + 63) / 64;
+    }
+    a.out = (uint16_t*)out;
+    a.out_f16 = 1;
+    a.err = L->err;
+    a.B = shared ? 1 : rows;
+    a.N = shared ? rows : 1;
+    a.nq = c.n_heads;
+    a.nkv = c.n_kv_heads;
+    a.d = c.head_dim;
+    a.scale = (float)(1.0 / std::sqrt((double)c.head_dim));
+    a.part = (float*)part;
+    return a;
+}
+
+// The kernels of a 4-bit cache, a window and draft trees read the cache in 16-byte words.
+int check_cache(const layer_s* L, const void* kc, const void* vc, bool tree = false) {
+    if ((L->kv_format == W4_KV_INT4 || L->window > 0 || tree) && ((uintptr_t)kc % 16 || (uintptr_t)vc % 16))
+        return fail(W4_EINVAL, "the caches must be 16-byte aligned");
+    return W4_OK;
+}
+
+constexpr long long kKvMaxRows = 1 << 26, kKvMaxBatchRows = 1 << 30;   // queries times heads of a sequence, of a batch
+                                                                       // (a launch's threads along x stay below 2^32)
+int check_rows(const layer_s* L, int T, bool tree) {
+    if ((tree || L->window > 0) && (long long)T * L->cfg.n_heads > kKvMaxRows)
+        return fail(W4_ECAPACITY, "%d tokens of %d heads within a window", T, L->cfg.n_heads);
     return W4_OK;
 }
 
@@ -789,9 +851,9 @@ int check_cache(const layer_s* L, const void* kc, const void* vc) {
 // launches count for (2 decode, 0/1 prefill).
 int run_decode_seq(layer_s* L, const float* x, const int32_t* pos, const int32_t* ctx_lens, int ctx_base, bool shared,
                    const float* attn_mask, int B, int max_ctx, void* kc, void* vc, float* y, void* ws,
-                   size_t ws_bytes, hipStream_t st, int ps_stage, bool ordered) {
+                   size_t ws_bytes, hipStream_t st, int ps_stage, bool ordered, const DraftMask* tree = nullptr) {
     const layer_config& c = L->cfg;
-    const DecodeWs w = plan_decode(L, B, max_ctx);
+    const DecodeWs w = plan_decode(L, B, max_ctx, shared, tree != nullptr);
     if (ws_bytes < w.total) return fail(W4_EWORKSPACE, "workspace %zu bytes, need %zu", ws_bytes, w.total);
     char* base = (char*)ws;
     uint16_t* q = (uint16_t*)(base + w.q);
@@ -832,7 +894,8 @@ int run_decode_seq(layer_s* L, const float* x, const int32_t* pos, const int32_t
     a1.clear = h;
     a1.nclear = a2.ksplit > 1 ? B * H : 0;
     a1.zero = (unsigned*)g;                 // the attention's arrival counters
-    a1.nzero = !kv4 && w.nsplit > 1 ? B * c.n_kv_heads : 0;
+    const bool kva = tree || L->window > 0;
+    a1.nzero = !kv4 && !kva && w.nsplit > 1 ? B * c.n_kv_heads : 0;
     // the rows are normalised in every block, or, many of them, once beforehand
     const bool prenorm = !gemv_norm_fits(B, H);
     f16* xn = (f16*)(base + w.xn);
@@ -872,7 +935,12 @@ int run_decode_seq(layer_s* L, const float* x, const int32_t* pos, const int32_t
     ad.cnt = (unsigned*)g;
     ad.scale_log2 = (float)(1.4426950408889634 / std::sqrt((double)d));
     ad.err = L->err;
-    if (!kv4) {
+    if (kva) {
+        KvAttnArgs wa = kv_attn_layer(L, q, kc, vc, attn, B, shared, ctx_lens, ctx_base, max_ctx, tree, part);
+        wa.mask = attn_mask;
+        ProfScope ps(L, ps_stage, ps_stage == 2 ? 1 : 2, st);
+        rc |= launch_kv_attn(wa, w.part_bytes, st);
+    } else if (!kv4) {
         ProfScope ps(L, ps_stage, ps_stage == 2 ? 1 : 2, st);
         rc |= launch_attn_decode(ad, st);
     }
@@ -953,16 +1021,16 @@ FusedPlan small_prefill_plan(layer_s* L, int T, int hist) {
 }
 bool small_prefill_seq(const layer_s* L, int T) { return L->decode_path == 0 && T <= 8; }
 
-size_t prefill_ws_bytes(layer_s* L, int T, int hist) {
-    size_t n = plan_prefill(L, T, hist).total;
-    const FusedPlan fp = small_prefill_plan(L, T, hist);
+size_t prefill_ws_bytes(layer_s* L, int T, int hist, bool tree = false) {
+    size_t n = plan_prefill(L, T, hist, tree).total;
+    const FusedPlan fp = tree ? FusedPlan{} : small_prefill_plan(L, T, hist);
     if (fp.ok) n = std::max(n, fp.total);
-    if (small_prefill_seq(L, T)) n = std::max(n, plan_decode(L, T, hist + T - 1).total);
+    if (small_prefill_seq(L, T)) n = std::max(n, plan_decode(L, T, hist + T - 1, true, tree).total);
     return n;
 }
 
 int run_prefill(layer_s* L, const float* x, const int32_t* pos, int T, int hist, void* kc, void* vc, float* y,
-                void* ws, size_t ws_bytes, void* stream_) {
+                void* ws, size_t ws_bytes, void* stream_, const DraftMask* tree = nullptr) {
     if (!L) return fail(W4_EINVAL, "null layer");
     if (!x || !pos || !kc || !vc || !y || !ws) return fail(W4_EINVAL, "null pointer argument");
     if ((const void*)x == (const void*)y) return fail(W4_EINVAL, "x and y must not alias");
@@ -971,9 +1039,9 @@ int run_prefill(layer_s* L, const float* x, const int32_t* pos, int T, int hist,
     if ((long long)hist + T > c.max_seq) return fail(W4_ECAPACITY, "hist_len + T = %lld exceeds max_seq %d", (long long)hist + T, c.max_seq);
     hipStream_t st = (hipStream_t)stream_;
     int rc0;
-    if ((rc0 = check_cache(L, kc, vc))) return rc0;
+    if ((rc0 = check_cache(L, kc, vc, tree != nullptr)) || (rc0 = check_rows(L, T, tree != nullptr))) return rc0;
     const int stage = hist > 0 ? 1 : 0;
-    FusedPlan fp = small_prefill_plan(L, T, hist);
+    FusedPlan fp = tree ? FusedPlan{} : small_prefill_plan(L, T, hist);
     const bool cap = fp.ok && capturing(st);
     if (cap && L->decode_path == 2) fp.ok = false;         // (the prefill kernels)
     const bool seq = fp.ok && (cap || (prefer_seq(L, T, hist + T - 1) && ws_bytes >= plan_decode(L, T, hist + T - 1).total));
@@ -985,8 +1053,8 @@ int run_prefill(layer_s* L, const float* x, const int32_t* pos, int T, int hist,
         return W4_OK;
     }
     if (small_prefill_seq(L, T))
-        return run_decode_seq(L, x, pos, nullptr, hist, true, nullptr, T, hist + T - 1, kc, vc, y, ws, ws_bytes, st, stage, seq);
-    const PrefillWs w = plan_prefill(L, T, hist);
+        return run_decode_seq(L, x, pos, nullptr, hist, true, nullptr, T, hist + T - 1, kc, vc, y, ws, ws_bytes, st, stage, seq, tree);
+    const PrefillWs w = plan_prefill(L, T, hist, tree != nullptr);
     if (ws_bytes < w.total) return fail(W4_EWORKSPACE, "workspace %zu bytes, need %zu", ws_bytes, w.total);
     char* base = (char*)ws;
     f16* xn1 = (f16*)(base + w.xn1);
@@ -1035,7 +1103,10 @@ int run_prefill(layer_s* L, const float* x, const int32_t* pos, int T, int hist,
     aa.scale_log2 = (float)(1.4426950408889634 / std::sqrt((double)d));
     aa.part = part;
     aa.err = L->err;
-    if (!kv4) {
+    if (tree || L->window > 0) {
+        ProfScope ps(L, stage, 2, st);
+        rc |= launch_kv_attn(kv_attn_layer(L, q, kc, vc, attn, T, true, nullptr, hist, hist, tree, part), w.part_bytes, st);
+    } else if (!kv4) {
         ProfScope ps(L, stage, 2, st);
         rc |= launch_attn_prefill(aa, w.at, st);
     }
@@ -1105,6 +1176,17 @@ int prefill_check(layer_s* L, int T, int hist) {
     if (T < 1 || hist < 0) return fail(W4_EINVAL, "T must be >= 1 and hist_len >= 0");
     if ((long long)hist + T > L->cfg.max_seq)
         return fail(W4_ECAPACITY, "hist_len + T = %lld exceeds max_seq %d", (long long)hist + T, L->cfg.max_seq);
+    return check_rows(L, T, false);
+}
+
+// The same for a call on T drafted tokens.
+int tree_check(layer_s* L, int T, int hist, const DraftMask& tree) {
+    int rc;
+    if ((rc = prefill_check(L, T, hist))) return rc;
+    if (T > W4_TREE_MAX) return fail(W4_EUNSUPPORTED, "T = %d, at most %d drafted tokens", T, W4_TREE_MAX);
+    if (!tree.mask) return fail(W4_EINVAL, "null pointer argument");
+    if ((uintptr_t)tree.mask % 8) return fail(W4_EINVAL, "tree_mask must be 8-byte aligned");
+    if (L->kv_format != W4_KV_BF16) return fail(W4_EUNSUPPORTED, "draft trees need a bf16 cache");
     return W4_OK;
 }
 
@@ -1294,6 +1376,10 @@ size_t layer_workspace_size(layer_t L, int32_t stage, int32_t batch, int32_t T, 
         if (T < 1 || max_ctx < 0) return 0;
         return prefill_ws_bytes(L, T, stage == 1 ? max_ctx : 0);
     }
+    if (stage == 3) {
+        if (T < 1 || T > W4_TREE_MAX || max_ctx < 0 || L->kv_format != W4_KV_BF16) return 0;
+        return prefill_ws_bytes(L, T, max_ctx, true);
+    }
     if (stage == 2) {
         if (batch < 1 || max_ctx < 0) return 0;
         size_t n = plan_decode(L, batch, max_ctx).total;
@@ -1312,6 +1398,14 @@ int layer_prefill(layer_t L, const float* x, const int32_t* pos, int32_t T, void
 int layer_prefill_kv(layer_t L, const float* x, const int32_t* pos, int32_t T, int32_t hist_len, void* kc, void* vc,
                      float* y, void* ws, size_t ws_bytes, void* stream) {
     return run_prefill(L, x, pos, T, hist_len, kc, vc, y, ws, ws_bytes, stream);
+}
+
+int layer_verify_tree(layer_t L, const float* x, const int32_t* pos, const uint64_t* tree_mask, int32_t T, int32_t hist_len,
+                      void* kc, void* vc, float* y, void* ws, size_t ws_bytes, void* stream) {
+    if (!L) return fail(W4_EINVAL, "null layer");
+    const DraftMask tree{tree_mask, pos};
+    if (int rc = tree_check(L, T, hist_len, tree)) return rc;
+    return run_prefill(L, x, pos, T, hist_len, kc, vc, y, ws, ws_bytes, stream, &tree);
 }
 
 size_t layer_prefill_chunked_workspace_size(layer_t L, int32_t T, int32_t chunk) {
@@ -1595,7 +1689,6 @@ int kv4_attn_prefill(const kv4_desc* d, const void* q, int32_t T, int32_t hist_l
 
 // ---------------------------------------------------------------- attention over the bf16 cache, draft trees
 
-constexpr int kKvMaxRows = INT_MAX - 256;        // of a kv head: queries times heads, in whole tiles
 constexpr int64_t kKvMaxStride = 1 << 24;        // (64 slots' offsets fit 32 bits)
 
 // B is the batch of a call on the cache; of a launch, at most 65535.
@@ -1625,6 +1718,7 @@ static int check_kv_heads(const kv_desc* d, int32_t n_heads) {
 static int check_tree_size(int32_t B, int32_t N) {
     if (B < 1 || N < 1) return fail(W4_EINVAL, "B and N must be >= 1");
     if (N > W4_TREE_MAX) return fail(W4_EUNSUPPORTED, "N = %d, at most %d", N, W4_TREE_MAX);
+    if (B > 65535) return fail(W4_ECAPACITY, "B = %d, at most 65535", B);
     return W4_OK;
 }
 
@@ -1648,8 +1742,8 @@ static int kv_attn_run(const kv_desc* d, KvAttnArgs a, int32_t stage, int32_t wi
                        const void* kc, const void* vc, void* out, void* ws, size_t ws_bytes, void* stream) {
     int rc;
     if ((rc = check_kv_desc(d, a.B)) || (rc = check_kv_heads(d, n_heads)) || (rc = check_window(window, sinks))) return rc;
-    const long long slots = (long long)a.max_ctx + a.N, rows = (long long)a.N * (n_heads / d->n_kv_heads);
-    if (rows > kKvMaxRows) return fail(W4_ECAPACITY, "%lld rows per kv head, at most %d", rows, kKvMaxRows);
+    const long long slots = (long long)a.max_ctx + a.N, rows = (long long)a.N * n_heads;
+    if (rows > kKvMaxRows || rows * a.B > kKvMaxBatchRows) return fail(W4_ECAPACITY, "%lld rows of %d sequences", rows, a.B);
     if (slots > d->max_seq) return fail(W4_ECAPACITY, "%lld slots, max_seq %d", slots, d->max_seq);
     if (!aligned16({q, kc, vc, out, ws})) return fail(W4_EINVAL, "pointers must be 16-byte aligned");
     if (q == out) return fail(W4_EINVAL, "q and out must not alias");
@@ -1711,6 +1805,7 @@ int kv_attn_tree(const kv_desc* d, const void* q, const int32_t* ctx_lens, int32
                  const void* vc, void* out, void* ws, size_t ws_bytes, void* stream) {
     if (!d || !q || !ctx_lens || !tree_mask || !kc || !vc || !out || !ws) return fail(W4_EINVAL, "null pointer argument");
     if (window > 0 && !pos) return fail(W4_EINVAL, "a window needs the nodes' positions");
+    if ((uintptr_t)tree_mask % 8) return fail(W4_EINVAL, "tree_mask must be 8-byte aligned");
     if (max_ctx < 0) return fail(W4_EINVAL, "max_ctx must be >= 0");
     if (int rc = check_tree_size(B, N)) return rc;
     KvAttnArgs a{};
@@ -1754,6 +1849,7 @@ int kv_append_step(const kv_desc* d, void* kc, void* vc, const void* k_new, cons
 int tree_plan(const int32_t* parents, const int32_t* ctx_lens, int32_t B, int32_t N, int32_t window, int32_t sinks,
               uint64_t* tree_mask, int32_t* pos, void* stream) {
     if (!parents || !ctx_lens || !tree_mask || !pos) return fail(W4_EINVAL, "null pointer argument");
+    if ((uintptr_t)tree_mask % 8) return fail(W4_EINVAL, "tree_mask must be 8-byte aligned");
     int rc;
     if ((rc = check_tree_size(B, N)) || (rc = check_window(window, sinks))) return rc;
     const TreePlanArgs a{parents, ctx_lens, B, N, window ? window : INT_MAX, sinks, (unsigned long long*)tree_mask, pos};
@@ -1854,25 +1950,41 @@ size_t stack_workspace_size(const layer_t* layers, int32_t n, int32_t stage, int
     return stack_act_offset(w) + 2 * rows * layers[0]->cfg.hidden * sizeof(float);
 }
 
-int stack_prefill(const layer_t* layers, int32_t n, const float* x, const int32_t* pos, int32_t T, int32_t hist_len,
-                  void* const* k_caches, void* const* v_caches, float* y, void* ws, size_t ws_bytes, void* stream) {
+// tree: of drafted tokens, or null.
+static int stack_run(const layer_t* layers, int32_t n, const float* x, const int32_t* pos, int32_t T, int32_t hist_len,
+                     void* const* k_caches, void* const* v_caches, float* y, void* ws, size_t ws_bytes, void* stream,
+                     const DraftMask* tree) {
     int rc;
     if ((rc = check_stack(layers, n))) return rc;
     if (!x || !y || !ws || !k_caches || !v_caches) return fail(W4_EINVAL, "null pointer argument");
     if ((const void*)x == (const void*)y) return fail(W4_EINVAL, "x and y must not alias");
     for (int i = 0; i < n; i++)
-        if ((rc = prefill_check(layers[i], T, hist_len)) || (rc = check_cache(layers[i], k_caches[i], v_caches[i]))) return rc;
-    const size_t need = stack_workspace_size(layers, n, hist_len > 0 ? 1 : 0, 1, T, hist_len);
+        if ((rc = tree ? tree_check(layers[i], T, hist_len, *tree) : prefill_check(layers[i], T, hist_len)) ||
+            (rc = check_cache(layers[i], k_caches[i], v_caches[i], tree != nullptr)))
+            return rc;
+    const size_t need = stack_workspace_size(layers, n, tree ? 3 : hist_len > 0 ? 1 : 0, 1, T, hist_len);
     if (need == 0 || ws_bytes < need) return fail(W4_EWORKSPACE, "workspace %zu bytes, need %zu", ws_bytes, need);
     const size_t act = stack_act_offset(need - 2 * (size_t)T * layers[0]->cfg.hidden * sizeof(float));
     float* buf[2] = {(float*)((char*)ws + act), (float*)((char*)ws + act) + (size_t)T * layers[0]->cfg.hidden};
     const float* in = x;
     for (int i = 0; i < n; i++) {
         float* out = i == n - 1 ? y : buf[i & 1];
-        if ((rc = run_prefill(layers[i], in, pos, T, hist_len, k_caches[i], v_caches[i], out, ws, act, stream))) return rc;
+        if ((rc = run_prefill(layers[i], in, pos, T, hist_len, k_caches[i], v_caches[i], out, ws, act, stream, tree))) return rc;
         in = out;
     }
     return W4_OK;
+}
+
+int stack_prefill(const layer_t* layers, int32_t n, const float* x, const int32_t* pos, int32_t T, int32_t hist_len,
+                  void* const* k_caches, void* const* v_caches, float* y, void* ws, size_t ws_bytes, void* stream) {
+    return stack_run(layers, n, x, pos, T, hist_len, k_caches, v_caches, y, ws, ws_bytes, stream, nullptr);
+}
+
+int stack_verify_tree(const layer_t* layers, int32_t n, const float* x, const int32_t* pos, const uint64_t* tree_mask, int32_t T,
+                      int32_t hist_len, void* const* k_caches, void* const* v_caches, float* y, void* ws, size_t ws_bytes,
+                      void* stream) {
+    const DraftMask tree{tree_mask, pos};
+    return stack_run(layers, n, x, pos, T, hist_len, k_caches, v_caches, y, ws, ws_bytes, stream, &tree);
 }
 
 int stack_decode(const layer_t* layers, int32_t n, const float* x, const int32_t* pos, const int32_t* ctx_lens,
@@ -1953,7 +2065,18 @@ int layer_set_kv_format(layer_t L, int32_t format) {
     if (format != W4_KV_BF16 && format != W4_KV_INT4) return fail(W4_EINVAL, "unknown cache format %d", format);
     if (format == W4_KV_INT4 && L->cfg.max_seq > kKv4MaxSeq)
         return fail(W4_EUNSUPPORTED, "max_seq must be at most 2^27 for a 4-bit cache");
+    if (format == W4_KV_INT4 && L->window > 0) return fail(W4_EUNSUPPORTED, "the layer has a window, which needs a bf16 cache");
     L->kv_format = format;
+    return W4_OK;
+}
+
+int layer_set_window(layer_t L, int32_t window, int32_t sinks) {
+    if (!L) return fail(W4_EINVAL, "null layer");
+    if (window < 0 || sinks < 0) return fail(W4_EINVAL, "window and sinks must be >= 0");
+    if (window > 0 && L->kv_format != W4_KV_BF16) return fail(W4_EUNSUPPORTED, "a window needs a bf16 cache");
+    if (window > 0 && L->cfg.max_seq > kKv4MaxSeq) return fail(W4_EUNSUPPORTED, "max_seq must be at most 2^27 for a window");
+    L->window = window;
+    L->sinks = sinks;
     return W4_OK;
 }
 

@@ -21,7 +21,9 @@ struct KvAttnArgs {
     const unsigned long long* tree;   // [B][N][words], or null
     const int32_t* pos;      // [B][N]; null: no window
     int words;
-    uint16_t* out;           // bf16 [B][N][nq][d]
+    uint16_t* out;           // [B][N][nq][d]: bf16, or (out_f16) bf16 values held as fp16
+    int out_f16;
+    int* err;                // raised with W4_FLAG_F16_RANGE (out_f16), or null
     int B, N, nq, nkv, d;
     float scale;             // of the scores
     int nsplit;              // set by the launcher: shares of a row tile's keys,

@@ -52,6 +52,15 @@ __device__ __forceinline__ bool not_finite(u32x4 w) {
     return bad;
 }
 
+// Two neighbouring outputs, as the caller takes them.
+__device__ __forceinline__ uint32_t out_pair(const KvAttnArgs& a, float x, float y, bool& bad) {
+    if (a.out_f16) {
+        const f16 u = act_f16(x, bad), v = act_f16(y, bad);
+        return (uint32_t)__builtin_bit_cast(uint16_t, u) | (uint32_t)__builtin_bit_cast(uint16_t, v) << 16;
+    }
+    return (uint32_t)bf16_bits_rne(x) | (uint32_t)bf16_bits_rne(y) << 16;
+}
+
 // ---------------------------------------------------------------- what rows see
 
 // First slot of the window at position p.
@@ -295,6 +304,7 @@ __global__ void __launch_bounds__(64 * FW) kv_attn_few_kernel(KvAttnArgs a) {
     const size_t slot = (((size_t)b * a.nkv + hk) * a.nsplit + part) * R + row0;
     float* const po = a.part + slot * D;
     float2* const pst = reinterpret_cast<float2*>(a.part + (size_t)a.B * a.nkv * a.nsplit * R * D) + slot;
+    bool range = false;
     for (int idx = tid; idx < nr * (D / 2); idx += 64 * FW) {
         const int lr = idx / (D / 2), d = 2 * (idx % (D / 2));
         float M = -INFINITY;
@@ -313,13 +323,13 @@ __global__ void __launch_bounds__(64 * FW) kv_attn_few_kernel(KvAttnArgs a) {
         if (a.nsplit == 1) {
             const int orow = row0 + lr;
             const float u = lt == 0.f ? 0.f : x / lt, v = lt == 0.f ? 0.f : y / lt;
-            *reinterpret_cast<uint32_t*>(a.out + (((size_t)b * a.N + orow / r) * a.nq + hk * r + orow % r) * D + d) =
-                (uint32_t)bf16_bits_rne(u) | (uint32_t)bf16_bits_rne(v) << 16;
+            *reinterpret_cast<uint32_t*>(a.out + (((size_t)b * a.N + orow / r) * a.nq + hk * r + orow % r) * D + d) = out_pair(a, u, v, range);
         } else {
             *reinterpret_cast<float2*>(po + lr * D + d) = float2{x, y};
             if (d == 0) pst[lr] = float2{M, lt};
         }
     }
+    flag_range(a.err, range);
 }
 
 // Merges the shares of a row: one block each, wave w takes shares w, w + 4, ..;
@@ -369,12 +379,12 @@ __global__ void __launch_bounds__(256) kv_attn_few_merge_kernel(KvAttnArgs a) {
         join(sm[w][0][lane], sm[w][1][lane], v);
     }
     uint16_t* const out = a.out + (((size_t)b * a.N + row / r) * a.nq + hk * r + row % r) * D + E * lane;
-    if constexpr (E == 2) {
-        const float x = L == 0.f ? 0.f : acc[0] / L, y = L == 0.f ? 0.f : acc[1] / L;
-        *reinterpret_cast<uint32_t*>(out) = (uint32_t)bf16_bits_rne(x) | (uint32_t)bf16_bits_rne(y) << 16;
-    } else {
-        *out = bf16_bits_rne(L == 0.f ? 0.f : acc[0] / L);
-    }
+    bool range = false;
+    const float x = L == 0.f ? 0.f : acc[0] / L, y = E == 1 || L == 0.f ? 0.f : acc[E - 1] / L;
+    const uint32_t w = out_pair(a, x, y, range);
+    if constexpr (E == 2) *reinterpret_cast<uint32_t*>(out) = w;
+    else *out = (uint16_t)w;
+    flag_range(a.err, range);
 }
 
 // ---------------------------------------------------------------- many rows
@@ -669,14 +679,15 @@ __global__ void __launch_bounds__(64 * MW) kv_attn_many_kernel(KvAttnArgs a) {
     if (mt.n == 1) {
         if (row >= R) return;
         const float inv = lt == 0.f ? 0.f : 1.f / lt;
+        bool range = false;
         uint16_t* const out = a.out + (((size_t)mt.b * a.N + row / r) * a.nq + mt.hk * r + row % r) * D + 4 * h;
 #pragma unroll
         for (int i = 0; i < NS; i++)
 #pragma unroll
             for (int e = 0; e < 16; e += 4)
-                *reinterpret_cast<uint2*>(out + i * 32 + 2 * e) =
-                    uint2{(uint32_t)bf16_bits_rne(o[i][e] * inv) | (uint32_t)bf16_bits_rne(o[i][e + 1] * inv) << 16,
-                          (uint32_t)bf16_bits_rne(o[i][e + 2] * inv) | (uint32_t)bf16_bits_rne(o[i][e + 3] * inv) << 16};
+                *reinterpret_cast<uint2*>(out + i * 32 + 2 * e) = uint2{out_pair(a, o[i][e] * inv, o[i][e + 1] * inv, range),
+                                                                        out_pair(a, o[i][e + 2] * inv, o[i][e + 3] * inv, range)};
+        flag_range(a.err, range);
         return;
     }
     if (!active) return;
@@ -732,13 +743,14 @@ __global__ void __launch_bounds__(64) kv_attn_many_merge_kernel(KvAttnArgs a) {
     const float lt = L + __shfl_xor(L, 32, 64);
     if (row >= R) return;
     const float inv = lt == 0.f ? 0.f : 1.f / lt;
+    bool range = false;
     // (register e of block i is dim 32 i + 8 (e / 4) + 4 h + e % 4)
     uint16_t* const out = a.out + (((size_t)mt.b * a.N + row / r) * a.nq + mt.hk * r + row % r) * D + 2 * e0 + 4 * h;
 #pragma unroll
     for (int e = 0; e < 16; e += 4)
-        *reinterpret_cast<uint2*>(out + 2 * e) =
-            uint2{(uint32_t)bf16_bits_rne(acc[e] * inv) | (uint32_t)bf16_bits_rne(acc[e + 1] * inv) << 16,
-                  (uint32_t)bf16_bits_rne(acc[e + 2] * inv) | (uint32_t)bf16_bits_rne(acc[e + 3] * inv) << 16};
+        *reinterpret_cast<uint2*>(out + 2 * e) = uint2{out_pair(a, acc[e] * inv, acc[e + 1] * inv, range),
+                                                       out_pair(a, acc[e + 2] * inv, acc[e + 3] * inv, range)};
+    flag_range(a.err, range);
 }
 
 }  // namespace
@@ -839,11 +851,11 @@ size_t kv_attn_part_bytes(const KvAttnShape& s, const KvAttnPlan& p) {
     return (pairs * ((R + MROWS - 1) / MROWS) - p.whole) * p.nsplit * MROWS * (s.d + 4) * 4;
 }
 
-// (either kernel's; a product of what grows, and a constant)
+// (either kernel's, where both may be taken; a product of what grows, and a constant)
 size_t kv_attn_part_bound(const KvAttnShape& s) {
     const size_t R = (size_t)s.N * s.r, pairs = (size_t)s.B * s.nkv, slots = (size_t)s.max_ctx + s.N;
     const size_t few = std::min<size_t>(pairs * R * (slots / FKT + 2), (size_t)kFewBlocks * 16);
-    const size_t many = std::min<size_t>(pairs * ((R + MROWS - 1) / MROWS) * (slots / MKT + 2), kManyParts) * MROWS;
+    const size_t many = R <= 16 ? 0 : std::min<size_t>(pairs * ((R + MROWS - 1) / MROWS) * (slots / MKT + 2), kManyParts) * MROWS;
     return std::max<size_t>(256, std::max(few, many) * (s.d + 4) * 4);
 }
 
@@ -864,9 +876,9 @@ static int launch_many(const KvAttnArgs& a, hipStream_t stream) {
     x.rest = (int)(tiles - a.whole);
     const long long blocks = a.whole + (long long)x.rest * a.nsplit;
     if (tiles > INT_MAX || x.rest < 0 || blocks > INT_MAX) return -1;
-    const size_t lds = (size_t)8 * MKT * D * 2 + 4 * 8 + (size_t)MROWS * a.words * 8;
-    static LdsLimit lim;
-    if (ensure_lds_limit(lim, (const void*)kv_attn_many_kernel<D>, lds)) return -1;
+    const size_t fixed = (size_t)8 * MKT * D * 2 + 4 * 8, lds = fixed + (size_t)MROWS * a.words * 8;
+    static LdsLimit lim;                                     // (for the largest trees at once)
+    if (ensure_lds_limit(lim, (const void*)kv_attn_many_kernel<D>, fixed + (size_t)MROWS * (W4_TREE_MAX / 64) * 8)) return -1;
     hipLaunchKernelGGL(kv_attn_many_kernel<D>, dim3((unsigned)blocks), dim3(64 * MW), lds, stream, x);
     if (x.rest) hipLaunchKernelGGL(kv_attn_many_merge_kernel<D>, dim3(x.rest, MW, D / 32), dim3(64), 0, stream, x);
     return hipGetLastError() == hipSuccess ? 0 : -1;

@@ -187,6 +187,25 @@ def test_strided_caches():
     check_prefill(c, q, run_prefill(c, q, 100, 64, 4, row=1), 100, 64, 4, row=1)
 
 
+def test_append_of_more_sequences_than_a_launch_takes():
+    g = gen(19)
+    c = filled(g, 4, 2, 64, 40, 150)
+    want = [c.k.clone(), c.v.clone()]
+    new, slots = [randn(g, 130, 3, 2, 64) for _ in range(2)], [(7 * b) % 38 for b in range(130)]
+    c.append(*new, slots)
+    torch.cuda.synchronize()
+    for t, w, x in zip((c.k, c.v), want, new):
+        for b, s in enumerate(slots):
+            w[b, :, s:s + 3] = x[b].transpose(0, 1)
+        assert torch.equal(t, w)
+    with pytest.raises(binding.W4Error):
+        c.append(*new, slots[:-1] + [38])
+    with pytest.raises(ValueError):
+        c.append(*new, slots[:-1])
+    torch.cuda.synchronize()
+    assert torch.equal(c.k, want[0]) and torch.equal(c.v, want[1])
+
+
 def test_offsets_beyond_32_bits():
     """A window at the end of a cache of 2^24 slots and more: element and byte offsets beyond 2^31 and 2^32."""
     n = (1 << 24) + 4000

@@ -84,7 +84,14 @@ def test_attention_refusals(call):
     if call is not decode:
         assert call(t=0) == B.W4_EINVAL and call(t=-1) == B.W4_EINVAL
         assert call(t=BIG) in (B.W4_ECAPACITY, B.W4_EUNSUPPORTED)
+    if call is prefill:                      # (more queries times heads than a launch takes)
+        big = synth.replace(CFG, max_seq=1 << 27)
+        assert call(desc(1, big), t=1 << 21, n=0) == B.W4_EWORKSPACE and call(desc(1, big), t=(1 << 21) + 1) == B.W4_ECAPACITY
     if call is tree:
+        big = synth.replace(CFG, max_seq=1000)
+        assert call(desc(40000, big), b=32768, t=256, nq=128, n=0) == B.W4_EWORKSPACE
+        assert call(desc(40000, big), b=32769, t=256, nq=128) == B.W4_ECAPACITY
+        assert call(mask=P + 4) == B.W4_EINVAL
         assert call(t=257) == B.W4_EUNSUPPORTED
         assert call(pos=0) == B.W4_EINVAL and "positions" in B.layer_last_error()
 
@@ -142,6 +149,8 @@ def test_tree_refusals():
         assert accept(**{name: 0}) == B.W4_EINVAL
     for call in (plan, accept):
         assert call(b=0) == B.W4_EINVAL and call(n=0) == B.W4_EINVAL and call(n=257) == B.W4_EUNSUPPORTED
+        assert call(b=65536) == B.W4_ECAPACITY
+    assert plan(mask=P + 4) == B.W4_EINVAL
     assert plan(window=-1) == B.W4_EINVAL and plan(sinks=-1) == B.W4_EINVAL
 
 
