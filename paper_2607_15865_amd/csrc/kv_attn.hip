@@ -814,10 +814,11 @@ KvAttnPlan kv_attn_plan(const KvAttnShape& s) {
         longest = std::max(longest, t);
     }
     const double mean = sum / samples, start = s.tree ? 6.0 : 5.0;
-    const double t1 = (wide ? 1.0 : 0.85) * (R <= 32 ? 1.2 : R <= 128 ? 1.4 : 1.45), tf = t1 * (R <= 128 ? 1.1 : 1.2);
-    const double state = std::min<double>(R, MROWS) * (s.d + 4) * 8 / 5e6, floor = pairs * mean * MKT * s.d * 4 / 5.3e6;
+    const double t1 = (wide ? 1.0 : 0.85) * (R <= 32 ? 1.2 : R <= 128 ? 1.4 : 1.45), tf = t1 * (R <= 128 ? 1.1 : 1.2);   // of one block, with the chip full
+    const double state = std::min<double>(R, MROWS) * (s.d + 4) * 8 / 6e6, floor = pairs * mean * MKT * s.d * 4 / 5.3e6;
     auto rounds = [&](long long n, long long parts) {        // us of so many blocks, a row tile in n parts
-        const double t = parts <= kCus / 2 ? t1 : tf, part = (double)((longest + n - 1) / n) * t + start;
+        const double t = t1 + (tf - t1) * std::min(1.0, std::max(0.0, (double)parts / (kCus / 2) - 1));
+        const double part = (double)((longest + n - 1) / n) * t + start;
         if (parts <= kCus) return std::max(floor, part);
         if (mean > 0.9 * longest) return std::max(floor, (double)((parts + kCus - 1) / kCus) * part);
         return std::max(part, parts * (mean / n * t + start) / kCus + 0.5 * mean / n * t);      // (the longest go first)
