@@ -122,6 +122,9 @@ constexpr int FW = 8;            // waves per block
 // in the operand layout of P^T.  A maximum moves only when a score passes it by more
 // than 5 (weights below e^5); the weights are multiplied as bf16 pairs hi + lo: the matrix units
 // have the time, and the weights of short contexts keep 16 bits.
+//
+// Bound by the cache read: 32 rows of 28 heads of 4 of 128, windows of 8192 (538 MB), 96 us, 5.6 TB/s; alone on the chip a wave
+// takes 2.1 us a tile (d = 64: 1.2).  Tiles requested two ahead need more registers than there are: 114 against 99 us.
 template <int D>
 __global__ void __launch_bounds__(64 * FW) kv_attn_few_kernel(KvAttnArgs a) {
     constexpr int NCK = D / 8, KROWS = 64 / NCK, NV = FKT / KROWS, NS = D / 32, NDB = D / 16, RT = 16;
@@ -333,7 +336,7 @@ __global__ void __launch_bounds__(64 * FW) kv_attn_few_kernel(KvAttnArgs a) {
 }
 
 // Merges the shares of a row: one block each, wave w takes shares w, w + 4, ..;
-// their order does not depend on timing.
+// their order does not depend on timing.  A chain of loads: 2.8 us for 128 rows of 5 shares, 5.2 for 896 of 2.
 template <int D>
 __global__ void __launch_bounds__(256) kv_attn_few_merge_kernel(KvAttnArgs a) {
     constexpr int CB = 4, E = D / 64;        // shares of a wave requested together, dims of a lane
@@ -394,14 +397,25 @@ constexpr int MROWS = 32 * MW;   // rows per block
 constexpr int MKT = 64;          // keys per stage
 
 // One block: 256 rows of a (sequence, kv head), 32 to a wave, and a part of the
-// stages of 64 keys that they see.  Every thread takes 16-byte pieces of the next stage's K and V through
-// registers into LDS, in rows whose pieces are swizzled so that the operand reads of K, and the transposing reads
-// that take V^T, meet no bank twice.  Scores are formed transposed, S^T =
+// stages of 64 keys that they see.  K and V go straight from memory into an LDS ring of four stages each, requested
+// three (V: two) stages ahead (through registers, one stage ahead, a stage took 2.1 us in place of 1.45 with part of
+// the chip at work).  A row's 16-byte chunks are swizzled by choosing which one a lane asks for, so that the operand
+// reads of K, and the transposing reads that take V^T, meet no bank twice.  Scores are formed transposed, S^T =
 // K Q^T on the 32x32x16 MFMA, with the keys of a tile in an order (bits 2 and 3 of the row index
 // swapped) that leaves the weights in the operand layout of P^T.  A lane owns one row: the
 // online softmax needs a lane exchange only when a maximum moves, which it does when a
 // score passes it by more than 8 (log2 units).  The two halves of the block's waves run half
 // a stage apart: one multiplies while the other does its softmax.
+//
+// The weights are rounded to bf16, as the matrix units take them in one product (a pair would take half as much
+// again of a stage's matrix time): against 64 bits the outputs are off by 0.0023 in the norm, by 0.0017 with pairs,
+// which is the outputs' own rounding.
+//
+// Bound by the matrix units, the LDS reads (a wave reads a whole stage for its 32 rows: 128 bytes a cycle at the
+// full matrix rate) and the vector units about alike: a build without exponentials took 8% less, one without loads 8%, one
+// without the second product 20%.  8001 queries of 28 heads of 4 of 128 behind 2999, window 4096: 455 us, 1.02 PFLOP/s (a
+// library product of two 8192^2 bf16 matrices 1.25); 512 of 32 heads of 8 behind 8192 47 us.  A stage takes 1.2 us with one
+// wave's rows, 1.45 with all, 1.9 with all CUs at work.
 template <int D>
 constexpr int M_NREG = 2 + 16 * (D / 32);    // floats of a lane's state: maximum, sum, output
 
@@ -701,7 +715,8 @@ __global__ void __launch_bounds__(64 * MW) kv_attn_many_kernel(KvAttnArgs a) {
 }
 
 // Merges the parts of the row tiles that have more than one: block (row tile, wave of it, 32 dims), a lane its
-// registers of them, part after part in key order.
+// registers of them, eight parts of them asked for at once, joined in key order.  Bound by the chain of its loads and the states
+// (64 row tiles of 4 parts, 34 MB: 8 us, the caches hold most of them).
 template <int D>
 __global__ void __launch_bounds__(64) kv_attn_many_merge_kernel(KvAttnArgs a) {
     constexpr int CB = 8;                                    // parts requested together
@@ -772,7 +787,7 @@ static int tiles_of(const KvAttnShape& s, long long i0, long long i1) {
 // may be cut alone.  Measured (few and many rows, each in its best number of parts): 32 heads of 8 of 128, 1 sequence of 8190 tokens,
 // 4, 8, 16, 32 and 64 drafts 17.3 and 22.3, 17.4 and 22.3, 21.7 and 25.8, 36 and 27.4, 55 and 31.4; 16 sequences of 4000, 4, 8 and 13
 // drafts 53.3 and 55.1, 58.5 and 55.0, 98.7 and 61.4; 28 heads of 4, 8001 queries, 876 row tiles in one part 477, the last 108 in
-// two 454.  Tiles of 32 rows in the kernel of few rows (two column tiles) were within 3% of the better of these at best.
+// two 454.  Tiles of 32 rows in the kernel of few rows were within 3% of the better of these at best, of 64 rows slower.
 KvAttnPlan kv_attn_plan(const KvAttnShape& s) {
     KvAttnPlan best;
     double least = -1;
