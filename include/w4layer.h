@@ -232,7 +232,7 @@ int layer_prefill_kv(layer_t layer, const float* x, const int32_t* pos, int32_t 
  * its mask (tree_plan, which also makes pos; kv_attn_tree).  The path that the model's picks
  * follow (tree_accept) is then moved together in the caches (kv_tree_keep).
  *   pos        int32 [T] device, as tree_plan gives them;
- *   tree_mask  uint64 [T][ceil(T / 64)] device, 8-byte aligned;
+ *   tree_mask  uint64 [T][ceil(T / 64)] device, 8-byte aligned, planned with the layer's window and sinks;
  *   k_cache, v_cache  bf16, 16-byte aligned;
  *   ws         at least layer_workspace_size(layer, 3, 1, T, hist_len).
  * Errors: as layer_prefill_kv, W4_EUNSUPPORTED (T, a layer on a 4-bit cache). */
@@ -314,6 +314,8 @@ size_t layer_decode_noalloc_max_bytes(void);
  * max_ctx); 0 for invalid arguments.
  * stack_prefill: every layer runs layer_prefill_kv with hist_len (0: prefill).
  * stack_verify_tree: every layer runs layer_verify_tree (workspace: stage 3).
+ * One tree_mask serves layers of different windows if none is below T; else all have the same
+ * window and sinks (W4_EUNSUPPORTED).
  * stack_decode: every layer runs layer_decode with the same pos, ctx_lens,
  * max_ctx, attn_mask and B.
  * Errors: those of the single-layer calls, and W4_EINVAL for a null or
@@ -608,14 +610,15 @@ int layer_set_window(layer_t layer, int32_t window, int32_t sinks);
  * q and out are [B][N][n_heads][head_dim].
  *   tree_mask  uint64 [B][N][ceil(N / 64)] device, 8-byte aligned: bit a % 64 of word a / 64 of
  *              node i is set if it sees node a (its own among them);
- *   pos        int32 [B][N] device, every one >= ctx_lens[b]; may be NULL without a window;
+ *   pos        int32 [B][N] device, in ctx_lens[b] .. ctx_lens[b] + N - 1 (any other counts as the
+ *              nearest of these); may be NULL without a window;
  *   ws         at least kv_attn_workspace_size(desc, n_heads, 3, B, N, max_ctx).
  *
  * The workspace may hold anything, and belongs to one call at a time.
  * kv_attn_workspace_size: 0 for invalid arguments; it does not decrease with B, T
  * or max_ctx, and serves every window.
  * Errors: W4_EINVAL, W4_ECAPACITY (B > desc->batch, slots beyond max_seq, more than 2^26 queries
- * times heads in a sequence or 2^30 in the batch), W4_EUNSUPPORTED (heads, head_dim, N), W4_EWORKSPACE, W4_EHIP. */
+ * times heads in a sequence or 2^30 in the batch, more than 2^21 sequences times kv heads), W4_EUNSUPPORTED (heads, head_dim, N), W4_EWORKSPACE, W4_EHIP. */
 #define W4_TREE_MAX 256
 size_t kv_attn_workspace_size(const kv_desc* desc, int32_t n_heads, int32_t stage, int32_t B, int32_t T,
                               int32_t max_ctx);
@@ -649,7 +652,7 @@ int kv_append_step(const kv_desc* desc, void* k_cache, void* v_cache, const void
  * 1 <= N <= W4_TREE_MAX.  All deterministic, on the device, capturable.
  *
  * tree_plan: what the model's layers need: pos[b][i] = ctx_lens[b] + depth of
- * node i (0 for ctx_lens[b] < 0; int32 [B][N] out, also RoPE's positions) and
+ * node i (ctx_lens[b] < 0 counts as 0 here; int32 [B][N] out, also RoPE's positions) and
  * tree_mask (out, as kv_attn_tree takes it): node i sees itself and those ancestors a
  * with pos[a] > pos[i] - window (window 0: all) or pos[a] < sinks.
  *

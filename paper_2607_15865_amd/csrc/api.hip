@@ -834,7 +834,8 @@ int check_cache(const layer_s* L, const void* kc, const void* vc, bool tree = fa
     return W4_OK;
 }
 
-constexpr long long kKvMaxRows = 1 << 26, kKvMaxBatchRows = 1 << 30;   // queries times heads of a sequence, of a batch
+constexpr long long kKvMaxRows = 1 << 26, kKvMaxBatchRows = 1 << 30;   // queries times heads of a sequence, of a batch,
+constexpr long long kKvMaxPairs = 1 << 21;                             // sequences times kv heads of one
                                                                        // (a launch's threads along x stay below 2^32)
 int check_rows(const layer_s* L, int T, bool tree) {
     if ((tree || L->window > 0) && (long long)T * L->cfg.n_heads > kKvMaxRows)
@@ -1744,6 +1745,7 @@ static int kv_attn_run(const kv_desc* d, KvAttnArgs a, int32_t stage, int32_t wi
     if ((rc = check_kv_desc(d, a.B)) || (rc = check_kv_heads(d, n_heads)) || (rc = check_window(window, sinks))) return rc;
     const long long slots = (long long)a.max_ctx + a.N, rows = (long long)a.N * n_heads;
     if (rows > kKvMaxRows || rows * a.B > kKvMaxBatchRows) return fail(W4_ECAPACITY, "%lld rows of %d sequences", rows, a.B);
+    if ((long long)a.B * d->n_kv_heads > kKvMaxPairs) return fail(W4_ECAPACITY, "%d sequences of %d kv heads", a.B, d->n_kv_heads);
     if (slots > d->max_seq) return fail(W4_ECAPACITY, "%lld slots, max_seq %d", slots, d->max_seq);
     if (!aligned16({q, kc, vc, out, ws})) return fail(W4_EINVAL, "pointers must be 16-byte aligned");
     if (q == out) return fail(W4_EINVAL, "q and out must not alias");
@@ -1962,6 +1964,13 @@ static int stack_run(const layer_t* layers, int32_t n, const float* x, const int
         if ((rc = tree ? tree_check(layers[i], T, hist_len, *tree) : prefill_check(layers[i], T, hist_len)) ||
             (rc = check_cache(layers[i], k_caches[i], v_caches[i], tree != nullptr)))
             return rc;
+    // One mask has to be that of all layers: a window below T may hide a node from another.
+    for (int i = 1; tree && i < n; i++) {
+        const layer_s *L = layers[i], *F = layers[0];
+        const bool narrow = L->window > 0 && L->window < T, first = F->window > 0 && F->window < T;
+        if (narrow != first || (narrow && (L->window != F->window || L->sinks != F->sinks)))
+            return fail(W4_EUNSUPPORTED, "layer %d: a window below T = %d that is not the first layer's", i, T);
+    }
     const size_t need = stack_workspace_size(layers, n, tree ? 3 : hist_len > 0 ? 1 : 0, 1, T, hist_len);
     if (need == 0 || ws_bytes < need) return fail(W4_EWORKSPACE, "workspace %zu bytes, need %zu", ws_bytes, need);
     const size_t act = stack_act_offset(need - 2 * (size_t)T * layers[0]->cfg.hidden * sizeof(float));

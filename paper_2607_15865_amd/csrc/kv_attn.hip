@@ -91,10 +91,10 @@ __device__ __forceinline__ u64 up_to(int x, int kb) {
     return n < 0 ? 0 : n >= 63 ? ~0ull : (2ull << n) - 1;
 }
 
-// First slot of the window of query i of a sequence, and, as bits, what it sees of keys kb .. kb + 63; tree: its mask
-// (of a tree).
+// First slot of the window of query i of a sequence (a node's position within those that a tree can have, for which a block's
+// tiles are chosen), and, as bits, what it sees of keys kb .. kb + 63; tree: its mask (of a tree).
 __device__ __forceinline__ int row_low(const KvAttnArgs& a, int b, int i, int ctx) {
-    return window_low(a.tree ? (a.pos ? a.pos[(size_t)b * a.N + i] : ctx) : ctx + i, a.window);
+    return window_low(a.tree ? (a.pos ? min(max(a.pos[(size_t)b * a.N + i], ctx), ctx + a.N - 1) : ctx) : ctx + i, a.window);
 }
 __device__ __forceinline__ u64 seen_bits(const KvAttnArgs& a, int low, int i, const u64* tree, int ctx, int kb) {
     u64 x = up_to(a.tree ? ctx - 1 : ctx + i, kb) & (~up_to(low - 1, kb) | up_to(a.sinks - 1, kb));

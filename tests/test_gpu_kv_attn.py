@@ -435,6 +435,24 @@ def test_tree_with_masks_of_the_callers_own():
     assert torch.all(out[1, 5] == 0)
 
 
+@pytest.mark.parametrize("N", [3, 70])
+def test_tree_positions_that_no_tree_has(N):
+    """A position outside ctx .. ctx + N - 1 counts as the nearest of these."""
+    g = gen(78 + N)
+    n, window, sinks = 300, 90, 3
+    c = filled(g, 14, 2, 64, n + N, 1)
+    q = randn(g, 1, N, 14, 64)
+    far = torch.randint(n - 2 * N, n + 3 * N, (1, N), generator=g, device="cuda").int()
+    far[0, 0], far[0, 1], far[0, 2] = 2 ** 31 - 1, -2 ** 31, n + N
+    words = torch.zeros((1, N, (N + 63) // 64), dtype=torch.int64, device="cuda")        # (no node sees another, or itself)
+    dev = torch.tensor([n], dtype=torch.int32, device="cuda")
+    out, ws = torch.full_like(q, 7.0), torch.empty(1 << 26, dtype=torch.uint8, device="cuda")
+    binding.check(binding.kv_attn_tree(c.desc, q, dev, n, words, far, window, sinks, 1, N, 14, c.k, c.v, out, ws, ws.numel()))
+    torch.cuda.synchronize()
+    seen = O.seen_from(far[0].clamp(n, n + N - 1), torch.arange(n, device="cuda"), window, sinks)
+    check(out[0], q[0], c.k[0, :, :n], c.v[0, :, :n], seen, None, f"positions of {N} nodes")
+
+
 def test_a_chain_is_a_prefill_and_single_steps():
     """The same tokens as a chain of drafts, as a prefill behind the same context and one by one: the same values up to the
     roundings (all three within the oracle's bound)."""

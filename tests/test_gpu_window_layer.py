@@ -216,6 +216,45 @@ def test_refusals_and_sizes():
     lay.close()
 
 
+def test_one_mask_for_a_stack_of_windows():
+    """Layers of different windows share a mask only where no window hides a node: those are the layers one by one, the
+    others are refused."""
+    cfg, w = host_layer("tiny")
+    layers = [binding.Layer(cfg, w) for _ in range(3)]
+    T, hist = 6, 40
+    caches = [filled(cfg, layers[0], 1, seed=i) for i in range(3)]
+    x = inputs(cfg, T)
+    tree = binding.DraftTree(1, T)
+    tree.plan(torch.tensor([[-1, 0, 0, 1, 3, 4]], dtype=torch.int32, device="cuda"), torch.tensor([hist], dtype=torch.int32, device="cuda"))
+    stack = binding.Stack(layers)
+    y = torch.empty_like(x)
+
+    def run():
+        stack.verify_tree(x, tree.pos[0], tree.mask[0], hist, [k[0] for k, _ in caches], [v[0] for _, v in caches], y)
+
+    for lay, window in zip(layers, (0, 6, 17)):
+        lay.set_window(window, 2)
+    run()
+    a, b = x, torch.empty_like(x)
+    for lay, (k, v) in zip(layers, caches):
+        lay.verify_tree(a, tree.pos[0], tree.mask[0], hist, k[0], v[0], b)
+        a, b = b, torch.empty_like(x)
+    torch.cuda.synchronize()
+    assert_parity(y.cpu().numpy(), a.cpu().numpy(), "stack of windows")
+    for windows in (((0, 0), (5, 2), (0, 0)), ((5, 2), (5, 1), (5, 2)), ((5, 2), (5, 2), (4, 2)), ((5, 2), (5, 2), (6, 2))):
+        for lay, (window, sinks) in zip(layers, windows):
+            lay.set_window(window, sinks)
+        with pytest.raises(binding.W4Error) as e:
+            run()
+        assert e.value.code == binding.W4_EUNSUPPORTED
+    for lay in layers:
+        lay.set_window(5, 2)
+    run()
+    torch.cuda.synchronize()
+    for lay in layers:
+        lay.close()
+
+
 def test_windowed_decode_without_allocation_and_captured():
     cfg, lay = layer("tiny")
     lay.set_window(20, 2)

@@ -96,6 +96,14 @@ def test_attention_refusals(call):
         assert call(pos=0) == B.W4_EINVAL and "positions" in B.layer_last_error()
 
 
+@pytest.mark.parametrize("call", [decode, tree])
+def test_more_pairs_than_a_launch_takes(call):
+    """2^21 sequences times kv heads."""
+    d = desc(1 << 16, synth.replace(CFG, n_kv_heads=64, n_heads=64, max_seq=300))
+    assert call(d, b=1 << 15, nq=64, n=0) == B.W4_EWORKSPACE
+    assert call(d, b=(1 << 15) + 1, nq=64) == B.W4_ECAPACITY and "kv heads" in B.layer_last_error()
+
+
 @pytest.mark.parametrize("stage", [0, 1, 2, 3])
 def test_workspace_sizes(stage):
     d = desc(rows=64)
