@@ -968,7 +968,7 @@ class KVCache(_OnDevice):
             raise ValueError("either both caches or none")
         if k is None:
             k, v = (torch.empty(shape, dtype=torch.bfloat16, device="cuda") for _ in range(2))
-        self.n_heads, self.k, self.v = cfg.n_heads, k, v
+        self.n_heads, self._k, self._v = cfg.n_heads, k, v
         self._setup(k.device, "the cache")
         for t, what in ((k, "k"), (v, "v")):
             if tuple(t.shape) != shape or t.dtype not in self._bits16 or t.device != k.device or t.device.type != "cuda":
@@ -985,6 +985,14 @@ class KVCache(_OnDevice):
         self._no_ws = (self._kp, 0)
         self._head = (cfg.n_kv_heads, cfg.head_dim)
         self._q_head = (cfg.n_heads, cfg.head_dim)
+
+    @property
+    def k(self):
+        return self._k
+
+    @property
+    def v(self):
+        return self._v
 
     def append(self, k_new, v_new, slot_start, stream=None):
         """k_new, v_new [B][T][n_kv_heads][head_dim] into slots slot_start[b] .. + T - 1 (host integers).  For caches whose
@@ -1045,8 +1053,8 @@ class KVCache(_OnDevice):
         if tree.window is None:
             raise ValueError("the tree has no plan yet")
         max_ctx, st = self._i32(max_ctx, "max_ctx"), self._on(stream)
-        self._attend(_lib.kv_attn_tree, (self._desc_ref, qp, cp, max_ctx, tree.mask.data_ptr(), tree.pos.data_ptr(), tree.window,
-                                         tree.sinks, B, N, self.n_heads, self._kp, self._vp, op), STAGE_TREE, B, N, max_ctx, st)
+        self._attend(_lib.kv_attn_tree, (self._desc_ref, qp, cp, max_ctx, *tree._plan_out, tree.window, tree.sinks, B, N, self.n_heads,
+                                         self._kp, self._vp, op), STAGE_TREE, B, N, max_ctx, st)
 
 
 class DraftTree(_OnDevice):
@@ -1061,24 +1069,32 @@ class DraftTree(_OnDevice):
         if batch < 1 or not 1 <= nodes <= W4_TREE_MAX:
             raise ValueError(f"trees of {nodes} nodes for {batch} sequences")
         self.batch, self.nodes, self.window, self.sinks = batch, nodes, None, 0
-        self.mask = torch.zeros((batch, nodes, (nodes + 63) // 64), dtype=torch.int64, device="cuda")
-        self.pos, self.path = (torch.zeros((batch, nodes), dtype=torch.int32, device="cuda") for _ in range(2))
-        self.n_path, self.next_tokens = (torch.zeros(batch, dtype=torch.int32, device="cuda") for _ in range(2))
-        self._setup(self.mask.device, "the tree")
+        self._shape, self._rows = (batch, nodes), (batch,)
+        self._mask = torch.zeros((batch, nodes, (nodes + 63) // 64), dtype=torch.int64, device="cuda")
+        self._pos, self._path = (torch.zeros((batch, nodes), dtype=torch.int32, device="cuda") for _ in range(2))
+        self._n_path, self._next_tokens = (torch.zeros(batch, dtype=torch.int32, device="cuda") for _ in range(2))
+        # what every call needs, in the form that costs a call least
+        self._plan_out = (self._mask.data_ptr(), self._pos.data_ptr())
+        self._accept_out = (self._path.data_ptr(), self._n_path.data_ptr(), self._next_tokens.data_ptr())
+        self._setup(self._mask.device, "the tree")
         check(kv_attn_load())
 
+    mask = property(lambda self: self._mask)
+    pos = property(lambda self: self._pos)
+    path = property(lambda self: self._path)
+    n_path = property(lambda self: self._n_path)
+    next_tokens = property(lambda self: self._next_tokens)
+
     def plan(self, parents, ctx_lens, window: int = 0, sinks: int = 0, stream=None):
-        B, N = self.batch, self.nodes
-        pp, cp = self._ints(parents, (B, N), "parents"), self._ints(ctx_lens, (B,), "ctx_lens")
+        pp, cp = self._ints(parents, self._shape, "parents"), self._ints(ctx_lens, self._rows, "ctx_lens")
         window, sinks = self._i32(window, "window"), self._i32(sinks, "sinks")
-        check(_lib.tree_plan(pp, cp, B, N, window, sinks, self.mask.data_ptr(), self.pos.data_ptr(), self._on(stream)))
+        check(_lib.tree_plan(pp, cp, self.batch, self.nodes, window, sinks, *self._plan_out, self._on(stream)))
         self.window, self.sinks = window, sinks
 
     def accept(self, parents, tokens, picks, stream=None):
-        B, N = self.batch, self.nodes
-        pp, tp, kp = (self._ints(t, (B, N), what) for t, what in ((parents, "parents"), (tokens, "tokens"), (picks, "picks")))
-        check(_lib.tree_accept(pp, tp, kp, B, N, self.path.data_ptr(), self.n_path.data_ptr(), self.next_tokens.data_ptr(),
-                               self._on(stream)))
+        shape = self._shape
+        pp, tp, kp = self._ints(parents, shape, "parents"), self._ints(tokens, shape, "tokens"), self._ints(picks, shape, "picks")
+        check(_lib.tree_accept(pp, tp, kp, self.batch, self.nodes, *self._accept_out, self._on(stream)))
 
     def keep(self, caches, ctx_lens, stream=None):
         """Moves the path's rows together in the KVCaches of the model's layers (one layout, none twice)."""
@@ -1089,8 +1105,8 @@ class DraftTree(_OnDevice):
         for c in caches:
             if c._dev != self._dev:
                 raise ValueError(f"a cache is on {c._device}, the tree on {self._device}")
-            if bytes(c.desc) != bytes(d):
+            if c.desc is not d and bytes(c.desc) != bytes(d):
                 raise ValueError("the caches have different layouts")
-        kind, cp = ctypes.c_void_p * len(caches), self._ints(ctx_lens, (self.batch,), "ctx_lens")
-        check(_lib.kv_tree_keep(ctypes.byref(d), kind(*[c._kp for c in caches]), kind(*[c._vp for c in caches]), len(caches), cp,
-                                self.path.data_ptr(), self.n_path.data_ptr(), self.batch, self.nodes, self._on(stream)))
+        kind, cp = ctypes.c_void_p * len(caches), self._ints(ctx_lens, self._rows, "ctx_lens")
+        check(_lib.kv_tree_keep(caches[0]._desc_ref, kind(*[c._kp for c in caches]), kind(*[c._vp for c in caches]), len(caches), cp,
+                                *self._accept_out[:2], self.batch, self.nodes, self._on(stream)))

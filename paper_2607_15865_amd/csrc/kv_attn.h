@@ -37,6 +37,7 @@ struct KvAttnShape {
 };
 struct KvAttnPlan {
     bool few = false;        // the kernel of few rows
+    bool halves = false;     // many rows: tiles of 128, two waves for the keys of each
     int nsplit = 1;          // shares of a row tile's keys,
     int whole = 0;           // many rows: except for so many tiles
 };

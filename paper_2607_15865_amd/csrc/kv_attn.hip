@@ -396,7 +396,7 @@ constexpr int MW = 8;            // waves per block
 constexpr int MROWS = 32 * MW;   // rows per block
 constexpr int MKT = 64;          // keys per stage
 
-// One block: 256 rows of a (sequence, kv head), 32 to a wave, and a part of the
+// One block (KH = 1): 256 rows of a (sequence, kv head), 32 to a wave, and a part of the
 // stages of 64 keys that they see.  K and V go straight from memory into an LDS ring of four stages each, requested
 // three (V: two) stages ahead (through registers, one stage ahead, a stage took 2.1 us in place of 1.45 with part of
 // the chip at work).  A row's 16-byte chunks are swizzled by choosing which one a lane asks for, so that the operand
@@ -410,6 +410,11 @@ constexpr int MKT = 64;          // keys per stage
 // The weights are rounded to bf16, as the matrix units take them in one product (a pair would take half as much
 // again of a stage's matrix time): against 64 bits the outputs are off by 0.0023 in the norm, by 0.0017 with pairs,
 // which is the outputs' own rounding.
+//
+// KH = 2: 128 rows a block; the second half of the waves takes the second half of every stage's keys, and their states join
+// at the end.  With so few rows the time of a stage is what a wave goes through, here half: 1.1 us a stage, 1.3 with all CUs at
+// work, where the request for 32 KB by one CU, at 37 GB/s, takes 0.9.  16 sequences of 4000, 32 heads of 8, 32 drafts 74 -> 66 us; 1 of
+// 8190, 32 drafts 29.2 -> 27.1.
 //
 // Bound by the matrix units, the LDS reads (a wave reads a whole stage for its 32 rows: 128 bytes a cycle at the
 // full matrix rate) and the vector units about alike: a build without exponentials took 8% less, one without loads 8%, one
@@ -441,16 +446,17 @@ struct ManyTile {
     KeyTiles kt;
     int end, high_min, low_max, n;   // n: parts of the tile
 };
+template <int ROWS>
 __device__ __forceinline__ ManyTile many_tile(const KvAttnArgs& a, int order) {
     ManyTile t;
     const int units = a.B * a.nkv, unit = order % units;
     const int r = a.nq / a.nkv, R = a.N * r;
     t.b = unit / a.nkv;
     t.hk = unit % a.nkv;
-    t.q = (R + MROWS - 1) / MROWS - 1 - order / units;
+    t.q = (R + ROWS - 1) / ROWS - 1 - order / units;
     t.ctx = min(a.ctx_lens ? a.ctx_lens[t.b] : a.ctx_base, a.max_ctx);
     const int q = t.q;
-    const int i0 = q * MROWS / r, i1 = (min((q + 1) * MROWS, R) - 1) / r;
+    const int i0 = q * ROWS / r, i1 = (min((q + 1) * ROWS, R) - 1) / r;
     t.end = t.ctx < 0 ? -1 : a.tree ? t.ctx + a.N - 1 : t.ctx + i1;
     t.high_min = a.tree ? t.ctx - 1 : t.ctx + i0;
     t.low_max = window_low(a.tree ? t.ctx + a.N - 1 : t.ctx + i1, a.window);
@@ -459,9 +465,10 @@ __device__ __forceinline__ ManyTile many_tile(const KvAttnArgs& a, int order) {
     return t;
 }
 
-template <int D>
+template <int D, int KH>
 __global__ void __launch_bounds__(64 * MW) kv_attn_many_kernel(KvAttnArgs a) {
     constexpr int NS = D / 32, NF = D / 16, NCH = D / 8, NL = MKT * NCH / (64 * MW);     // loads per wave of K (of V)
+    constexpr int ROWS = MROWS / KH, GROUPS = MW / KH, T = 2 / KH;       // of the block; tiles of 32 keys of a wave's stage
     constexpr int STB = MKT * D * 2;
     extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
     unsigned char* const Ks = smem;                          // [4 stages][64 keys][D]
@@ -474,7 +481,7 @@ __global__ void __launch_bounds__(64 * MW) kv_attn_many_kernel(KvAttnArgs a) {
     const int r = a.nq / a.nkv, R = a.N * r;
     const int in = (int)blockIdx.x - a.whole;                // place among the parts
     const int part = in < 0 ? 0 : in / a.rest;
-    const ManyTile mt = many_tile(a, in < 0 ? blockIdx.x : a.whole + in % a.rest);
+    const ManyTile mt = many_tile<ROWS>(a, in < 0 ? blockIdx.x : a.whole + in % a.rest);
     if (part >= mt.n) return;
     const int st0 = (int)((long long)mt.kt.n * part / mt.n), st1 = (int)((long long)mt.kt.n * (part + 1) / mt.n);
     const long long base = mt.b * a.stride_b + mt.hk * a.stride_h;
@@ -506,8 +513,9 @@ __global__ void __launch_bounds__(64 * MW) kv_attn_many_kernel(KvAttnArgs a) {
 
     const int n = st1 - st0;
     // ---- queries: this lane's row, dims 16 f + 8 h .. + 7 of every fragment f
-    // (the two waves of a SIMD, one of either half of the block, take neighbouring rows)
-    const int grp = 2 * (wave % (MW / 2)) + wave / (MW / 2), row = mt.q * MROWS + grp * 32 + c, rowc = min(row, R - 1);
+    // (the two waves of a SIMD, one of either half of the block, take neighbouring rows, or the halves of the keys)
+    const int grp = KH == 2 ? wave % GROUPS : 2 * (wave % (MW / 2)) + wave / (MW / 2), half = KH == 2 ? wave / GROUPS : 0;
+    const int row = mt.q * ROWS + grp * 32 + c, rowc = min(row, R - 1);
     const uint16_t* qp = a.q + (((size_t)mt.b * a.N + rowc / r) * a.nq + mt.hk * r + rowc % r) * D + 8 * h;
     bf16x8 qf[NF];
 #pragma unroll
@@ -517,10 +525,10 @@ __global__ void __launch_bounds__(64 * MW) kv_attn_many_kernel(KvAttnArgs a) {
     u64* const mask = masks + (grp * 32 + c) * a.words;
     if (a.tree && h == 0)
         for (int w = 0; w < a.words; w++) mask[w] = a.tree[((size_t)mt.b * a.N + node) * a.words + w];
-    const bool active = mt.q * MROWS + grp * 32 < R;
+    const bool active = mt.q * ROWS + grp * 32 < R;
     const float sl = a.scale * LOG2E;
     // (of the wave's rows: what all see)
-    const int wi0 = min(mt.q * MROWS + grp * 32, R - 1) / r, wi1 = min(mt.q * MROWS + grp * 32 + 31, R - 1) / r;
+    const int wi0 = min(mt.q * ROWS + grp * 32, R - 1) / r, wi1 = min(mt.q * ROWS + grp * 32 + 31, R - 1) / r;
     const int w_low_max = window_low(a.tree ? mt.ctx + a.N - 1 : mt.ctx + wi1, a.window), w_high_min = a.tree ? mt.ctx - 1 : mt.ctx + wi0;
 
     f32x16 o[NS];
@@ -547,28 +555,28 @@ __global__ void __launch_bounds__(64 * MW) kv_attn_many_kernel(KvAttnArgs a) {
         if (tid < 4) vbad[tid] = 0;
 #pragma unroll
         for (int j = 0; j < NL; j++) *reinterpret_cast<u32x4*>(Vs + 3 * STB + (j * 64 * MW + tid) * 16) = u32x4{0u, 0u, 0u, 0u};
-        const int krow = key_perm(c);
-        f32x16 sc[2];
-        bf16x8 pf[4];
+        const int krow = key_perm(c) + 32 * half;
+        f32x16 sc[T];
+        bf16x8 pf[2 * T];
         auto scores = [&](int s) __attribute__((always_inline)) {
             const unsigned char* K = Ks + (s & 3) * STB;
-            sc[0] = f32x16{};
-            sc[1] = f32x16{};
+#pragma unroll
+            for (int t = 0; t < T; t++) sc[t] = f32x16{};
 #pragma unroll
             for (int f = 0; f < NF; f++)
 #pragma unroll
-                for (int t = 0; t < 2; t++) {
+                for (int t = 0; t < T; t++) {
                     const bf16x8 kf = *reinterpret_cast<const bf16x8*>(K + (32 * t + krow) * 2 * D + (((2 * f + h) ^ kswz(krow)) << 4));
                     sc[t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf, qf[f], sc[t], 0, 0, 0);
                 }
         };
         // this lane's 8 keys 16 ks + 8 h .. + 7, dim 32 i + c, by two transposing reads: lane x of a 16-lane group points at
         // key 16 ks + 8 h + x / 4 (+ 4), dims 32 i + 16 (c / 16) + 4 (x % 4) .. + 3
-        const int vrow = 8 * h + ((lane & 15) >> 2), vch = 2 * (c >> 4) + ((lane & 3) >> 1);
+        const int vrow = 32 * half + 8 * h + ((lane & 15) >> 2), vch = 2 * (c >> 4) + ((lane & 3) >> 1);
         auto output = [&](int s) __attribute__((always_inline)) {
             const __bf16* V = reinterpret_cast<const __bf16*>(Vs + (s & 3) * STB);
 #pragma unroll
-            for (int ks = 0; ks < 4; ks++)
+            for (int ks = 0; ks < 2 * T; ks++)
 #pragma unroll
                 for (int i = 0; i < NS; i++) {
                     const __bf16* p0 = V + (16 * ks + vrow) * D + (((4 * i + vch) ^ vswz(vrow)) << 3) + 4 * (lane & 1);
@@ -598,7 +606,7 @@ __global__ void __launch_bounds__(64 * MW) kv_attn_many_kernel(KvAttnArgs a) {
             }
         };
 #pragma unroll
-        for (int i = 0; i < 4; i++) pf[i] = bf16x8{};
+        for (int i = 0; i < 2 * T; i++) pf[i] = bf16x8{};
 #pragma unroll
         for (int f = 0; f < NF; f++) asm volatile("" : "+v"(qf[f]));         // (waited for here, not in the loop)
         wait_for(-1);                                        // (K of stage 0)
@@ -629,12 +637,12 @@ __global__ void __launch_bounds__(64 * MW) kv_attn_many_kernel(KvAttnArgs a) {
             constexpr int DS = 0x100, MFMA = 0x008;          // (classes of the scheduler's groups)
             __builtin_amdgcn_sched_group_barrier(DS, 6, 0);
 #pragma unroll
-            for (int j = 0; j < 2 * NF - 6; j++) {
+            for (int j = 0; j < T * NF - 6; j++) {
                 __builtin_amdgcn_sched_group_barrier(MFMA, 1, 0);
                 __builtin_amdgcn_sched_group_barrier(DS, 1, 0);
             }
 #pragma unroll
-            for (int j = 0; j < 4 * NS; j++) {
+            for (int j = 0; j < 2 * T * NS; j++) {
                 __builtin_amdgcn_sched_group_barrier(MFMA, 1, 0);
                 __builtin_amdgcn_sched_group_barrier(DS, 2, 0);
             }
@@ -647,14 +655,14 @@ __global__ void __launch_bounds__(64 * MW) kv_attn_many_kernel(KvAttnArgs a) {
             const int kb = tile_at(mt.kt, st0 + s) * MKT;
             if (kb + MKT - 1 > w_high_min || (kb < w_low_max && kb + MKT > a.sinks)) {
                 const u64 seen = seen_bits(a, low, node, mask, mt.ctx, kb) >> (8 * h);
-                const uint32_t lo = (uint32_t)seen, hi = (uint32_t)(seen >> 32);
+                const uint32_t lo = (uint32_t)(seen >> (32 * half)), hi = (uint32_t)(seen >> 32);
 #pragma unroll
-                for (int e = 0; e < 32; e++)
+                for (int e = 0; e < 16 * T; e++)
                     sc[e / 16][e % 16] = (e < 16 ? lo : hi) >> (16 * (e % 16 / 8) + e % 8) & 1 ? sc[e / 16][e % 16] : -INFINITY;
             }
             float top = fmaxf(sc[0][0], sc[0][1]);
 #pragma unroll
-            for (int e = 2; e < 32; e++) top = fmaxf(top, sc[e / 16][e % 16]);
+            for (int e = 2; e < 16 * T; e++) top = fmaxf(top, sc[e / 16][e % 16]);
             if (__builtin_amdgcn_ballot_w64(top * sl > m + 8.f) != 0) {
                 const float mn = fmaxf(m, max_halves(top) * sl);
                 const float alpha = exp2_hw(m - (mn == -INFINITY ? 0.f : mn));
@@ -670,7 +678,7 @@ __global__ void __launch_bounds__(64 * MW) kv_attn_many_kernel(KvAttnArgs a) {
             const bf16x2 one{(__bf16)1.f, (__bf16)1.f};
             float ls[2] = {0.f, 0.f};
 #pragma unroll
-            for (int e = 0; e < 32; e += 2) {
+            for (int e = 0; e < 16 * T; e += 2) {
                 const float x = exp2_hw(__builtin_fmaf(sc[e / 16][e % 16], sl, -mb));
                 const float y = exp2_hw(__builtin_fmaf(sc[e / 16][e % 16 + 1], sl, -mb));
                 const bf16x2 w = __builtin_convertvector(f32x2{x, y}, bf16x2);
@@ -689,6 +697,28 @@ __global__ void __launch_bounds__(64 * MW) kv_attn_many_kernel(KvAttnArgs a) {
         }
         if (wave < MW / 2) __syncthreads();
     }
+    if constexpr (KH == 2) {                                 // the second half's state joins the first's, over the rings
+        float* const st = reinterpret_cast<float*>(smem) + grp * M_NREG<D> * 64 + lane;
+        __syncthreads();
+        if (half) {
+            st[0] = m;
+            st[64] = l;
+#pragma unroll
+            for (int i = 0; i < NS; i++)
+#pragma unroll
+                for (int e = 0; e < 16; e++) st[(2 + i * 16 + e) * 64] = o[i][e];
+        }
+        __syncthreads();
+        if (half) return;
+        const float m2 = st[0], l2 = st[64], mn = fmaxf(m, m2), mb = mn == -INFINITY ? 0.f : mn;
+        const float s1 = l != l ? 1.f : exp2_hw(m - mb), s2 = l2 != l2 ? 1.f : exp2_hw(m2 - mb);         // (NaN stays)
+        m = mn;
+        l = s1 * l + s2 * l2;
+#pragma unroll
+        for (int i = 0; i < NS; i++)
+#pragma unroll
+            for (int e = 0; e < 16; e++) o[i][e] = s1 * o[i][e] + s2 * st[(2 + i * 16 + e) * 64];
+    }
     const float lt = l + __shfl_xor(l, 32, 64);
     if (mt.n == 1) {
         if (row >= R) return;
@@ -705,7 +735,7 @@ __global__ void __launch_bounds__(64 * MW) kv_attn_many_kernel(KvAttnArgs a) {
         return;
     }
     if (!active) return;
-    float* pp = a.part + ((size_t)in * MW + grp) * M_NREG<D> * 64 + lane;       // state of this part
+    float* pp = a.part + ((size_t)in * GROUPS + grp) * M_NREG<D> * 64 + lane;       // state of this part
     pp[0] = m;
     pp[64] = l;
 #pragma unroll
@@ -717,21 +747,22 @@ __global__ void __launch_bounds__(64 * MW) kv_attn_many_kernel(KvAttnArgs a) {
 // Merges the parts of the row tiles that have more than one: block (row tile, wave of it, 32 dims), a lane its
 // registers of them, eight parts of them asked for at once, joined in key order.  Bound by the chain of its loads and the states
 // (64 row tiles of 4 parts, 34 MB: 8 us, the caches hold most of them).
-template <int D>
+template <int D, int KH>
 __global__ void __launch_bounds__(64) kv_attn_many_merge_kernel(KvAttnArgs a) {
+    constexpr int ROWS = MROWS / KH;
     constexpr int CB = 8;                                    // parts requested together
     const int lane = threadIdx.x, wave = blockIdx.y, h = lane >> 5, c = lane & 31, e0 = 16 * blockIdx.z;
     const int r = a.nq / a.nkv, R = a.N * r;
-    const ManyTile mt = many_tile(a, a.whole + blockIdx.x);
-    const int row = mt.q * MROWS + wave * 32 + c;
-    if (mt.n == 1 || mt.q * MROWS + wave * 32 >= R) return;
+    const ManyTile mt = many_tile<ROWS>(a, a.whole + blockIdx.x);
+    const int row = mt.q * ROWS + wave * 32 + c;
+    if (mt.n == 1 || mt.q * ROWS + wave * 32 >= R) return;
     float M = -INFINITY, L = 0.f, acc[16] = {};
     for (int p0 = 0; p0 < mt.n; p0 += CB) {
         float mc[CB], lc[CB], v[CB][16];
 #pragma unroll
         for (int j = 0; j < CB; j++) {
             if (p0 + j >= mt.n) break;
-            const float* pp = a.part + (((size_t)(p0 + j) * a.rest + blockIdx.x) * MW + wave) * M_NREG<D> * 64 + lane;
+            const float* pp = a.part + (((size_t)(p0 + j) * a.rest + blockIdx.x) * (MW / KH) + wave) * M_NREG<D> * 64 + lane;
             mc[j] = pp[0];
             lc[j] = pp[64];
 #pragma unroll
@@ -782,21 +813,24 @@ static int tiles_of(const KvAttnShape& s, long long i0, long long i1) {
 //
 // Few rows: a wave takes w a tile, most of it the latency of its memory, and more with the chip full; a block takes 4 to begin
 // and end, a second share the merge launch; a CU draws 35 GB/s, the chip 5.3 TB/s from memory and 8.2 through its L2.
-// Many rows: 1.2 to 1.45 a stage of one block, more with the chip full, 5 to begin and end (6 where the last stages are a
+// Many rows: 1.2 to 1.45 a stage of one block (of 128 rows 1.1), more with the chip full, 5 to begin and end (6 where the last stages are a
 // tree's), and the parts' states, written and read back; the row tiles that are left after the last full round of the chip
 // may be cut alone.  Measured (few and many rows, each in its best number of parts): 32 heads of 8 of 128, 1 sequence of 8190 tokens,
-// 4, 8, 16, 32 and 64 drafts 17.3 and 22.3, 17.4 and 22.3, 21.7 and 25.8, 36 and 27.4, 55 and 31.4; 16 sequences of 4000, 4, 8 and 13
-// drafts 53.3 and 55.1, 58.5 and 55.0, 98.7 and 61.4; 28 heads of 4, 8001 queries, 876 row tiles in one part 477, the last 108 in
-// two 454.  Tiles of 32 rows in the kernel of few rows were within 3% of the better of these at best, of 64 rows slower.
+// 5, 8, 16, 32 and 64 drafts 17.2 and 24.0, 17.8 and 24.0, 28.0 and 25.1, 37 and 27.1, 55 and 30.1; 16 sequences of 4000, 5, 8, 13 and 24
+// drafts 58.5 and 55.7, 58.5 and 55.6, 98.8 and 58.1, 142 and 61.4 (many rows: 128 a block except with 5 and 8 of 16 sequences; 256 take
+// 60.3 and 66.7 with 13 and 24 drafts); 28 heads of 4, 8001 queries, 876 row tiles in one part 477, the last 108 in
+// two 454.  Tiles of 32 rows in the kernel of few rows were within 3% of the better of these at best, of 64 rows slower; so were
+// blocks of four waves with all of 64 rows and LDS rings of their own: a CU draws 37 GB/s however the loads are made.
 KvAttnPlan kv_attn_plan(const KvAttnShape& s) {
     KvAttnPlan best;
     double least = -1;
     const long long R = (long long)s.N * s.r, pairs = (long long)s.B * s.nkv;
     const bool wide = s.d == 128;
-    auto consider = [&](double us, bool few, long long n, long long whole) {
+    auto consider = [&](double us, bool few, long long n, long long whole, bool halves = false) {
         if (least >= 0 && us >= least) return;
         least = us;
         best.few = few;
+        best.halves = halves;
         best.nsplit = (int)n;
         best.whole = (int)whole;
     };
@@ -817,33 +851,37 @@ KvAttnPlan kv_attn_plan(const KvAttnShape& s) {
         }
     }
     if (R <= 16 || s.mask) return best;                      // (masks are the kernel of few rows' alone)
-    const long long nqt = (R + MROWS - 1) / MROWS, blocks = pairs * nqt;
-    double sum = 0;                                          // stages of a row tile: mean of some, and the longest
-    int longest = 0;
-    const int samples = (int)std::min<long long>(nqt, 8);
-    for (int j = 0; j < samples; j++) {
-        const long long q = nqt - 1 - j * (nqt - 1) / std::max(samples - 1, 1);
-        const long long i0 = s.tree ? 0 : q * MROWS / s.r, i1 = s.tree ? s.N - 1 : (std::min((q + 1) * MROWS, R) - 1) / s.r;
-        const int t = tiles_of<MKT>(s, i0, i1);
-        sum += t;
-        longest = std::max(longest, t);
-    }
-    const double mean = sum / samples, start = s.tree ? 6.0 : 5.0;
-    const double t1 = (wide ? 1.0 : 0.85) * (R <= 32 ? 1.2 : R <= 128 ? 1.4 : 1.45), tf = t1 * (R <= 128 ? 1.1 : 1.2);   // of one block, with the chip full
-    const double state = std::min<double>(R, MROWS) * (s.d + 4) * 8 / 6e6, floor = pairs * mean * MKT * s.d * 4 / 5.3e6;
-    auto rounds = [&](long long n, long long parts) {        // us of so many blocks, a row tile in n parts
-        const double t = t1 + (tf - t1) * std::min(1.0, std::max(0.0, (double)parts / (kCus / 2) - 1));
-        const double part = (double)((longest + n - 1) / n) * t + start;
-        if (parts <= kCus) return std::max(floor, part);
-        if (mean > 0.9 * longest) return std::max(floor, (double)((parts + kCus - 1) / kCus) * part);
-        return std::max(part, parts * (mean / n * t + start) / kCus + 0.5 * mean / n * t);      // (the longest go first)
-    };
-    const long long full = blocks / kCus * kCus;
-    for (long long n = 1; n <= longest && (n == 1 || (blocks - full) * n <= kManyParts); n = step(n)) {
-        if (n == 1) consider(rounds(1, blocks), false, 1, blocks);
-        if (n > 1 && blocks * n <= kManyParts) consider(rounds(n, blocks * n) + 3.0 + blocks * n * state, false, n, 0);
-        if (n > 1 && full > 0 && full < blocks)
-            consider(rounds(1, full) + rounds(n, (blocks - full) * n) + 3.0 + (blocks - full) * n * state, false, n, full);
+    for (int halves = 0; halves < 2; halves++) {
+        const long long rows = MROWS >> halves, nqt = (R + rows - 1) / rows, blocks = pairs * nqt;
+        double sum = 0;                                      // stages of a row tile: mean of some, and the longest
+        int longest = 0;
+        const int samples = (int)std::min<long long>(nqt, 8);
+        for (int j = 0; j < samples; j++) {
+            const long long q = nqt - 1 - j * (nqt - 1) / std::max(samples - 1, 1);
+            const long long i0 = s.tree ? 0 : q * rows / s.r, i1 = s.tree ? s.N - 1 : (std::min((q + 1) * rows, R) - 1) / s.r;
+            const int t = tiles_of<MKT>(s, i0, i1);
+            sum += t;
+            longest = std::max(longest, t);
+        }
+        const double mean = sum / samples, start = s.tree ? 6.0 : 5.0;
+        // us of a stage of one block, and with the chip full
+        const double t1 = halves ? (wide ? 1.0 : 0.95) * (R <= 32 ? 1.07 : 1.15) : (wide ? 1.0 : 0.85) * (R <= 32 ? 1.2 : R <= 128 ? 1.4 : 1.45);
+        const double tf = t1 * (halves ? 1.15 : R <= 128 ? 1.1 : 1.2);
+        const double state = std::min<double>(R, rows) * (s.d + 4) * 8 / 6e6, floor = pairs * mean * MKT * s.d * 4 / 5.3e6;
+        auto rounds = [&](long long n, long long parts) {    // us of so many blocks, a row tile in n parts
+            const double t = t1 + (tf - t1) * std::min(1.0, std::max(0.0, (double)parts / (kCus / 2) - 1));
+            const double part = (double)((longest + n - 1) / n) * t + start;
+            if (parts <= kCus) return std::max(floor, part);
+            if (mean > 0.9 * longest) return std::max(floor, (double)((parts + kCus - 1) / kCus) * part);
+            return std::max(part, parts * (mean / n * t + start) / kCus + 0.5 * mean / n * t);      // (the longest go first)
+        };
+        const long long full = blocks / kCus * kCus;
+        for (long long n = 1; n <= longest && (n == 1 || (blocks - full) * n <= kManyParts); n = step(n)) {
+            if (n == 1) consider(rounds(1, blocks), false, 1, blocks, halves);
+            if (n > 1 && blocks * n <= kManyParts) consider(rounds(n, blocks * n) + 3.0 + blocks * n * state, false, n, 0, halves);
+            if (n > 1 && full > 0 && full < blocks)
+                consider(rounds(1, full) + rounds(n, (blocks - full) * n) + 3.0 + (blocks - full) * n * state, false, n, full, halves);
+        }
     }
     return best;
 }
@@ -853,7 +891,7 @@ extern "C" void w4_kv_attn_plan(int B, int N, int nkv, int r, int d, int max_ctx
                                 int* nsplit, int* whole, size_t* part, size_t* bound) {
     const KvAttnShape s{B, N, nkv, r, d, max_ctx, window ? window : INT_MAX, window ? sinks : 0, tree != 0, false};
     const KvAttnPlan p = kv_attn_plan(s);
-    *few = p.few;
+    *few = p.halves ? 2 : p.few;
     *nsplit = p.nsplit;
     *whole = p.whole;
     *part = kv_attn_part_bytes(s, p);
@@ -864,7 +902,8 @@ size_t kv_attn_part_bytes(const KvAttnShape& s, const KvAttnPlan& p) {
     const size_t R = (size_t)s.N * s.r, pairs = (size_t)s.B * s.nkv;
     if (p.nsplit == 1) return 0;
     if (p.few) return pairs * p.nsplit * R * (s.d + 2) * 4;
-    return (pairs * ((R + MROWS - 1) / MROWS) - p.whole) * p.nsplit * MROWS * (s.d + 4) * 4;
+    const size_t rows = p.halves ? MROWS / 2 : MROWS;
+    return (pairs * ((R + rows - 1) / rows) - p.whole) * p.nsplit * rows * (s.d + 4) * 4;
 }
 
 // (either kernel's, where both may be taken; a product of what grows, and a constant)
@@ -884,19 +923,20 @@ static int launch_few(const KvAttnArgs& a, hipStream_t stream) {
     return hipGetLastError() == hipSuccess ? 0 : -1;
 }
 
-template <int D>
+template <int D, int KH>
 static int launch_many(const KvAttnArgs& a, hipStream_t stream) {
+    constexpr int ROWS = MROWS / KH;
     const int R = a.N * (a.nq / a.nkv);
-    const long long tiles = (long long)a.B * a.nkv * ((R + MROWS - 1) / MROWS);
+    const long long tiles = (long long)a.B * a.nkv * ((R + ROWS - 1) / ROWS);
     KvAttnArgs x = a;
     x.rest = (int)(tiles - a.whole);
     const long long blocks = a.whole + (long long)x.rest * a.nsplit;
     if (tiles > INT_MAX || x.rest < 0 || blocks > INT_MAX) return -1;
-    const size_t fixed = (size_t)8 * MKT * D * 2 + 4 * 8, lds = fixed + (size_t)MROWS * a.words * 8;
+    const size_t fixed = (size_t)8 * MKT * D * 2 + 4 * 8, lds = fixed + (size_t)ROWS * a.words * 8;
     static LdsLimit lim;                                     // (for the largest trees at once)
-    if (ensure_lds_limit(lim, (const void*)kv_attn_many_kernel<D>, fixed + (size_t)MROWS * (W4_TREE_MAX / 64) * 8)) return -1;
-    hipLaunchKernelGGL(kv_attn_many_kernel<D>, dim3((unsigned)blocks), dim3(64 * MW), lds, stream, x);
-    if (x.rest) hipLaunchKernelGGL(kv_attn_many_merge_kernel<D>, dim3(x.rest, MW, D / 32), dim3(64), 0, stream, x);
+    if (ensure_lds_limit(lim, (const void*)kv_attn_many_kernel<D, KH>, fixed + (size_t)ROWS * (W4_TREE_MAX / 64) * 8)) return -1;
+    hipLaunchKernelGGL((kv_attn_many_kernel<D, KH>), dim3((unsigned)blocks), dim3(64 * MW), lds, stream, x);
+    if (x.rest) hipLaunchKernelGGL((kv_attn_many_merge_kernel<D, KH>), dim3(x.rest, MW / KH, D / 32), dim3(64), 0, stream, x);
     return hipGetLastError() == hipSuccess ? 0 : -1;
 }
 
@@ -909,7 +949,8 @@ int launch_kv_attn(const KvAttnArgs& args, size_t part_bytes, hipStream_t stream
     a.whole = p.whole;
     if (p.few) return a.d == 128 ? launch_few<128>(a, stream) : launch_few<64>(a, stream);
     if (a.mask) return -1;
-    return a.d == 128 ? launch_many<128>(a, stream) : launch_many<64>(a, stream);
+    if (p.halves) return a.d == 128 ? launch_many<128, 2>(a, stream) : launch_many<64, 2>(a, stream);
+    return a.d == 128 ? launch_many<128, 1>(a, stream) : launch_many<64, 1>(a, stream);
 }
 
 int load_kv_attn() { return load_code((const void*)kv_attn_few_kernel<128>); }

@@ -263,7 +263,8 @@ def test_prefill(nq, nkv, d, T, hist, window, sinks):
 
 @pytest.mark.parametrize("window,sinks", [(0, 0), (1024, 4), (4096, 0), (130, 500)])
 @pytest.mark.parametrize("nq,nkv,d,T,hist", [(14, 2, 64, 1500, 700), (32, 8, 128, 600, 5000), (28, 4, 128, 2011, 1001), (6, 1, 64, 40, 9000),
-                                             (28, 4, 128, 20, 7000), (40, 2, 128, 333, 1200), (4, 4, 128, 3000, 0)])
+                                             (28, 4, 128, 20, 7000), (40, 2, 128, 333, 1200), (4, 4, 128, 3000, 0), (14, 2, 64, 6000, 100),
+                                             (14, 2, 64, 500, 500)])
 def test_prefill_long(nq, nkv, d, T, hist, window, sinks):
     log(f"prefill heads {nq} {nkv} {d} T {T} hist {hist} window {window} sinks {sinks}")
     g = gen(T + hist + d + window)
@@ -281,7 +282,8 @@ def test_prefill_flat_and_sharp_scores(scale):
 
 
 @pytest.mark.parametrize("nq,nkv,d,T,hist,window,sinks", [(14, 2, 64, 300, 100, 0, 0), (32, 8, 128, 200, 300, 70, 3), (28, 4, 128, 12, 500, 200, 0),
-                                                          (28, 4, 128, 700, 0, 130, 4)])
+                                                          (28, 4, 128, 700, 0, 130, 4), (28, 4, 128, 2011, 101, 300, 4), (14, 2, 64, 1500, 300, 0, 0),
+                                                          (14, 2, 64, 1500, 300, 130, 500), (14, 2, 64, 500, 500, 0, 0)])
 def test_prefill_unseen_slots_may_hold_anything(nq, nkv, d, T, hist, window, sinks):
     """A NaN or infinity in a key or value reaches the rows that see its slot and no others, which keep their bits."""
     log(f"prefill NaN heads {nq} {nkv} {d} T {T} hist {hist} window {window}")
@@ -385,7 +387,7 @@ def test_tree_long(nq, nkv, d, B, N, ctx, window, sinks):
     check_tree(c, q, run_tree(c, binding.DraftTree(B, N), q, parents, lens, window, sinks, max_ctx=ctx + 9), parents, lens, window, sinks)
 
 
-@pytest.mark.parametrize("nq,nkv,d,N", [(14, 2, 64, 8), (32, 8, 128, 40), (28, 4, 128, 100), (32, 8, 128, 2)])
+@pytest.mark.parametrize("nq,nkv,d,N", [(14, 2, 64, 8), (32, 8, 128, 40), (28, 4, 128, 100), (32, 8, 128, 2), (32, 8, 128, 256), (28, 4, 128, 256)])
 @pytest.mark.parametrize("window,sinks", [(0, 0), (90, 3)])
 def test_tree_unseen_slots_may_hold_anything(nq, nkv, d, N, window, sinks):
     """A value that is not finite in a node's or a context's slot reaches the nodes that see it and no others."""

@@ -19,7 +19,9 @@ from paper_2607_15865_amd import binding  # noqa: E402
 def plan(B, N, nkv, r, d, max_ctx, window, sinks, tree):
     out = [ctypes.c_int() for _ in range(3)] + [ctypes.c_size_t() for _ in range(2)]
     binding._lib.w4_kv_attn_plan(B, N, nkv, r, d, max_ctx, window, sinks, tree, *[ctypes.byref(x) for x in out])
-    return dict(zip(("few", "nsplit", "whole", "part", "bound"), [x.value for x in out]))
+    p = dict(zip(("kind", "nsplit", "whole", "part", "bound"), [x.value for x in out]))
+    p["few"], p["rows"] = p["kind"] == 1, {0: 256, 1: 16, 2: 128}[p.pop("kind")]
+    return p
 
 
 def shapes(seed, count):
@@ -48,10 +50,10 @@ def test_plans_fit_launches_and_workspaces(seed):
             if p["nsplit"] > 1:              # (the merge's grid)
                 assert R <= 65535
         else:
-            blocks = B * nkv * -(-R // 256)
+            blocks = B * nkv * -(-R // p["rows"])
             rest = blocks - p["whole"]
             assert 0 <= p["whole"] <= blocks and (p["nsplit"] > 1) == (rest > 0) and rest * p["nsplit"] <= 512, s
-            assert p["part"] == rest * p["nsplit"] * 256 * (d + 4) * 4
+            assert p["part"] == rest * p["nsplit"] * p["rows"] * (d + 4) * 4
 
 
 @pytest.mark.parametrize("seed", range(4))
@@ -67,7 +69,8 @@ def test_sizes_cover_smaller_calls(seed):
 
 
 def test_single_queries_and_long_prefills():
-    """A single query's rows are few, a long prompt's many; a window bounds the work however long the context is."""
-    assert plan(1, 1, 8, 4, 128, 100000, 0, 0, False)["few"] and not plan(1, 4000, 8, 4, 128, 0, 0, 0, False)["few"]
+    """A single query's rows are few, a long prompt's many, those of many sequences' drafts between; a window bounds the work however long the context is."""
+    assert plan(1, 1, 8, 4, 128, 100000, 0, 0, False)["few"] and plan(1, 4000, 8, 4, 128, 0, 0, 0, False)["rows"] == 256
+    assert plan(16, 13, 8, 4, 128, 4000, 0, 0, True)["rows"] == 128
     assert plan(1, 1, 8, 4, 128, 1 << 26, 256, 4, False) == plan(1, 1, 8, 4, 128, 1 << 20, 256, 4, False) | dict(
         bound=plan(1, 1, 8, 4, 128, 1 << 26, 256, 4, False)["bound"])
