@@ -58,7 +58,7 @@ __device__ __forceinline__ uint32_t out_pair(const KvAttnArgs& a, float x, float
         const f16 u = act_f16(x, bad), v = act_f16(y, bad);
         return (uint32_t)__builtin_bit_cast(uint16_t, u) | (uint32_t)__builtin_bit_cast(uint16_t, v) << 16;
     }
-    return (uint32_t)bf16_bits_rne(x) | (uint32_t)bf16_bits_rne(y) << 16;
+    return __builtin_bit_cast(uint32_t, __builtin_convertvector(f32x2{x, y}, bf16x2));      // (to the nearest, even)
 }
 
 // ---------------------------------------------------------------- what rows see
@@ -512,6 +512,15 @@ __global__ void __launch_bounds__(64 * MW) kv_attn_many_kernel(KvAttnArgs a) {
     };
 
     const int n = st1 - st0;
+    // K of stage s + 3 and V of stage s + 2, of the block's part
+    auto load_ahead = [&](int s) __attribute__((always_inline)) {
+        if (s + 3 < n) load(kc, klane, (s + 3 & 3) * STB, st0 + s + 3);
+        if (s + 2 < n) load(vc, vlane, (4 + (s + 2 & 3)) * STB, st0 + s + 2);
+    };
+    if (n > 0) {
+        load(kc, klane, 0, st0);
+        load_ahead(-2);
+    }
     // ---- queries: this lane's row, dims 16 f + 8 h .. + 7 of every fragment f
     // (the two waves of a SIMD, one of either half of the block, take neighbouring rows, or the halves of the keys)
     const int grp = KH == 2 ? wave % GROUPS : 2 * (wave % (MW / 2)) + wave / (MW / 2), half = KH == 2 ? wave / GROUPS : 0;
@@ -537,11 +546,6 @@ __global__ void __launch_bounds__(64 * MW) kv_attn_many_kernel(KvAttnArgs a) {
     float m = -INFINITY, l = 0.f;
 
     if (n > 0) {
-        // K of stage s + 3 and V of stage s + 2, of the block's part
-        auto load_ahead = [&](int s) __attribute__((always_inline)) {
-            if (s + 3 < n) load(kc, klane, (s + 3 & 3) * STB, st0 + s + 3);
-            if (s + 2 < n) load(vc, vlane, (4 + (s + 2 & 3)) * STB, st0 + s + 2);
-        };
         // waits until K of stage s + 1 and V of stage s are there, after load_ahead(s)
         auto wait_for = [&](int s) __attribute__((always_inline)) {
             if (s + 3 < n) lds_load_wait<4 * NL>();
@@ -549,9 +553,6 @@ __global__ void __launch_bounds__(64 * MW) kv_attn_many_kernel(KvAttnArgs a) {
             else if (s + 2 == n) lds_load_wait<NL>();
             else lds_load_wait<0>();
         };
-        load(kc, klane, 0, st0);
-        load_ahead(-2);
-        load_ahead(-1);
         if (tid < 4) vbad[tid] = 0;
 #pragma unroll
         for (int j = 0; j < NL; j++) *reinterpret_cast<u32x4*>(Vs + 3 * STB + (j * 64 * MW + tid) * 16) = u32x4{0u, 0u, 0u, 0u};
@@ -609,6 +610,7 @@ __global__ void __launch_bounds__(64 * MW) kv_attn_many_kernel(KvAttnArgs a) {
         for (int i = 0; i < 2 * T; i++) pf[i] = bf16x8{};
 #pragma unroll
         for (int f = 0; f < NF; f++) asm volatile("" : "+v"(qf[f]));         // (waited for here, not in the loop)
+        load_ahead(-1);
         wait_for(-1);                                        // (K of stage 0)
         __syncthreads();
         // The second half of the waves runs half a stage behind: vector work where the others multiply.  What it loads has
@@ -698,26 +700,31 @@ __global__ void __launch_bounds__(64 * MW) kv_attn_many_kernel(KvAttnArgs a) {
         if (wave < MW / 2) __syncthreads();
     }
     if constexpr (KH == 2) {                                 // the second half's state joins the first's, over the rings
-        float* const st = reinterpret_cast<float*>(smem) + grp * M_NREG<D> * 64 + lane;
+        f32x4* const st = reinterpret_cast<f32x4*>(smem) + grp * (1 + 4 * NS) * 64 + lane;
         __syncthreads();
         if (half) {
-            st[0] = m;
-            st[64] = l;
+            st[0] = f32x4{m, l, 0.f, 0.f};
 #pragma unroll
             for (int i = 0; i < NS; i++)
 #pragma unroll
-                for (int e = 0; e < 16; e++) st[(2 + i * 16 + e) * 64] = o[i][e];
+                for (int e = 0; e < 16; e += 4)
+                    st[(1 + 4 * i + e / 4) * 64] = f32x4{o[i][e], o[i][e + 1], o[i][e + 2], o[i][e + 3]};
         }
         __syncthreads();
         if (half) return;
-        const float m2 = st[0], l2 = st[64], mn = fmaxf(m, m2), mb = mn == -INFINITY ? 0.f : mn;
+        const f32x4 s0 = st[0];
+        const float m2 = s0[0], l2 = s0[1], mn = fmaxf(m, m2), mb = mn == -INFINITY ? 0.f : mn;
         const float s1 = l != l ? 1.f : exp2_hw(m - mb), s2 = l2 != l2 ? 1.f : exp2_hw(m2 - mb);         // (NaN stays)
         m = mn;
         l = s1 * l + s2 * l2;
 #pragma unroll
         for (int i = 0; i < NS; i++)
 #pragma unroll
-            for (int e = 0; e < 16; e++) o[i][e] = s1 * o[i][e] + s2 * st[(2 + i * 16 + e) * 64];
+            for (int j = 0; j < 4; j++) {
+                const f32x4 x = st[(1 + 4 * i + j) * 64];
+#pragma unroll
+                for (int e = 0; e < 4; e++) o[i][4 * j + e] = s1 * o[i][4 * j + e] + s2 * x[e];
+            }
     }
     const float lt = l + __shfl_xor(l, 32, 64);
     if (mt.n == 1) {
