@@ -536,8 +536,9 @@ int kv4_read(const kv4_desc* desc, const void* k_cache, const void* v_cache,
  * kv4_attn_workspace_size: stage 0 or 1 for the prefill, 2 for the decode, as in
  * layer_workspace_size; 0 for invalid arguments.  It does not decrease with B, T
  * or max_ctx.
- * Errors: W4_EINVAL, W4_ECAPACITY (B > desc->batch, slots beyond max_seq),
- * W4_EUNSUPPORTED (heads), W4_EWORKSPACE, W4_EHIP. */
+ * Errors: W4_EINVAL, W4_ECAPACITY (B > desc->batch, slots beyond max_seq, more than 2^26 queries
+ * times heads in a sequence or 2^30 in the batch, more than 2^21 sequences times kv heads),
+ * W4_EUNSUPPORTED (heads, head_dim, N), W4_EWORKSPACE, W4_EHIP. */
 size_t kv4_attn_workspace_size(const kv4_desc* desc, int32_t n_heads, int32_t stage, int32_t B, int32_t T,
                                int32_t max_ctx);
 int kv4_attn_decode(const kv4_desc* desc, const void* q, const int32_t* ctx_lens, int32_t max_ctx,
@@ -669,7 +670,8 @@ int kv_append_step(const kv_desc* desc, void* k_cache, void* v_cache, const void
  * (host arrays, at most 1024; one pair per layer, all in the layout of *desc and none twice).  The context is then ctx_lens[b] +
  * n_path[b] tokens.  The other slots keep what they held.  Sequences with ctx_lens[b] < 0 are left alone; so
  * is a move whose slots are not below max_seq or whose node is not in t .. N-1.
- * Errors: W4_EINVAL, W4_EUNSUPPORTED (N, *desc as for the attention calls), W4_ECAPACITY (B beyond the cache's batch or 65535, n_caches), W4_EHIP. */
+ * Errors: W4_EINVAL, W4_EUNSUPPORTED (N, *desc as for the attention calls), W4_ECAPACITY (B beyond the
+ * cache's batch or 65535, n_caches), W4_EHIP. */
 int tree_plan(const int32_t* parents, const int32_t* ctx_lens, int32_t B, int32_t N, int32_t window, int32_t sinks,
               uint64_t* tree_mask, int32_t* pos, void* stream);
 int tree_accept(const int32_t* parents, const int32_t* tokens, const int32_t* picks, int32_t B, int32_t N,

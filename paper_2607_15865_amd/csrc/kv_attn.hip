@@ -123,7 +123,7 @@ constexpr int FW = 8;            // waves per block
 // than 5 (weights below e^5); the weights are multiplied as bf16 pairs hi + lo: the matrix units
 // have the time, and the weights of short contexts keep 16 bits.
 //
-// Bound by the cache read: 32 rows of 28 heads of 4 of 128, windows of 8192 (538 MB), 96 us, 5.6 TB/s; alone on the chip a wave
+// Bound by the cache read: 32 rows of 28 heads of 4 of 128, windows of 8192 (538 MB on average), 96 us, about 5.5 TB/s; alone on the chip a wave
 // takes 2.1 us a tile (d = 64: 1.2).  Tiles requested two ahead need more registers than there are: 114 against 99 us.
 template <int D>
 __global__ void __launch_bounds__(64 * FW) kv_attn_few_kernel(KvAttnArgs a) {
@@ -418,7 +418,7 @@ constexpr int MKT = 64;          // keys per stage
 //
 // Bound by the matrix units, the LDS reads (a wave reads a whole stage for its 32 rows: 128 bytes a cycle at the
 // full matrix rate) and the vector units about alike: a build without exponentials took 8% less, one without loads 8%, one
-// without the second product 20%.  8001 queries of 28 heads of 4 of 128 behind 2999, window 4096: 455 us, 1.02 PFLOP/s (a
+// without the second product 20%.  8001 queries of 28 heads of 4 of 128 behind 2999, window 4096: 452 us, 1.02 PFLOP/s (a
 // library product of two 8192^2 bf16 matrices 1.25); 512 of 32 heads of 8 behind 8192 47 us.  A stage takes 1.2 us with one
 // wave's rows, 1.45 with all, 1.9 with all CUs at work.
 template <int D>
@@ -474,7 +474,7 @@ __global__ void __launch_bounds__(64 * MW) kv_attn_many_kernel(KvAttnArgs a) {
     unsigned char* const Ks = smem;                          // [4 stages][64 keys][D]
     unsigned char* const Vs = smem + 4 * STB;
     u64* const vbad = reinterpret_cast<u64*>(smem + 8 * STB);   // [4] keys of V that are not finite, by stage % 4
-    u64* const masks = vbad + 4;                             // [256 rows][words] of a tree
+    u64* const masks = vbad + 4;                             // [ROWS][words] of a tree
     const int tid = threadIdx.x, lane = tid & 63;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int h = lane >> 5, c = lane & 31;

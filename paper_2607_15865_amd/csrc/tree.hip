@@ -3,7 +3,7 @@
 // together.  All of them move little and are bound by their chains of dependent
 // memory and LDS accesses: trees of 8, 64 and 129 nodes take 2.0, 4.0 and 4.8 us to
 // plan; 16 sequences of 64 nodes 3.8 to accept, 3.4 to append to a layer of 8 heads of
-// 128 (8.4 MB moved, 2.5 TB/s, start and end of a launch in it), and 6.3 to keep in four layers.
+// 128 (8.4 MB moved, 2.5 TB/s, start and end of a launch in it), and 7.2 to keep in four layers.
 #include <algorithm>
 
 #include "kv_attn.h"
