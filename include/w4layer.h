@@ -536,9 +536,8 @@ int kv4_read(const kv4_desc* desc, const void* k_cache, const void* v_cache,
  * kv4_attn_workspace_size: stage 0 or 1 for the prefill, 2 for the decode, as in
  * layer_workspace_size; 0 for invalid arguments.  It does not decrease with B, T
  * or max_ctx.
- * Errors: W4_EINVAL, W4_ECAPACITY (B > desc->batch, slots beyond max_seq, more than 2^26 queries
- * times heads in a sequence or 2^30 in the batch, more than 2^21 sequences times kv heads),
- * W4_EUNSUPPORTED (heads, head_dim, N), W4_EWORKSPACE, W4_EHIP. */
+ * Errors: W4_EINVAL, W4_ECAPACITY (B > desc->batch, slots beyond max_seq),
+ * W4_EUNSUPPORTED (heads), W4_EWORKSPACE, W4_EHIP. */
 size_t kv4_attn_workspace_size(const kv4_desc* desc, int32_t n_heads, int32_t stage, int32_t B, int32_t T,
                                int32_t max_ctx);
 int kv4_attn_decode(const kv4_desc* desc, const void* q, const int32_t* ctx_lens, int32_t max_ctx,
@@ -619,7 +618,8 @@ int layer_set_window(layer_t layer, int32_t window, int32_t sinks);
  * kv_attn_workspace_size: 0 for invalid arguments; it does not decrease with B, T
  * or max_ctx, and serves every window.
  * Errors: W4_EINVAL, W4_ECAPACITY (B > desc->batch, slots beyond max_seq, more than 2^26 queries
- * times heads in a sequence or 2^30 in the batch, more than 2^21 sequences times kv heads), W4_EUNSUPPORTED (heads, head_dim, N), W4_EWORKSPACE, W4_EHIP. */
+ * times heads in a sequence or 2^30 in the batch, more than 2^21 sequences times kv heads),
+ * W4_EUNSUPPORTED (heads, head_dim, N), W4_EWORKSPACE, W4_EHIP. */
 #define W4_TREE_MAX 256
 size_t kv_attn_workspace_size(const kv_desc* desc, int32_t n_heads, int32_t stage, int32_t B, int32_t T,
                               int32_t max_ctx);
